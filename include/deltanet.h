@@ -47,13 +47,13 @@
 extern "C" {
 #endif
 
-typedef enum { DN_F32 = 0, DN_BF16 = 1 } dn_dtype;
+typedef enum { DN_F32 = 0, DN_BF16 = 1, DN_FP8 = 2 /* e4m3; pages of a cache only */ } dn_dtype;
 
 typedef enum {
     DN_OK = 0,
     DN_ERR_NULL = -1,        /* a required pointer is NULL */
     DN_ERR_SHAPE = -2,       /* a size is non-positive or inconsistent */
-    DN_ERR_UNSUPPORTED = -3, /* (dtype, d_k, d_v, chunk) has no compiled kernel */
+    DN_ERR_UNSUPPORTED = -3, /* (dtype, d_k, d_v, chunk), or the attention's (types, d, page size, rot), has no compiled kernel */
     DN_ERR_ALIGN = -4,       /* a data pointer is not 16-byte aligned */
     DN_ERR_WORKSPACE = -5,   /* workspace is NULL or too small */
     DN_ERR_CUSEQLENS = -6,   /* cu_seqlens_host is not 0 = c[0] <= c[1] <= ... <= c[N] = L */
@@ -224,6 +224,114 @@ int deltanet_gated_bwd_saved(const dn_shape *shape, const void *q, const void *k
                              const float *g, const void *d_o, const float *dfinal_state, void *dq, void *dk, void *dv,
                              float *dbeta, float *dg, float *dinitial_state, void *saved, size_t saved_bytes,
                              void *hip_stream);
+
+/*
+ * The attention layers of a hybrid model (the paper's hybrids put sliding-window attention between DeltaNet layers, or replace
+ * two of those by global attention): the pass between the projections and the attention, a paged cache of keys and
+ * values, and the attention of new tokens over that cache.  The conventions above hold (device pointers, caller-owned
+ * buffers, the caller's stream, validation before the first launch, 16-byte alignment); what differs:
+ *  - Batches are packed: T rows in all, row t of a tensor with H heads is [H, d] at t * stride elements, so that q, k and v may
+ *    be the column blocks of one projection's output.  A stride is at least H * d elements and a multiple of 16 bytes.
+ *    Outputs are contiguous.
+ *  - Query heads share key/value heads in equal groups: Hq is a multiple of Hkv, query head h reads head h / (Hq / Hkv).
+ *
+ * Norm and rotation.  Per token and head, with x a row of q or k and w the weight of the layer,
+ *
+ *     z = x / sqrt(mean(x^2) + eps) * w ,    y_a = z_a cos - z_b sin ,  y_b = z_b cos + z_a sin
+ *
+ * for the pairs (a, b) among the first `rot` elements; the others stay z.  Pairs are (i, i + rot / 2), or (2i, 2i + 1) if
+ * `interleaved`; cos_sin (fp32 [max_pos, rot]) holds for each position the rot / 2 cosines, then the rot / 2 sines, of those
+ * pairs' angles.  Arithmetic is fp32; y is rounded once.  Weights have the element type of q and k; a NULL weight is all ones.
+ * Positions outside [0, max_pos) read the table's nearest row.
+ * Compiled: d = 32, 64, 128, 256 in fp32 and bf16; rot a multiple of 16 up to d, or 0 (no rotation; cos_sin may be NULL).
+ */
+typedef struct {
+    int32_t rot, interleaved, max_pos;
+    float eps; /* finite, >= 0 */
+} dn_rope;
+
+typedef struct {
+    int32_t T, Hq, Hkv, d;
+    int32_t dtype;                       /* DN_F32 or DN_BF16 */
+    int32_t seq_len;                     /* without a positions array: row t has position t % seq_len */
+    int64_t q_stride, k_stride;          /* elements between rows of q and k */
+} dn_qk_shape;
+
+/* y for every row of q and of k.  positions: int32 [T], or NULL. */
+int deltanet_qk_norm_rope_fwd(const dn_qk_shape *shape, const dn_rope *rope, const void *q, const void *k,
+                              const void *q_weight, const void *k_weight, const float *cos_sin, const int32_t *positions,
+                              void *q_out, void *k_out, void *hip_stream);
+
+/*
+ * Its gradient: from dq_out [T, Hq, d], dk_out [T, Hkv, d] (contiguous, element type dtype) and the q, k, weights and positions of
+ * the forward call (nothing of which has to be kept), dq and dk in the element type, and the weights' gradients dq_weight,
+ * dk_weight (fp32 [d]; NULL where not wanted), summed over rows and heads in fp32 in an order that the sizes alone decide.
+ * dq may take the place of dq_out and dk that of dk_out.  Workspace: deltanet_qk_norm_rope_workspace_bytes.
+ */
+int deltanet_qk_norm_rope_workspace_bytes(const dn_qk_shape *shape, size_t *out_bytes);
+int deltanet_qk_norm_rope_bwd(const dn_qk_shape *shape, const dn_rope *rope, const void *q, const void *k,
+                              const void *dq_out, const void *dk_out, const void *q_weight, const void *k_weight,
+                              const float *cos_sin, const int32_t *positions, void *dq, void *dk, float *dq_weight,
+                              float *dk_weight, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * The paged cache of a layer: k_pages, v_pages [num_pages, Hkv, page_size, d] of type cache_dtype, which is the tensors' type
+ * or, for bf16 tensors, DN_FP8; then k_scale, v_scale (fp32 [num_pages, Hkv, page_size]) hold a factor per token and head,
+ * max |x| / 448 over the row, and the pages the e4m3 numbers nearest to x / factor, divided in fp32 (a row whose largest magnitude is under
+ * 2^-100 is held as zeros, factor 0; one with an infinity reads back as NaN).  page_size is 16, 32, 64, 128 or 256.
+ * Sequence n of the batch has kv_len[n] tokens in the cache, the new ones of this step included; its token p stands in page
+ * page_table[n][p / page_size], slot p % page_size (entries past its last page are not read).  Its new tokens are rows
+ * cu_q[n] .. cu_q[n + 1] - 1 of the packed tensors, the last of them at position kv_len[n] - 1.
+ * These arrays live on the device and are not validated: kernels work on contexts held inside [0, max_kv] and on the rows that
+ * lie in the tensors, drop writes to pages outside [0, num_pages) and read page 0 or num_pages - 1 in the place of such ones,
+ * so that a malformed array gives meaningless results but no access outside the buffers.
+ */
+typedef struct {
+    int32_t num_seqs, T;                 /* T: rows of q (k, v): the new tokens of all sequences */
+    int32_t Hq, Hkv, d;
+    int32_t dtype, cache_dtype;
+    int32_t page_size, num_pages, max_pages; /* max_pages: columns of page_table */
+    int32_t max_q, max_kv;               /* no sequence has more new tokens or a longer context (bounds suffice) */
+    const int32_t *cu_q;                 /* DEVICE int32 [num_seqs + 1] */
+    const int32_t *kv_len;               /* DEVICE int32 [num_seqs] */
+    const int32_t *page_table;           /* DEVICE int32 [num_seqs, max_pages] */
+    int64_t q_stride, k_stride, v_stride;
+} dn_paged_shape;
+
+typedef struct { void *k_pages, *v_pages; float *k_scale, *v_scale; } dn_paged_cache; /* scales: NULL unless DN_FP8 */
+
+/* Writes the new tokens' k and v to the cache.  Rows whose position is negative (a context shorter than the chunk) are not
+ * written.  q_stride, max_q and Hq are not used. d as for the attention below. */
+int deltanet_paged_append(const dn_paged_shape *shape, const void *k, const void *v, const dn_paged_cache *cache,
+                          void *hip_stream);
+
+/* The serving form of the norm and rotation: q_out [T, Hq, d] = y of q, and y of k, unrounded until it takes the pages' type, and v go
+ * to the cache, in one launch.  Positions are those in the sequences. */
+int deltanet_paged_norm_rope_append(const dn_paged_shape *shape, const dn_rope *rope, const void *q, const void *k,
+                                    const void *v, const void *q_weight, const void *k_weight, const float *cos_sin,
+                                    void *q_out, const dn_paged_cache *cache, void *hip_stream);
+
+/* Reads tokens back: rows cu_out[n] .. cu_out[n + 1] - 1 of k_out, v_out [T_out, Hkv, d] (element type dtype) become the last ones of
+ * sequence n's context (all of it, if that many).  A row in front of the context's start, or in no sequence, becomes zero. */
+int deltanet_paged_read(const dn_paged_shape *shape, const dn_paged_cache *cache, const int32_t *cu_out, int32_t T_out,
+                        void *k_out, void *v_out, void *hip_stream);
+
+/*
+ * Attention of the new tokens over the cache, which holds their own keys and values already: for the row at position p
+ *
+ *     o = sum_j exp(scale q . k_j) v_j / sum_j exp(scale q . k_j) ,   max(0, p - window + 1) <= j <= p
+ *
+ * (window = 0: the whole past).  A row without a position in its context (p < 0), or in no sequence, becomes zero.  Scores, the running maximum and sum and the output
+ * are held in fp32; in bf16 the probabilities enter the product with v as bf16, the cache's factors having been multiplied in
+ * before.  scale > 0.  Nothing at or past kv_len reaches a result, whatever the pages hold there (keys that a row's window or
+ * place hides are given the weight zero: an infinity or NaN among THOSE values reaches rows that are worked on together with one
+ * that sees it).  Deterministic: the order of every sum depends on the sizes and lengths alone.
+ * Compiled: d = 64, 128, 256 in bf16, with bf16 or DN_FP8 pages; d = 32, 64, 128 in fp32 (the precision mode).
+ * Workspace: deltanet_paged_attn_workspace_bytes (it depends on num_seqs, T, the heads, d, the types, max_q, max_kv and window).
+ */
+int deltanet_paged_attn_workspace_bytes(const dn_paged_shape *shape, int32_t window, size_t *out_bytes);
+int deltanet_paged_attn_fwd(const dn_paged_shape *shape, const void *q, const dn_paged_cache *cache, float scale,
+                            int32_t window, void *o, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
  * Measurement aid (not part of the method): per-kernel device time.  After

@@ -33,3 +33,13 @@ from .binding import (  # noqa: F401
     library_path,
     load_library,
 )
+from .attention import (  # noqa: F401
+    deltanet_paged_append,
+    deltanet_paged_attn_fwd,
+    deltanet_paged_attn_workspace_bytes,
+    deltanet_paged_cache,
+    deltanet_paged_norm_rope_append,
+    deltanet_paged_read,
+    deltanet_qk_norm_rope_bwd,
+    deltanet_qk_norm_rope_fwd,
+)

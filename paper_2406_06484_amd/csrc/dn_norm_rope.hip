@@ -1,0 +1,452 @@
+// The pass between an attention layer's projections and the attention: RMS norm of every head's query and key with the position
+// rotation, its gradient, and the serving forms that quantise k and v and write them to the paged cache, or read them back.
+//
+// With r = 1 / sqrt(mean(x^2) + eps), xhat = r x, z = xhat * w and the rotation R of a position (orthogonal on its pairs),
+//
+//     y = R z ;    backward:  dz = R^T dy ,  dw = sum dz * xhat ,  g = dz * w ,  dx = r (g - xhat mean(g * xhat)).
+//
+// Everything is bound by HBM (about ten operations per element of two or four bytes): each row is read once, in 16-byte words,
+// and written once.  A row of one head is D * sizeof(T) / 16 lanes wide, so a wave holds 64 * 16 / (D * sizeof(T)) heads of one
+// token at a time and its sums are lane swaps inside a row.  A wave stays with one token and one tensor (q, k or v is
+// blockIdx.y), so that the token's cosines and sines and the weight are fetched once for all heads.
+#include "dn_attn_device.hpp"
+
+namespace dn {
+
+template <typename T, int D> struct RowLayout {
+    static constexpr int V = 16 / (int)sizeof(T); // elements per lane
+    static constexpr int LPR = D / V;             // lanes per row
+    static constexpr int RPW = 64 / LPR;          // rows (heads) per wave and step
+};
+
+// What a lane needs to turn its V elements: out_i = own_i c_i + other_i s_i, where `other` is the pair's other element and the
+// sign is in s; the transposed turn is own_i c_i - other_i s_i.  Elements past the rotated ones have c = 1, s = 0.
+template <int V> struct Turn {
+    float c[V], s[V];
+    int from; // the lane that holds the others (halves); unused for neighbours
+    __device__ inline void load(const RowArgs &a, int e0, int pos) {
+        const int lane = threadIdx.x & 63, half = a.rot >> 1;
+        from = lane;
+#pragma unroll
+        for (int i = 0; i < V; ++i) { c[i] = 1.f; s[i] = 0.f; }
+        if (e0 >= a.rot) return;
+        pos = min(max(pos, 0), a.max_pos - 1);
+        const float *row = a.cs + (long)pos * a.rot;
+        if (a.interleaved) {
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                const float co = row[e0 / 2 + i], si = row[half + e0 / 2 + i];
+                c[2 * i] = c[2 * i + 1] = co;
+                s[2 * i] = -si; s[2 * i + 1] = si;
+            }
+            return;
+        }
+        const bool second = e0 >= half;
+        const int at = second ? e0 - half : e0;
+        from = second ? lane - half / V : lane + half / V;
+#pragma unroll
+        for (int i = 0; i < V; i += 4) {
+            const float4 co = *reinterpret_cast<const float4 *>(row + at + i), si = *reinterpret_cast<const float4 *>(row + half + at + i);
+            c[i] = co.x; c[i + 1] = co.y; c[i + 2] = co.z; c[i + 3] = co.w;
+            s[i] = second ? si.x : -si.x; s[i + 1] = second ? si.y : -si.y; s[i + 2] = second ? si.z : -si.z; s[i + 3] = second ? si.w : -si.w;
+        }
+    }
+    // the others of the elements in word w (the whole wave takes part)
+    template <typename T> __device__ inline void others(const RowArgs &a, const uint4 &w, const float (&own)[V], float (&o)[V]) const {
+        if (a.interleaved) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) o[i] = own[i ^ 1];
+            return;
+        }
+        uint4 x;
+        x.x = __shfl(w.x, from); x.y = __shfl(w.y, from); x.z = __shfl(w.z, from); x.w = __shfl(w.w, from);
+        unpack16<T>(x, o);
+    }
+};
+
+template <typename T, int V> __device__ inline void load_weight(const void *w, int e0, float (&f)[V]) {
+    if (w) unpack16<T>(*reinterpret_cast<const uint4 *>(static_cast<const T *>(w) + e0), f);
+    else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = 1.f;
+    }
+}
+
+// Loads of up to NB heads' words are requested before the first is worked on.
+constexpr int kRowBatch = 4;
+
+// y of the words w[], in fp32
+template <typename T, int D> struct NormTurn {
+    using L = RowLayout<T, D>;
+    float w[L::V], wo[L::V]; // the weight at the lane's elements and at their pairs' other ones
+    Turn<L::V> turn;
+    __device__ inline void load_w(const RowArgs &a, const void *weight, int e0) {
+        load_weight<T>(weight, e0, w);
+        if (e0 < a.rot && !a.interleaved) load_weight<T>(weight, e0 < (a.rot >> 1) ? e0 + (a.rot >> 1) : e0 - (a.rot >> 1), wo);
+        else {
+#pragma unroll
+            for (int i = 0; i < L::V; ++i) wo[i] = w[i ^ 1];
+        }
+    }
+    __device__ inline void apply(const RowArgs &a, const uint4 &x, float (&y)[L::V]) const {
+        float own[L::V], oth[L::V], ss = 0.f;
+        unpack16<T>(x, own);
+#pragma unroll
+        for (int i = 0; i < L::V; ++i) ss = fmaf(own[i], own[i], ss);
+        const float r = rsqrtf(lanes_sum<L::LPR>(ss) * (1.f / D) + a.eps);
+        turn.template others<T>(a, x, own, oth);
+#pragma unroll
+        for (int i = 0; i < L::V; ++i) {
+            const float z = own[i] * r * w[i];
+            y[i] = fmaf(z, turn.c[i], oth[i] * r * wo[i] * turn.s[i]);
+        }
+    }
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_norm_rope_fwd(RowArgs a) {
+    using L = RowLayout<T, D>;
+    const int lane = threadIdx.x & 63, e0 = (lane % L::LPR) * L::V, sub = lane / L::LPR;
+    const bool is_q = blockIdx.y == 0;
+    const int H = is_q ? a.Hq : a.Hkv;
+    const long stride = is_q ? a.q_stride : a.k_stride;
+    const T *in = static_cast<const T *>(is_q ? a.q : a.k);
+    T *out = static_cast<T *>(is_q ? a.q_out : a.k_out);
+    NormTurn<T, D> nt;
+    nt.load_w(a, is_q ? a.qw : a.kw, e0);
+    for (int t = blockIdx.x * 4 + (threadIdx.x >> 6); t < a.T; t += gridDim.x * 4) {
+        const T *row = in + t * stride;
+        T *to = out + (long)t * H * D;
+        nt.turn.load(a, e0, a.positions ? a.positions[t] : t % a.seq_len);
+        for (int h0 = 0; h0 < H; h0 += kRowBatch * L::RPW) {
+            uint4 x[kRowBatch];
+#pragma unroll
+            for (int b = 0; b < kRowBatch; ++b) {
+                const int h = h0 + b * L::RPW + sub;
+                x[b] = h < H ? *reinterpret_cast<const uint4 *>(row + h * D + e0) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int b = 0; b < kRowBatch; ++b) {
+                const int h = h0 + b * L::RPW + sub;
+                float y[L::V];
+                nt.apply(a, x[b], y);
+                if (h < H) *reinterpret_cast<uint4 *>(to + h * D + e0) = pack16<T>(y);
+            }
+        }
+    }
+}
+
+// Rows' gradients; every workgroup also leaves its sum of dz * xhat, which k_weight_grad adds up in the workgroups' order.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_norm_rope_bwd(RowArgs a) {
+    using L = RowLayout<T, D>;
+    __shared__ float part[4][D];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e0 = (lane % L::LPR) * L::V, sub = lane / L::LPR;
+    const bool is_q = blockIdx.y == 0;
+    const int H = is_q ? a.Hq : a.Hkv;
+    const long stride = is_q ? a.q_stride : a.k_stride;
+    const T *in = static_cast<const T *>(is_q ? a.q : a.k), *grad = static_cast<const T *>(is_q ? a.dq_out : a.dk_out);
+    T *out = static_cast<T *>(is_q ? a.q_out : a.k_out);
+    float w[L::V], dw[L::V];
+    load_weight<T>(is_q ? a.qw : a.kw, e0, w);
+#pragma unroll
+    for (int i = 0; i < L::V; ++i) dw[i] = 0.f;
+    Turn<L::V> turn;
+    for (int t = blockIdx.x * 4 + wave; t < a.T; t += gridDim.x * 4) {
+        const T *row = in + t * stride, *dy = grad + (long)t * H * D;
+        T *to = out + (long)t * H * D;
+        turn.load(a, e0, a.positions ? a.positions[t] : t % a.seq_len);
+        for (int h0 = 0; h0 < H; h0 += kRowBatch * L::RPW) {
+            uint4 x[kRowBatch], g[kRowBatch];
+#pragma unroll
+            for (int b = 0; b < kRowBatch; ++b) {
+                const int h = h0 + b * L::RPW + sub;
+                x[b] = h < H ? *reinterpret_cast<const uint4 *>(row + h * D + e0) : make_uint4(0, 0, 0, 0);
+                g[b] = h < H ? *reinterpret_cast<const uint4 *>(dy + h * D + e0) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int b = 0; b < kRowBatch; ++b) {
+                const int h = h0 + b * L::RPW + sub;
+                float xf[L::V], own[L::V], oth[L::V], ss = 0.f, gx = 0.f;
+                unpack16<T>(x[b], xf);
+                unpack16<T>(g[b], own);
+                turn.template others<T>(a, g[b], own, oth);
+#pragma unroll
+                for (int i = 0; i < L::V; ++i) {
+                    ss = fmaf(xf[i], xf[i], ss);
+                    own[i] = fmaf(own[i], turn.c[i], -oth[i] * turn.s[i]); // dz
+                    gx = fmaf(own[i] * w[i], xf[i], gx);
+                }
+                const float r = rsqrtf(lanes_sum<L::LPR>(ss) * (1.f / D) + a.eps);
+                const float m = lanes_sum<L::LPR>(gx) * r * (1.f / D);
+#pragma unroll
+                for (int i = 0; i < L::V; ++i) {
+                    const float xh = xf[i] * r;
+                    if (h < H) dw[i] = fmaf(own[i], xh, dw[i]);
+                    own[i] = r * fmaf(-xh, m, own[i] * w[i]);
+                }
+                if (h < H) *reinterpret_cast<uint4 *>(to + h * D + e0) = pack16<T>(own);
+            }
+        }
+    }
+    if (!a.partial) return;
+    // the wave's rows side by side, then the four waves
+#pragma unroll
+    for (int i = 0; i < L::V; ++i) {
+#pragma unroll
+        for (int m = L::LPR; m < 64; m <<= 1) dw[i] += __shfl_xor(dw[i], m);
+        if (sub == 0) part[wave][e0 + i] = dw[i];
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < D; e += 256)
+        a.partial[((long)blockIdx.x * 2 + blockIdx.y) * D + e] = (part[0][e] + part[1][e]) + (part[2][e] + part[3][e]);
+}
+
+// Sums the workgroups' partial weight gradients: a workgroup takes 16 elements, 16 threads each, every sixteenth partial per thread.
+__global__ __launch_bounds__(256) void k_weight_grad(RowArgs a, int D, int blocks) {
+    __shared__ float part[16][17];
+    const int e = blockIdx.x * 16 + (threadIdx.x & 15), of = threadIdx.x >> 4; // D is a multiple of 16
+    float *to = blockIdx.y == 0 ? a.dqw : a.dkw;
+    if (!to) return;
+    float s = 0.f;
+    for (int b = of; b < blocks; b += 16) s += a.partial[((long)b * 2 + blockIdx.y) * D + e];
+    part[of][threadIdx.x & 15] = s;
+    __syncthreads();
+    if (of == 0) {
+        s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += part[i][threadIdx.x];
+        to[e] = s;
+    }
+}
+
+// Where the wave's packed row t stands in the cache; false for a row that is not written.
+struct Slot { long base; int stride; }; // of head 0, in rows of d elements; rows between heads
+__device__ inline bool slot_of(const PagedArgs &c, int n, int pos, int Hkv, bool clamp, Slot *s) {
+    const int page = pos >> c.page_shift;
+    if (pos < 0 || page >= c.max_pages) return false;
+    int id = c.table[(long)n * c.max_pages + page];
+    if (clamp) id = min(max(id, 0), c.num_pages - 1);
+    else if (id < 0 || id >= c.num_pages) return false;
+    s->base = (((long)id * Hkv) << c.page_shift) + (pos & ((1 << c.page_shift) - 1));
+    s->stride = 1 << c.page_shift;
+    return true;
+}
+
+// Quantises the row that `y` is part of (LPR lanes) and writes it to the cache.
+template <typename T, typename CT, int D>
+__device__ inline void cache_row(void *pages, float *scale, long row, int e0, const float (&y)[RowLayout<T, D>::V], bool live) {
+    using L = RowLayout<T, D>;
+    if constexpr (__is_same(CT, fp8)) {
+        float amax = 0.f;
+#pragma unroll
+        for (int i = 0; i < L::V; ++i) amax = fmaxf(amax, fabsf(y[i]));
+        amax = lanes_max<L::LPR>(amax);
+        const bool none = amax < 0x1p-100f; // (its factor would leave the range of normal numbers)
+        const float s = none ? 0.f : __fdiv_rn(amax, 448.f), inv = none ? 0.f : __fdiv_rn(1.f, s);
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            // y / s to the last bit (the product with the rounded reciprocal, corrected once): rows of bf16 values meet ties often
+            const float x = y[i] * inv;
+            v[i] = fmaf(fmaf(-x, s, y[i]), inv, x);
+        }
+        if (live) {
+            *reinterpret_cast<uint2 *>(static_cast<unsigned char *>(pages) + row * D + e0) = to_fp8x8(v);
+            if (e0 == 0) scale[row] = s;
+        }
+    } else if (live) *reinterpret_cast<uint4 *>(static_cast<T *>(pages) + row * D + e0) = pack16<T>(y);
+}
+
+// New tokens: blockIdx.y = 0: k, 1: v, 2: q (only with NORM, which also normalises and rotates k).
+template <typename T, typename CT, int D, bool NORM>
+__global__ __launch_bounds__(256) void k_paged_append(RowArgs a, PagedArgs c) {
+    using L = RowLayout<T, D>;
+    const int lane = threadIdx.x & 63, e0 = (lane % L::LPR) * L::V, sub = lane / L::LPR;
+    const int t = blockIdx.x * 4 + (threadIdx.x >> 6), what = blockIdx.y;
+    if (t >= a.T) return;
+    const int H = what == 2 ? a.Hq : a.Hkv;
+    const long stride = what == 0 ? a.k_stride : what == 1 ? a.v_stride : a.q_stride;
+    const T *row = static_cast<const T *>(what == 0 ? a.k : what == 1 ? a.v : a.q) + t * stride;
+    uint4 x[kRowBatch];
+    auto fetch = [&](int h0) {
+#pragma unroll
+        for (int b = 0; b < kRowBatch; ++b) {
+            const int h = h0 + b * L::RPW + sub;
+            x[b] = h < H ? *reinterpret_cast<const uint4 *>(row + h * D + e0) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    const int hb = blockIdx.z * kRowBatch * L::RPW; // heads of this workgroup
+    if (hb >= H) return;
+    fetch(hb); // on its way while the row's place is looked up
+    NormTurn<T, D> nt;
+    if (NORM && what != 1) nt.load_w(a, what == 0 ? a.kw : a.qw, e0);
+    const int n = seq_of_row(c.cu, c.N, t);
+    int pos = -1;
+    Slot s{0, 0};
+    bool live = false;
+    if (n < c.N) {
+        pos = min(c.kv_len[n], c.max_kv) - c.cu[n + 1] + t;
+        live = slot_of(c, n, pos, a.Hkv, false, &s);
+    }
+    if (NORM && what != 1) nt.turn.load(a, e0, pos);
+    for (int h0 = hb;;) {
+#pragma unroll
+        for (int b = 0; b < kRowBatch; ++b) {
+            const int h = h0 + b * L::RPW + sub;
+            float y[L::V];
+            if (NORM && what != 1) nt.apply(a, x[b], y);
+            else unpack16<T>(x[b], y);
+            if (what == 2) {
+                if (h < H) *reinterpret_cast<uint4 *>(static_cast<T *>(a.q_out) + ((long)t * H + h) * D + e0) = pack16<T>(y);
+            } else
+                cache_row<T, CT, D>(what == 0 ? c.kp : c.vp, what == 0 ? c.ks : c.vs, s.base + (long)h * s.stride, e0, y, live && h < H);
+        }
+        h0 += gridDim.z * kRowBatch * L::RPW;
+        if (h0 >= H) break;
+        fetch(h0);
+    }
+}
+
+// Tokens read back: blockIdx.y = 0: k, 1: v; a.T rows of output, c.cu their offsets.
+template <typename T, typename CT, int D>
+__global__ __launch_bounds__(256) void k_paged_read(RowArgs a, PagedArgs c) {
+    using L = RowLayout<T, D>;
+    const int lane = threadIdx.x & 63, e0 = (lane % L::LPR) * L::V, sub = lane / L::LPR;
+    const int t = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t >= a.T) return;
+    const bool is_k = blockIdx.y == 0;
+    const void *pages = is_k ? c.kp : c.vp;
+    const float *scale = is_k ? c.ks : c.vs;
+    T *to = static_cast<T *>(is_k ? a.k_out : a.v_out) + (long)t * a.Hkv * D;
+    const int n = seq_of_row(c.cu, c.N, t);
+    Slot s{0, 0};
+    const bool live = n < c.N && slot_of(c, n, min(c.kv_len[n], c.max_kv) - c.cu[n + 1] + t, a.Hkv, true, &s);
+    for (int h0 = 0; h0 < a.Hkv; h0 += kRowBatch * L::RPW) {
+        uint4 x[kRowBatch];
+        float f[kRowBatch];
+#pragma unroll
+        for (int b = 0; b < kRowBatch; ++b) {
+            const int h = h0 + b * L::RPW + sub;
+            const long row = s.base + (long)h * s.stride;
+            x[b] = make_uint4(0, 0, 0, 0);
+            f[b] = 0.f;
+            if (live && h < a.Hkv) {
+                if constexpr (__is_same(CT, fp8)) {
+                    const uint2 w = *reinterpret_cast<const uint2 *>(static_cast<const unsigned char *>(pages) + row * D + e0);
+                    x[b].x = w.x; x[b].y = w.y;
+                    f[b] = scale[row];
+                } else x[b] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(pages) + row * D + e0);
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < kRowBatch; ++b) {
+            const int h = h0 + b * L::RPW + sub;
+            if constexpr (__is_same(CT, fp8)) {
+                float y[8];
+                from_fp8x8(make_uint2(x[b].x, x[b].y), y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] *= f[b];
+                x[b] = pack16<T>(y);
+            }
+            if (h < a.Hkv) *reinterpret_cast<uint4 *>(to + h * D + e0) = x[b];
+        }
+    }
+}
+
+namespace {
+
+int launch(const char *name, const void *fn, dim3 grid, void **args, hipStream_t stream) {
+    prof_begin(name, stream);
+    const hipError_t e = hipLaunchKernel(fn, grid, dim3(256), args, 0, stream);
+    prof_end(stream);
+    return (int)e;
+}
+
+// One workgroup per four tokens up to the number that fills the chip, from where on they loop (and keep the weight).
+int token_blocks(int T) { const int b = (T + 3) / 4; return b < 4096 ? b : 4096; }
+
+// f<T, D>() for the given (dtype, d); with a cache fp32 ends at 128 and bf16 starts at 64, as the attention does
+template <bool PAGED, typename F> int by_type(int dtype, int d, F f) {
+    if (dtype == 0) {
+        if (d == 32) return f.template operator()<float, 32>();
+        if (d == 64) return f.template operator()<float, 64>();
+        if (d == 128) return f.template operator()<float, 128>();
+        if constexpr (!PAGED) if (d == 256) return f.template operator()<float, 256>();
+    } else {
+        if constexpr (!PAGED) if (d == 32) return f.template operator()<bf16, 32>();
+        if (d == 64) return f.template operator()<bf16, 64>();
+        if (d == 128) return f.template operator()<bf16, 128>();
+        if (d == 256) return f.template operator()<bf16, 256>();
+    }
+    return (int)hipErrorInvalidValue;
+}
+
+struct FwdLaunch {
+    RowArgs a;
+    hipStream_t stream;
+    template <typename T, int D> int operator()() {
+        void *args[] = {&a};
+        return launch("k_norm_rope_fwd", reinterpret_cast<const void *>(k_norm_rope_fwd<T, D>), dim3(token_blocks(a.T), 2), args, stream);
+    }
+};
+struct BwdLaunch {
+    RowArgs a;
+    hipStream_t stream;
+    template <typename T, int D> int operator()() {
+        int blocks = norm_rope_bwd_blocks(a.T), d = D;
+        if (a.T > 0) {
+            void *args[] = {&a};
+            if (const int e = launch("k_norm_rope_bwd", reinterpret_cast<const void *>(k_norm_rope_bwd<T, D>), dim3(blocks, 2), args, stream)) return e;
+        }
+        if (!a.dqw && !a.dkw) return 0;
+        void *args[] = {&a, &d, &blocks};
+        return launch("k_weight_grad", reinterpret_cast<const void *>(k_weight_grad), dim3(D / 16, 2), args, stream);
+    }
+};
+// heads of one token are spread over workgroups where there are few tokens
+template <typename T, int D> int head_blocks(int T_rows, int H) {
+    const int per = kRowBatch * RowLayout<T, D>::RPW, most = (H + per - 1) / per;
+    return T_rows >= 1024 ? 1 : most;
+}
+struct AppendLaunch {
+    RowArgs a;
+    PagedArgs c;
+    bool fp8_pages, norm;
+    hipStream_t stream;
+    template <typename T, int D> int operator()() {
+        void *args[] = {&a, &c};
+        const void *fn;
+        if constexpr (sizeof(T) == 2) {
+            if (fp8_pages) fn = norm ? reinterpret_cast<const void *>(k_paged_append<T, fp8, D, true>) : reinterpret_cast<const void *>(k_paged_append<T, fp8, D, false>);
+            else fn = norm ? reinterpret_cast<const void *>(k_paged_append<T, T, D, true>) : reinterpret_cast<const void *>(k_paged_append<T, T, D, false>);
+        } else fn = norm ? reinterpret_cast<const void *>(k_paged_append<T, T, D, true>) : reinterpret_cast<const void *>(k_paged_append<T, T, D, false>);
+        return launch("k_paged_append", fn, dim3((a.T + 3) / 4, norm ? 3 : 2, head_blocks<T, D>(a.T, norm ? a.Hq : a.Hkv)), args, stream);
+    }
+};
+struct ReadLaunch {
+    RowArgs a;
+    PagedArgs c;
+    bool fp8_pages;
+    hipStream_t stream;
+    template <typename T, int D> int operator()() {
+        void *args[] = {&a, &c};
+        const void *fn = reinterpret_cast<const void *>(k_paged_read<T, T, D>);
+        if constexpr (sizeof(T) == 2)
+            if (fp8_pages) fn = reinterpret_cast<const void *>(k_paged_read<T, fp8, D>);
+        return launch("k_paged_read", fn, dim3((a.T + 3) / 4, 2), args, stream);
+    }
+};
+
+} // namespace
+
+int run_norm_rope_fwd(int dtype, int d, const RowArgs &a, hipStream_t stream) { return a.T == 0 ? 0 : by_type<false>(dtype, d, FwdLaunch{a, stream}); }
+int run_norm_rope_bwd(int dtype, int d, const RowArgs &a, hipStream_t stream) { return by_type<false>(dtype, d, BwdLaunch{a, stream}); }
+int run_paged_append(int dtype, int d, bool fp8, bool norm, const RowArgs &a, const PagedArgs &c, hipStream_t stream) {
+    return a.T == 0 ? 0 : by_type<true>(dtype, d, AppendLaunch{a, c, fp8, norm, stream});
+}
+int run_paged_read(int dtype, int d, bool fp8, const RowArgs &a, const PagedArgs &c, hipStream_t stream) {
+    return a.T == 0 ? 0 : by_type<true>(dtype, d, ReadLaunch{a, c, fp8, stream});
+}
+
+} // namespace dn
