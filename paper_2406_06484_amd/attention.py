@@ -6,7 +6,7 @@ import ctypes
 from typing import Optional, Tuple
 
 from . import binding
-from .binding import DN_BF16, DN_F32, _check, _p, _stream
+from .binding import DN_BF16, DN_F32, _check, _p
 
 DN_FP8 = 2
 
@@ -58,33 +58,51 @@ def _library():
     return _lib
 
 
+# A decode step calls these functions some tens of times, and the device is done with each call in a few microseconds: the checks are
+# written for the call that passes them (one condition per tensor; what was wrong is found out afterwards).
+
 def _type_of(t, name) -> int:
-    if t.dtype != torch.float32 and t.dtype != torch.bfloat16:
+    if t.dtype is not torch.float32 and t.dtype is not torch.bfloat16:
         raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
     return _TYPES[t.dtype]
 
 
-def _rows(t, name, dtype, heads=None, d=None, T=None) -> int:
-    """t is a device tensor [T, heads, d] whose rows are contiguous; returns the elements between rows"""
+def _refuse(t, name, dtype, shape):
     if not t.is_cuda:
         raise ValueError("%s must be a device tensor" % name)
-    if t.dtype != dtype:
-        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    if t.dim() != 3 or (T is not None and t.shape != (T, heads, d)):
-        raise ValueError("%s must have shape %s, got %s" % (name, ("T", "heads", "d") if T is None else (T, heads, d), tuple(t.shape)))
-    s = t.stride()
-    if (s[2] != 1 and t.shape[2] > 1) or (s[1] != t.shape[2] and t.shape[1] > 1):
-        raise ValueError("%s must have contiguous rows of heads x d" % name)
-    return s[0] if t.shape[0] > 1 else t.shape[1] * t.shape[2]
-
-
-def _whole(t, name, dtype, shape):
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous device tensor" % name)
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
     if t.shape != shape:
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    raise ValueError("%s must be contiguous%s" % (name, " within its rows of heads x d" if t.dim() == 3 else ""))
+
+
+def _rows(t, name, dtype, shape) -> int:
+    """t is a device tensor [T, heads, d] whose rows are contiguous; returns the elements between rows"""
+    T, H, d = shape
+    if not (t.is_cuda and t.dtype is dtype and t.shape == shape):
+        _refuse(t, name, dtype, shape)
+    s0, s1, s2 = t.stride()
+    if s2 != 1 or s1 != d:      # (strides of axes with one element say nothing)
+        if (s2 != 1 and d > 1) or (s1 != d and H > 1):
+            _refuse(t, name, dtype, shape)
+    return s0 if T > 1 else H * d
+
+
+def _whole(t, name, dtype, shape):
+    if not (t.is_cuda and t.dtype is dtype and t.is_contiguous() and t.shape == shape):
+        _refuse(t, name, dtype, shape)
+
+
+def _three(t, name):
+    if t.dim() != 3:
+        raise ValueError("%s must be [T, heads, d], got %s" % (name, tuple(t.shape)))
+    return t.shape
+
+
+def _stream_of(stream, t) -> Optional[int]:
+    """The given stream's handle, or that of the current stream of t's device."""
+    return (torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream) or None
 
 
 def _flat(t, name):
@@ -97,9 +115,9 @@ def _flat(t, name):
     return t
 
 
-def _rope(rope, d, eps, interleaved, device) -> dn_rope:
+def _rope(rope, d, eps, interleaved) -> dn_rope:
     r = dn_rope()
-    r.interleaved, r.eps = int(bool(interleaved)), eps
+    r.interleaved, r.eps = bool(interleaved), eps
     if rope is not None:
         if rope.dim() != 2:
             raise ValueError("rope must be [max_pos, rot], cosines then sines")
@@ -116,26 +134,44 @@ def _weights(q_weight, k_weight, dtype, d):
 
 def _qk_shape(q, k, positions) -> Tuple[dn_qk_shape, "torch.Tensor", "torch.Tensor"]:
     s = dn_qk_shape()
-    s.seq_len = q.shape[1] if q.dim() == 4 else q.shape[0]
+    seq_len = q.shape[0]
+    if q.dim() == 4 and k.dim() == 4:
+        if k.shape[:2] != q.shape[:2]:
+            raise ValueError("q and k must have the same rows")
+        seq_len = q.shape[1]
+        q, k = _flat(q, "q"), _flat(k, "k")
     s.dtype = _type_of(q, "q")
-    if k.dim() != q.dim() or (q.dim() == 4 and k.shape[:2] != q.shape[:2]):
-        raise ValueError("q and k must have the same rows")
-    q, k = _flat(q, "q"), _flat(k, "k")
-    s.q_stride = _rows(q, "q", q.dtype)
-    s.T, s.Hq, s.d = q.shape
-    s.Hkv = k.shape[1] if k.dim() == 3 else 0
-    s.k_stride = _rows(k, "k", q.dtype, s.Hkv, s.d, s.T)
-    s.seq_len = max(s.seq_len, 1)
+    T, Hq, d = shape = _three(q, "q")
+    Hkv = _three(k, "k")[1]
+    s.q_stride = _rows(q, "q", q.dtype, shape)
+    s.k_stride = _rows(k, "k", q.dtype, (T, Hkv, d))
+    s.T, s.Hq, s.Hkv, s.d, s.seq_len = T, Hq, Hkv, d, max(seq_len, 1)
     if positions is not None:
-        _whole(positions, "positions", torch.int32, (s.T,))
+        _whole(positions, "positions", torch.int32, (T,))
     return s, q, k
 
 
-def _out(t, name, like_shape, dtype, device):
+def _out(t, name, shape, like):
     if t is None:
-        return torch.empty(like_shape, dtype=dtype, device=device)
-    _whole(t, name, dtype, like_shape)
+        return like.new_empty(shape)
+    _whole(t, name, like.dtype, shape)
     return t
+
+
+def _sum_out(t, name, d, like):
+    if t is None:
+        return torch.empty(d, dtype=torch.float32, device=like.device)
+    _whole(t, name, torch.float32, (d,))
+    return t
+
+
+def _scratch(workspace, need, like):
+    """(pointer, bytes) of the caller's workspace, or of one for this call, and what keeps it alive"""
+    if workspace is None:
+        if need == 0:
+            return None, 0, None
+        workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
 def deltanet_qk_norm_rope_fwd(q, k, q_weight=None, k_weight=None, rope=None, positions=None, *, eps: float = 1e-6,
@@ -147,12 +183,12 @@ def deltanet_qk_norm_rope_fwd(q, k, q_weight=None, k_weight=None, rope=None, pos
     lib = _library()
     q_shape, k_shape = q.shape, k.shape
     s, q, k = _qk_shape(q, k, positions)
-    r = _rope(rope, s.d, eps, interleaved, q.device)
+    r = _rope(rope, s.d, eps, interleaved)
     _weights(q_weight, k_weight, q.dtype, s.d)
-    q_out = _out(q_out, "q_out", q_shape, q.dtype, q.device)
-    k_out = _out(k_out, "k_out", k_shape, q.dtype, q.device)
+    q_out = _out(q_out, "q_out", q_shape, q)
+    k_out = _out(k_out, "k_out", k_shape, q)
     _check(lib.deltanet_qk_norm_rope_fwd(s, r, _p(q), _p(k), _p(q_weight), _p(k_weight), _p(rope), _p(positions), _p(q_out), _p(k_out),
-                                         _stream(stream)))
+                                         _stream_of(stream, q)))
     return q_out, k_out
 
 
@@ -164,25 +200,23 @@ def deltanet_qk_norm_rope_bwd(q, k, dq_out, dk_out, q_weight=None, k_weight=None
     lib = _library()
     q_shape, k_shape = q.shape, k.shape
     s, q, k = _qk_shape(q, k, positions)
-    r = _rope(rope, s.d, eps, interleaved, q.device)
+    r = _rope(rope, s.d, eps, interleaved)
     _weights(q_weight, k_weight, q.dtype, s.d)
     _whole(dq_out, "dq_out", q.dtype, q_shape)
     _whole(dk_out, "dk_out", q.dtype, k_shape)
-    dq = _out(dq, "dq", q_shape, q.dtype, q.device)
-    dk = _out(dk, "dk", k_shape, q.dtype, q.device)
+    dq = _out(dq, "dq", q_shape, q)
+    dk = _out(dk, "dk", k_shape, q)
     if q_weight is not None:
-        dq_weight = _out(dq_weight, "dq_weight", (s.d,), torch.float32, q.device)
+        dq_weight = _sum_out(dq_weight, "dq_weight", s.d, q)
     if k_weight is not None:
-        dk_weight = _out(dk_weight, "dk_weight", (s.d,), torch.float32, q.device)
+        dk_weight = _sum_out(dk_weight, "dk_weight", s.d, q)
     if (q_weight is None and dq_weight is not None) or (k_weight is None and dk_weight is not None):
         raise ValueError("no gradient of a weight that is not there")
     need = ctypes.c_size_t(0)
     _check(lib.deltanet_qk_norm_rope_workspace_bytes(s, need))
-    if workspace is None:
-        workspace = torch.empty(max(need.value, 16), dtype=torch.uint8, device=q.device)
+    ws, ws_bytes, workspace = _scratch(workspace, need.value if dq_weight is not None or dk_weight is not None else 0, q)
     _check(lib.deltanet_qk_norm_rope_bwd(s, r, _p(q), _p(k), _p(dq_out), _p(dk_out), _p(q_weight), _p(k_weight), _p(rope), _p(positions),
-                                         _p(dq), _p(dk), _p(dq_weight), _p(dk_weight), _p(workspace),
-                                         workspace.numel() * workspace.element_size(), _stream(stream)))
+                                         _p(dq), _p(dk), _p(dq_weight), _p(dk_weight), ws, ws_bytes, _stream_of(stream, q)))
     return dq, dk, dq_weight, dk_weight
 
 
@@ -200,36 +234,35 @@ def deltanet_paged_cache(num_pages: int, page_size: int, heads: int, d: int, dty
 
 
 def _paged(k_pages, v_pages, k_scale, v_scale, page_table, kv_len, cu_q, dtype) -> Tuple[dn_paged_shape, dn_paged_cache]:
-    if k_pages.dim() != 4:
-        raise ValueError("k_pages must be [num_pages, heads, page_size, d]")
-    if k_pages.dtype not in _TYPES:
-        raise TypeError("k_pages must be float32, bfloat16 or float8_e4m3fn, got %s" % k_pages.dtype)
-    shape = k_pages.shape
-    _whole(k_pages, "k_pages", k_pages.dtype, shape)
-    _whole(v_pages, "v_pages", k_pages.dtype, shape)
-    quantised = k_pages.dtype == torch.float8_e4m3fn
-    if not quantised and k_pages.dtype != dtype:
-        raise TypeError("pages must be %s or float8_e4m3fn, got %s" % (dtype, k_pages.dtype))
-    for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
-        if quantised:
-            if t is None:
-                raise ValueError("%s is needed for an 8-bit cache" % name)
-            _whole(t, name, torch.float32, shape[:3])
-        elif t is not None:
-            raise ValueError("%s belongs to an 8-bit cache" % name)
+    if k_pages.dim() != 4 or page_table.dim() != 2:
+        raise ValueError("k_pages must be [num_pages, heads, page_size, d], page_table [sequences, max_pages]")
+    pages, heads, page_size, d = shape = k_pages.shape
+    N, width = of_table = page_table.shape
+    held, i32 = k_pages.dtype, torch.int32
+    if held not in _TYPES:
+        raise TypeError("k_pages must be float32, bfloat16 or float8_e4m3fn, got %s" % held)
+    _whole(k_pages, "k_pages", held, shape)
+    _whole(v_pages, "v_pages", held, shape)
+    c = dn_paged_cache(k_pages.data_ptr(), v_pages.data_ptr())
+    if held is torch.float8_e4m3fn:
+        if k_scale is None or v_scale is None:
+            raise ValueError("k_scale and v_scale are needed for an 8-bit cache")
+        _whole(k_scale, "k_scale", torch.float32, (pages, heads, page_size))
+        _whole(v_scale, "v_scale", torch.float32, (pages, heads, page_size))
+        c.k_scale, c.v_scale = k_scale.data_ptr(), v_scale.data_ptr()
+    elif held is not dtype:
+        raise TypeError("pages must be %s or float8_e4m3fn, got %s" % (dtype, held))
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError("scales belong to an 8-bit cache")
+    _whole(page_table, "page_table", i32, of_table)
+    _whole(kv_len, "kv_len", i32, (N,))
+    _whole(cu_q, "cu_q", i32, (N + 1,))
     s = dn_paged_shape()
-    if page_table.dim() != 2:
-        raise ValueError("page_table must be [sequences, max_pages]")
-    N, M = page_table.shape
-    _whole(page_table, "page_table", torch.int32, page_table.shape)
-    _whole(kv_len, "kv_len", torch.int32, (N,))
-    _whole(cu_q, "cu_q", torch.int32, (N + 1,))
-    s.num_seqs, s.max_pages = N, M
-    s.num_pages, s.Hkv, s.page_size, s.d = shape
-    s.dtype, s.cache_dtype = _TYPES[dtype], _TYPES[k_pages.dtype]
-    s.max_kv = min(M * shape[2], 2 ** 31 - 1)
+    s.num_seqs, s.max_pages = N, width
+    s.num_pages, s.Hkv, s.page_size, s.d = pages, heads, page_size, d
+    s.dtype, s.cache_dtype = _TYPES[dtype], _TYPES[held]
+    s.max_kv = min(width * page_size, 2 ** 31 - 1)
     s.cu_q, s.kv_len, s.page_table = cu_q.data_ptr(), kv_len.data_ptr(), page_table.data_ptr()
-    c = dn_paged_cache(k_pages.data_ptr(), v_pages.data_ptr(), _p(k_scale), _p(v_scale))
     return s, c
 
 
@@ -238,12 +271,13 @@ def deltanet_paged_append(k, v, k_pages, v_pages, page_table, kv_len, cu_q, *, k
     rows cu_q[n] .. cu_q[n + 1] - 1, the last of them token kv_len[n] - 1 of its context; its token p stands in page
     page_table[n, p // page_size], slot p % page_size."""
     lib = _library()
-    dt = _type_of(k, "k")
+    _type_of(k, "k")
     s, c = _paged(k_pages, v_pages, k_scale, v_scale, page_table, kv_len, cu_q, k.dtype)
-    s.dtype, s.T, s.Hq = dt, k.shape[0], s.Hkv
-    s.k_stride = _rows(k, "k", k.dtype, s.Hkv, s.d, s.T)
-    s.v_stride = _rows(v, "v", k.dtype, s.Hkv, s.d, s.T)
-    _check(lib.deltanet_paged_append(s, _p(k), _p(v), c, _stream(stream)))
+    T = _three(k, "k")[0]
+    s.T, s.Hq = T, s.Hkv
+    s.k_stride = _rows(k, "k", k.dtype, (T, s.Hkv, s.d))
+    s.v_stride = _rows(v, "v", k.dtype, (T, s.Hkv, s.d))
+    _check(lib.deltanet_paged_append(s, k.data_ptr(), v.data_ptr(), c, _stream_of(stream, k)))
 
 
 def deltanet_paged_norm_rope_append(q, k, v, k_pages, v_pages, page_table, kv_len, cu_q, q_weight=None, k_weight=None, rope=None, *,
@@ -252,19 +286,19 @@ def deltanet_paged_norm_rope_append(q, k, v, k_pages, v_pages, page_table, kv_le
     """The serving form of deltanet_qk_norm_rope_fwd, in one pass with deltanet_paged_append: k normalised and rotated, and v, go to the
     cache; returns q normalised and rotated.  Positions are the tokens' places in their contexts."""
     lib = _library()
-    dt = _type_of(q, "q")
+    _type_of(q, "q")
     s, c = _paged(k_pages, v_pages, k_scale, v_scale, page_table, kv_len, cu_q, q.dtype)
-    s.dtype = dt
-    s.q_stride = _rows(q, "q", q.dtype)
-    s.T, s.Hq = q.shape[:2]
-    if q.shape[2] != s.d:
-        raise ValueError("q must have the cache's head size")
-    s.k_stride = _rows(k, "k", q.dtype, s.Hkv, s.d, s.T)
-    s.v_stride = _rows(v, "v", q.dtype, s.Hkv, s.d, s.T)
-    r = _rope(rope, s.d, eps, interleaved, q.device)
-    _weights(q_weight, k_weight, q.dtype, s.d)
-    q_out = _out(q_out, "q_out", q.shape, q.dtype, q.device)
-    _check(lib.deltanet_paged_norm_rope_append(s, r, _p(q), _p(k), _p(v), _p(q_weight), _p(k_weight), _p(rope), _p(q_out), c, _stream(stream)))
+    T, Hq, _ = shape = _three(q, "q")
+    Hkv, d = s.Hkv, s.d
+    s.T, s.Hq = T, Hq
+    s.q_stride = _rows(q, "q", q.dtype, (T, Hq, d))
+    s.k_stride = _rows(k, "k", q.dtype, (T, Hkv, d))
+    s.v_stride = _rows(v, "v", q.dtype, (T, Hkv, d))
+    r = _rope(rope, d, eps, interleaved)
+    _weights(q_weight, k_weight, q.dtype, d)
+    q_out = _out(q_out, "q_out", shape, q)
+    _check(lib.deltanet_paged_norm_rope_append(s, r, q.data_ptr(), k.data_ptr(), v.data_ptr(), _p(q_weight), _p(k_weight), _p(rope),
+                                               q_out.data_ptr(), c, _stream_of(stream, q)))
     return q_out
 
 
@@ -275,14 +309,18 @@ def deltanet_paged_read(k_pages, v_pages, page_table, kv_len, cu_out, rows: int,
     lib = _library()
     if dtype is None:
         dtype = torch.bfloat16 if k_pages.dtype == torch.float8_e4m3fn else k_pages.dtype
-    if dtype != torch.float32 and dtype != torch.bfloat16:
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
         raise TypeError("dtype must be float32 or bfloat16, got %s" % dtype)
     s, c = _paged(k_pages, v_pages, k_scale, v_scale, page_table, kv_len, cu_out, dtype)
     s.T, s.Hq = 0, s.Hkv
     shape = (rows, s.Hkv, s.d)
-    k_out = _out(k_out, "k_out", shape, dtype, k_pages.device)
-    v_out = _out(v_out, "v_out", shape, dtype, k_pages.device)
-    _check(lib.deltanet_paged_read(s, c, cu_out.data_ptr(), rows, _p(k_out), _p(v_out), _stream(stream)))
+    if k_out is None:
+        k_out = torch.empty(shape, dtype=dtype, device=k_pages.device)
+    if v_out is None:
+        v_out = torch.empty(shape, dtype=dtype, device=k_pages.device)
+    _whole(k_out, "k_out", dtype, shape)
+    _whole(v_out, "v_out", dtype, shape)
+    _check(lib.deltanet_paged_read(s, c, cu_out.data_ptr(), rows, k_out.data_ptr(), v_out.data_ptr(), _stream_of(stream, k_pages)))
     return k_out, v_out
 
 
@@ -300,20 +338,18 @@ def deltanet_paged_attn_fwd(q, k_pages, v_pages, page_table, kv_len, cu_q, *, k_
     default.  max_q and max_kv: bounds on the longest chunk and the longest context (T and the page table's width by default; close bounds
     make for better-sized launches)."""
     lib = _library()
-    dt = _type_of(q, "q")
+    _type_of(q, "q")
     s, c = _paged(k_pages, v_pages, k_scale, v_scale, page_table, kv_len, cu_q, q.dtype)
-    s.dtype = dt
-    s.q_stride = _rows(q, "q", q.dtype)
-    s.T, s.Hq = q.shape[:2]
-    if q.shape[2] != s.d:
-        raise ValueError("q must have the cache's head size")
-    s.max_q = s.T if max_q is None else max_q
+    T, Hq, _ = shape = _three(q, "q")
+    s.T, s.Hq = T, Hq
+    s.q_stride = _rows(q, "q", q.dtype, (T, Hq, s.d))
+    s.max_q = T if max_q is None else max_q
     if max_kv is not None:
         s.max_kv = max_kv
-    o = _out(o, "o", q.shape, q.dtype, q.device)
-    need = deltanet_paged_attn_workspace_bytes(s, window)
-    if workspace is None:
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
-    _check(lib.deltanet_paged_attn_fwd(s, _p(q), c, s.d ** -0.5 if scale is None else scale, window, _p(o), _p(workspace),
-                                       workspace.numel() * workspace.element_size(), _stream(stream)))
+    o = _out(o, "o", shape, q)
+    need = ctypes.c_size_t(0)
+    _check(lib.deltanet_paged_attn_workspace_bytes(s, window, need))
+    ws, ws_bytes, workspace = _scratch(workspace, need.value, q)
+    _check(lib.deltanet_paged_attn_fwd(s, q.data_ptr(), c, s.d ** -0.5 if scale is None else scale, window, o.data_ptr(), ws, ws_bytes,
+                                       _stream_of(stream, q)))
     return o

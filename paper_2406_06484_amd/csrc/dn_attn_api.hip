@@ -115,7 +115,7 @@ AttnArgs attn_args(const dn_paged_shape *s, const dn_paged_cache *c, int window)
     a.r = row_args(s->T, s->Hq, s->Hkv);
     a.r.q_stride = s->q_stride;
     a.c = paged_args(s, c);
-    a.scale = 0.f; a.window = window; a.max_q = s->max_q;
+    a.scale = 0.f; a.window = window; a.max_q = s->max_q; a.splits = 1;
     a.workspace = nullptr;
     return a;
 }

@@ -33,6 +33,7 @@ struct AttnArgs {
     PagedArgs c;
     float scale;
     int window, max_q;
+    int splits;                          // most splits of any row (the workspace's layout)
     void *workspace;
 };
 

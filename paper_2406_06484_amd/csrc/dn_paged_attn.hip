@@ -11,6 +11,9 @@
 
 namespace dn {
 
+// How the key axis is cut: `splits` pieces of `keys` keys from the first that a row tile sees.
+struct Cut { int splits, keys; };
+
 constexpr float kNoScore = -1e30f; // the running maximum before the first key: finite, so that differences are never NaN
 
 // The rows of sequence n and its context, held inside the tensors whatever the arrays say.
@@ -31,11 +34,11 @@ __device__ inline void key_range(const AttnArgs &a, const SeqRows &s, int G, int
     lo = a.window > 0 ? max(first - a.window + 1, 0) / step * step : 0;
 }
 
-// Cache row (of d elements) of key kk, a multiple of 16 (a page holds at least 16): the same for the whole wave.
-__device__ inline int page_of(const PagedArgs &c, int n, int kk) {
-    const int id = c.table[(long)n * c.max_pages + min(kk >> c.page_shift, c.max_pages - 1)];
-    return __builtin_amdgcn_readfirstlane(min(max(id, 0), c.num_pages - 1));
-}
+// The page table's entry for key kk, the page that it stands for, and (the wave's key kk, a multiple of 16: a page holds at least 16) the
+// cache row of d elements.
+__device__ inline int page_entry(const PagedArgs &c, int n, int kk) { return c.table[(long)n * c.max_pages + min(kk >> c.page_shift, c.max_pages - 1)]; }
+__device__ inline int page_id(const PagedArgs &c, int entry) { return min(max(entry, 0), c.num_pages - 1); }
+__device__ inline int page_of(const PagedArgs &c, int n, int kk) { return __builtin_amdgcn_readfirstlane(page_id(c, page_entry(c, n, kk))); }
 __device__ inline long row_of(const PagedArgs &c, int page, int kk, int kvh, int Hkv) {
     return (((long)page * Hkv + kvh) << c.page_shift) + (kk & ((1 << c.page_shift) - 1));
 }
@@ -48,6 +51,17 @@ template <typename T, int D> __device__ inline void zero_rest(const AttnArgs &a,
         const long row = (from + i / (G * W)) * a.r.Hq + kvh * G + i / W % G;
         reinterpret_cast<uint4 *>(a.r.q_out)[row * W + i % W] = make_uint4(0, 0, 0, 0);
     }
+}
+
+// What a sum of weights divides by: nothing where there is nothing, and NaN stays NaN.
+__device__ inline float inverse_sum(float l) { return l > 0.f ? 1.f / l : (l == l ? 0.f : l); }
+
+// Where a split's (maximum, sum) and unnormalised output of a row (token and head) stand in the workspace.
+__device__ inline void partial_of(const AttnArgs &a, int split, long row, int D, float **ml, float **po) {
+    const long rows = (long)a.r.T * a.r.Hq, at = split * rows + row;
+    float *base = static_cast<float *>(a.workspace);
+    *ml = base + 2 * at;
+    *po = base + ((2 * a.splits * rows + 3) & ~3l) + at * D;
 }
 
 // --- Few rows: generation, and short chunks.
@@ -80,9 +94,12 @@ __device__ inline unsigned bf16_pair(unsigned w, bool hi) {
     return __builtin_bit_cast(unsigned, v);
 }
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+// eight e4m3 numbers as bf16
+__device__ inline u32x4 widen(unsigned lo, unsigned hi) { return u32x4{bf16_pair(lo, false), bf16_pair(lo, true), bf16_pair(hi, false), bf16_pair(hi, true)}; }
 
 template <typename T, typename CT, int D>
-__global__ __launch_bounds__(64 * kFewWaves) void k_attn_few(AttnArgs a, int tiles, int splits, int split_keys, int max_rows) {
+__global__ __launch_bounds__(64 * kFewWaves) void k_attn_few(AttnArgs a, int tiles, Cut cut, int max_rows) {
+    const int splits = cut.splits, split_keys = cut.keys;
     constexpr int EB = PageElem<T, CT>::bytes;
     constexpr int KE = D / 4, VE = D / 16;              // elements of a key, of a value, that a lane holds
     constexpr int KW = KE * EB / 4, VW = VE * EB / 4;   // in words
@@ -166,7 +183,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_attn_few(AttnArgs a, int til
 #pragma unroll
                 for (int e = 0; e < KE / 8; ++e) {
                     u32x4 kk;
-                    if constexpr (FP8) kk = u32x4{bf16_pair(kw[h][2 * e], false), bf16_pair(kw[h][2 * e], true), bf16_pair(kw[h][2 * e + 1], false), bf16_pair(kw[h][2 * e + 1], true)};
+                    if constexpr (FP8) kk = widen(kw[h][2 * e], kw[h][2 * e + 1]);
                     else kk = u32x4{kw[h][4 * e], kw[h][4 * e + 1], kw[h][4 * e + 2], kw[h][4 * e + 3]};
                     const u32x4 qq = u32x4{qw[4 * e], qw[4 * e + 1], qw[4 * e + 2], qw[4 * e + 3]};
                     st[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kk), __builtin_bit_cast(bf16x8, qq), st[h], 0, 0, 0);
@@ -287,56 +304,333 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_attn_few(AttnArgs a, int til
     }
     const long row = (long)(s.r0 + (row0 + q) / G) * a.r.Hq + kvh * G + (row0 + q) % G;
     if (splits == 1) {
-        const float inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
+        const float inv = inverse_sum(L);
         T *to = static_cast<T *>(a.r.q_out) + row * D + e0;
 #pragma unroll
         for (int j = 0; j < VE; ++j) to[j] = (T)(acc[j] * inv);
     } else {
-        const long at = (long)split * a.r.T * a.r.Hq + row, all = (long)splits * a.r.T * a.r.Hq;
-        float *ml = static_cast<float *>(a.workspace), *po = ml + ((2 * all + 3) & ~3l);
-        if (e0 == 0) *reinterpret_cast<float2 *>(ml + 2 * at) = make_float2(M, L);
+        float *ml, *po;
+        partial_of(a, split, row, D, &ml, &po);
+        if (e0 == 0) *reinterpret_cast<float2 *>(ml) = make_float2(M, L);
 #pragma unroll
-        for (int j = 0; j < VE; j += 2) *reinterpret_cast<float2 *>(po + at * D + e0 + j) = make_float2(acc[j], acc[j + 1]);
+        for (int j = 0; j < VE; j += 2) *reinterpret_cast<float2 *>(po + e0 + j) = make_float2(acc[j], acc[j + 1]);
     }
 }
 
-// Joins the splits of every row (a wave per row and head).
+// --- Many rows: prompts and long chunks.
+//
+// Bound by the matrix cores.  A workgroup has 128 rows, 32 per wave, and walks over its keys 64 at a time: K and V travel through
+// registers (8-bit pages become bf16 on the way, exactly) into one of two LDS buffers while the other is worked on, so that a tile costs one
+// barrier.  Rows of a tile are not padded: their 16-byte pieces are permuted by an XOR with the row, which spreads both the row
+// reads (K) and the transposing reads (V, four rows at a time) over the banks.
+constexpr int kWideRows = 128, kWideWaves = 4;
+// keys of a tile (at d = 256 twice as many would need more registers than there are)
+constexpr int wide_keys(int d) { return d > 128 ? 32 : 64; }
+
+template <typename CT, int D> struct WideTile {
+    static constexpr bool FP8 = __is_same(CT, fp8);
+    static constexpr int KEYS = wide_keys(D);
+    static constexpr int CH = D / 8, ROWB = 2 * D;                 // 16-byte pieces, bytes of a row in the LDS
+    static constexpr int PER = FP8 ? 2 : 1, LPR = CH / PER;        // pieces per load, lanes per row
+    static constexpr int NL = KEYS * LPR / (64 * kWideWaves); // loads per thread and tensor
+    static constexpr int BYTES = KEYS * ROWB;
+    static constexpr int oV = BYTES, oKS = 2 * BYTES, oVS = oKS + (FP8 ? 4 * KEYS : 0), SIZE = oVS + (FP8 ? 4 * KEYS : 0);
+    __device__ static inline int swizzle(int row) { return D == 64 ? ((row >> 1) & 1) << 2 | ((row >> 2) & 3) : (row & 3) << 2 | ((row >> 2) & 3); }
+};
+
+// The sequence and the row tile that a slot stands for: slots count the tiles of 128 rows of the sequences with more than `few` rows.
+// Later tiles see more keys and come first, so that the workgroups that start last are short: of each 64 sequences the last tiles, then the ones
+// before those, and so on (in the order of the sequences, prompts of 4 x 2048 tokens took 160 us instead of TIMEHERE).  False past the last slot.
+__device__ inline bool tile_of_slot(const AttnArgs &a, int G, int few, int slot, int *seq, int *tile) {
+    const int lane = threadIdx.x & 63;
+    for (int base = 0; base < a.c.N; base += 64) {
+        const int n = base + lane;
+        int tiles = 0;
+        if (n < a.c.N) {
+            const int r0 = min(max(a.c.cu[n], 0), a.r.T), r1 = min(max(a.c.cu[n + 1], r0), a.r.T), R = (r1 - r0) * G;
+            tiles = R > few ? (R + kWideRows - 1) / kWideRows : 0;
+        }
+        int rank = 0; // tiles behind this one in its sequence
+        for (unsigned long long on = __ballot(tiles > 0); on; on = __ballot(tiles > rank)) {
+            const int count = __builtin_popcountll(on);
+            if (slot < count) {
+                const bool mine = (on >> lane & 1) && __builtin_popcountll(on & ((1ull << lane) - 1)) == slot;
+                const int at = __builtin_ctzll(__ballot(mine));
+                *seq = base + at;
+                *tile = __shfl(tiles, at) - 1 - rank;
+                return true;
+            }
+            // the ranks up to the shortest sequence's first tile hold as many
+            int least = tiles > rank ? tiles : 0x7fffffff;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) least = min(least, __shfl_xor(least, o));
+            const int steps = min(least - rank, slot / count);
+            rank += steps;
+            slot -= steps * count;
+        }
+    }
+    return false;
+}
+
+template <typename CT, int D>
+__global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(AttnArgs a, Cut cut, int few) {
+    const int splits = cut.splits, split_keys = cut.keys;
+    using W = WideTile<CT, D>;
+    constexpr bool FP8 = W::FP8;
+    constexpr int EB = FP8 ? 1 : 2, NB = D / 32, KEYS = W::KEYS, NX = KEYS / 32;
+    extern __shared__ __align__(16) unsigned char wsmem[];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 31, h = lane >> 5;
+    const int Hkv = a.r.Hkv, G = a.r.Hq / Hkv;
+    int b = blockIdx.x;
+    const int kvh = b % Hkv; b /= Hkv;
+    const int split = b % splits, slot = b / splits;
+    int n, tile;
+    if (!tile_of_slot(a, G, few, slot, &n, &tile)) return;
+    n = __builtin_amdgcn_readfirstlane(n);
+    tile = __builtin_amdgcn_readfirstlane(tile);
+    SeqRows s;
+    s.load(a, n);
+    const int R = (s.r1 - s.r0) * G, row0 = tile * kWideRows, row1 = min(row0 + kWideRows, R);
+    int lo, hi;
+    key_range(a, s, G, row0, row1, KEYS, lo, hi);
+    const int k_begin = lo + split * split_keys, k_end = min(hi, k_begin + split_keys);
+    if (splits > 1 && k_begin >= k_end) return; // (the rows' other splits know)
+    const int wrow = row0 + 32 * wave, before = s.kv - (s.r1 - s.r0);
+    const int row = min(wrow + col, row1 - 1), tok = row / G, head = kvh * G + row % G;
+    const int p = before + tok, p_lo = a.window > 0 ? p - a.window + 1 : 0;   // the lane's query's position, and the first key it sees
+    // keys that some row, that every row of the wave sees
+    const int last = before + (min(wrow + 32, row1) - 1) / G, first = before + min(wrow, row1 - 1) / G;
+    const int some_from = a.window > 0 ? first - a.window + 1 : 0, some_to = wrow < row1 ? last : -1;
+    const int all_from = a.window > 0 ? last - a.window + 1 : 0, all_to = first;
+    const float c = a.scale * 1.4426950408889634f;
+
+    bf16x8 q[D / 16];
+    {
+        const bf16 *src = static_cast<const bf16 *>(a.r.q) + (long)(s.r0 + tok) * a.r.q_stride + head * D + 8 * h;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) q[i] = *reinterpret_cast<const bf16x8 *>(src + 16 * i);
+    }
+    f32x16 o[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+    float m = kNoScore, l = 0.f;
+
+    // this thread's pieces of a tile on their way
+    u32x4 rk[W::NL], rv[W::NL];
+    float rs = 0.f;
+    const char *kp = static_cast<const char *>(a.c.kp), *vp = static_cast<const char *>(a.c.vp);
+    const int piece = t % W::LPR;
+    int page[W::NL], spage = 0; // of the next tile to fetch, looked up a tile ahead
+    auto look_up = [&](int k0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < W::NL; ++i) page[i] = page_entry(a.c, n, k0 + ((i * 256 + wave * 64) / W::LPR & ~15));
+        if constexpr (FP8) spage = page_entry(a.c, n, k0 + (lane & 48));
+    };
+    auto fetch = [&](int k0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < W::NL; ++i) {
+            const int r0 = (i * 256 + wave * 64) / W::LPR, kk = k0 + (r0 & ~15); // the wave's rows lie in one group of 16 keys
+            const long at = row_of(a.c, __builtin_amdgcn_readfirstlane(page_id(a.c, page[i])), kk, kvh, Hkv) * (D * EB);
+            const int off = ((r0 & 15) + lane / W::LPR) * (D * EB) + piece * 16;
+            rk[i] = *reinterpret_cast<const u32x4 *>(kp + at + off);
+            rv[i] = *reinterpret_cast<const u32x4 *>(vp + at + off);
+        }
+        if constexpr (FP8)
+            if (wave < 2 && lane < KEYS) rs = (wave ? a.c.vs : a.c.ks)[row_of(a.c, page_id(a.c, spage), k0 + (lane & 48), kvh, Hkv) + (lane & 15)];
+        look_up(k0 + KEYS);
+    };
+    auto park = [&](unsigned char *buf, int k0) __attribute__((always_inline)) {
+        const bool tail = k0 + KEYS > hi; // nothing past the last key that a row sees is read into a result, whatever stands there
+#pragma unroll
+        for (int i = 0; i < W::NL; ++i) {
+            const int r = (i * 256 + t) / W::LPR;
+            u32x4 v = rv[i];
+            if (tail && k0 + r >= hi) v = u32x4{0, 0, 0, 0};
+            if constexpr (FP8) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    unsigned char *at = buf + r * W::ROWB + (((2 * piece + u) ^ W::swizzle(r)) << 4);
+                    *reinterpret_cast<u32x4 *>(at) = widen(rk[i][2 * u], rk[i][2 * u + 1]);
+                    *reinterpret_cast<u32x4 *>(at + W::oV) = widen(v[2 * u], v[2 * u + 1]);
+                }
+            } else {
+                unsigned char *at = buf + r * W::ROWB + ((piece ^ W::swizzle(r)) << 4);
+                *reinterpret_cast<u32x4 *>(at) = rk[i];
+                *reinterpret_cast<u32x4 *>(at + W::oV) = v;
+            }
+        }
+        if constexpr (FP8)
+            if (wave < 2 && lane < KEYS) reinterpret_cast<float *>(buf + (wave ? W::oVS : W::oKS))[lane] = tail && k0 + lane >= hi ? 0.f : rs;
+    };
+    auto work = [&](const unsigned char *buf, int k0) __attribute__((always_inline)) {
+        f32x16 st[NX];
+#pragma unroll
+        for (int x = 0; x < NX; ++x) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) st[x][r] = 0.f;
+            const unsigned char *kr = buf + (32 * x + col) * W::ROWB;
+            const int sw = W::swizzle(col);
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+                st[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(kr + (((2 * i + h) ^ sw) << 4)), q[i], st[x], 0, 0, 0);
+            if constexpr (FP8)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4 f = *reinterpret_cast<const float4 *>(buf + W::oKS + (32 * x + 8 * g + 4 * h) * 4);
+                    st[x][4 * g] *= f.x; st[x][4 * g + 1] *= f.y; st[x][4 * g + 2] *= f.z; st[x][4 * g + 3] *= f.w;
+                }
+        }
+        if (k0 < all_from || k0 + KEYS - 1 > all_to) {
+#pragma unroll
+            for (int x = 0; x < NX; ++x)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int key = k0 + 32 * x + 8 * (r >> 2) + 4 * h + (r & 3);
+                    if (key > p || key < p_lo) st[x][r] = -INFINITY;
+                }
+        }
+        float mt = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < NX; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mt = fmaxf(mt, st[x][r]);
+        {
+            const unsigned u = __float_as_uint(mt);
+            const auto x = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+            mt = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) * c;
+        }
+        // m need not be the maximum, only near it: sums are rescaled when a row's has grown by 2^8 or more
+        if (__any(mt > m + 8.f)) {
+            const float mn = fmaxf(m, mt), f = __builtin_amdgcn_exp2f(m - mn);
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < NB; ++i) o[i] *= f;
+            m = mn;
+        }
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < NX; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                st[x][r] = __builtin_amdgcn_exp2f(fmaf(st[x][r], c, -m));
+                sum[r & 3] += st[x][r];
+            }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        const int i = lane & 15;
+        const int sw[2] = {W::swizzle((i >> 2) + 4 * h), W::swizzle((i >> 2) + 4 * h + 8)};
+        const int c0 = ((lane & 16) >> 3) + ((i & 3) >> 1);
+#pragma unroll
+        for (int x = 0; x < NX; ++x) {
+            if constexpr (FP8) {
+                __builtin_amdgcn_sched_barrier(0); // (the factors would be fetched for both halves, into registers that are not there)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4 f = *reinterpret_cast<const float4 *>(buf + W::oVS + (32 * x + 8 * g + 4 * h) * 4);
+                    st[x][4 * g] *= f.x; st[x][4 * g + 1] *= f.y; st[x][4 * g + 2] *= f.z; st[x][4 * g + 3] *= f.w;
+                }
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                bf16x8 pt;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) pt[u] = (bf16)st[x][8 * y + u];
+                const unsigned char *vr = buf + W::oV + (32 * x + 16 * y + 4 * h + (i >> 2)) * W::ROWB + 8 * (i & 1);
+#pragma unroll
+                for (int d = 0; d < NB; ++d) {
+                    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+                    const s16x4 va = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vr + (((4 * d + c0) ^ sw[0]) << 4)));
+                    const s16x4 vb = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vr + 8 * W::ROWB + (((4 * d + c0) ^ sw[1]) << 4)));
+                    const s16x8 v = __builtin_shufflevector(va, vb, 0, 1, 2, 3, 4, 5, 6, 7);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), pt, o[d], 0, 0, 0);
+                }
+            }
+        }
+    };
+
+    if (k_begin < k_end) {
+        look_up(k_begin);
+        fetch(k_begin);
+        park(wsmem, k_begin);
+        if (k_begin + KEYS < k_end) fetch(k_begin + KEYS);
+        lds_barrier();
+        for (int k0 = k_begin, j = 0; k0 < k_end; k0 += KEYS, j ^= 1) {
+            // (the other buffer was last read before the barrier that ended the last tile)
+            if (k0 + KEYS < k_end) park(wsmem + (j ^ 1) * W::SIZE, k0 + KEYS);
+            if (k0 + 2 * KEYS < k_end) fetch(k0 + 2 * KEYS);
+            if (k0 <= some_to && k0 + KEYS > some_from) work(wsmem + j * W::SIZE, k0);
+            lds_barrier();
+        }
+    }
+    {
+        const unsigned u = __float_as_uint(l);
+        const auto x = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+    }
+    if (wrow + col >= row1) return;
+    // element 32 d + 8 g + 4 h + i of the lane's row stands at o[d][4 g + i]
+    const long out = (long)(s.r0 + tok) * a.r.Hq + head;
+    if (splits == 1) {
+        const float inv = inverse_sum(l);
+        bf16 *to = static_cast<bf16 *>(a.r.q_out) + out * D + 4 * h;
+#pragma unroll
+        for (int d = 0; d < NB; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<bf16x4 *>(to + 32 * d + 8 * g) = bf16x4{(bf16)(o[d][4 * g] * inv), (bf16)(o[d][4 * g + 1] * inv), (bf16)(o[d][4 * g + 2] * inv), (bf16)(o[d][4 * g + 3] * inv)};
+    } else {
+        float *ml, *po;
+        partial_of(a, split, out, D, &ml, &po);
+        if (h == 0) *reinterpret_cast<float2 *>(ml) = make_float2(m, l);
+#pragma unroll
+        for (int d = 0; d < NB; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<float4 *>(po + 32 * d + 8 * g + 4 * h) = make_float4(o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]);
+    }
+}
+
+// Joins the splits of every row (a wave per row and head).  Where a launch splits the rows of one kind only, the others' outputs are there.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, int splits, int split_keys) {
+__global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, Cut few, Cut wide, int few_rows) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long row = (long)blockIdx.x * 4 + wave;
     if (row >= (long)a.r.T * a.r.Hq) return;
     const int t = (int)(row / a.r.Hq), h = (int)(row % a.r.Hq), G = a.r.Hq / a.r.Hkv;
+    const int n = seq_of_row(a.c.cu, a.c.N, t);
+    if (n >= a.c.N) return; // (zeroed)
+    SeqRows s;
+    s.load(a, n);
+    const int R = (s.r1 - s.r0) * G, r = max(t - s.r0, 0) * G + h % G;
+    const Cut cut = R > few_rows ? wide : few;
+    if (cut.splits == 1) return;
+    const int rows = R > few_rows ? kWideRows : kFewTile, row0 = r / rows * rows;
+    int lo, hi;
+    key_range(a, s, G, row0, min(row0 + rows, R), R > few_rows ? wide_keys(D) : kFewKeys, lo, hi);
+    const int live = hi > lo ? min((hi - lo + cut.keys - 1) / cut.keys, cut.splits) : 0;
     constexpr int E = D >= 64 ? D / 64 : 1;
     const bool on = lane * E < D;
-    T *to = static_cast<T *>(a.r.q_out) + row * D + lane * E;
-    const int n = seq_of_row(a.c.cu, a.c.N, t);
-    int live = 0;
-    if (n < a.c.N) {
-        SeqRows s;
-        s.load(a, n);
-        const int R = (s.r1 - s.r0) * G, r = max(t - s.r0, 0) * G + h % G, row0 = r / kFewTile * kFewTile;
-        int lo, hi;
-        key_range(a, s, G, row0, min(row0 + kFewTile, R), kFewKeys, lo, hi);
-        live = hi > lo ? min((hi - lo + split_keys - 1) / split_keys, splits) : 0;
-    }
-    const long rows = (long)a.r.T * a.r.Hq;
-    const float *ml = static_cast<const float *>(a.workspace), *po = ml + ((2 * splits * rows + 3) & ~3l);
     float M = kNoScore, L = 0.f, acc[E];
-    for (int i = lane; i < live; i += 64) M = fmaxf(M, ml[2 * (i * rows + row)]);
+    float *ml, *po;
+    for (int i = lane; i < live; i += 64) {
+        partial_of(a, i, row, D, &ml, &po);
+        M = fmaxf(M, ml[0]);
+    }
     M = lanes_max<64>(M);
 #pragma unroll
     for (int j = 0; j < E; ++j) acc[j] = 0.f;
     for (int i = 0; i < live; ++i) {
-        const float2 x = *reinterpret_cast<const float2 *>(ml + 2 * (i * rows + row));
-        const float f = __builtin_amdgcn_exp2f(x.x - M);
-        L = fmaf(x.y, f, L);
+        partial_of(a, i, row, D, &ml, &po);
+        const float f = __builtin_amdgcn_exp2f(ml[0] - M);
+        L = fmaf(ml[1], f, L);
         if (on) {
 #pragma unroll
-            for (int j = 0; j < E; ++j) acc[j] = fmaf(po[(i * rows + row) * D + lane * E + j], f, acc[j]);
+            for (int j = 0; j < E; ++j) acc[j] = fmaf(po[lane * E + j], f, acc[j]);
         }
     }
-    const float inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
+    const float inv = inverse_sum(L);
+    T *to = static_cast<T *>(a.r.q_out) + row * D + lane * E;
     if (on) {
 #pragma unroll
         for (int j = 0; j < E; ++j) to[j] = (T)(acc[j] * inv);
@@ -345,75 +639,104 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, int splits, int s
 
 namespace {
 
-struct Plan { int tiles, splits, split_keys; };
+// Rows of a sequence and key/value head up to which the kernel for few rows takes them (fp32: always).
+constexpr int kFewMost = 32;
+
+struct Plan { int few_rows, tiles, slots; Cut few, wide; };
+
+// `range` keys at most, in `blocks` workgroups without a cut: as many splits as make `want` workgroups, each of `least` keys or more.
+Cut cut_keys(long range, long blocks, long want, int least, int step) {
+    long splits = blocks > 0 ? want / blocks : want, most = (range + least - 1) / least;
+    splits = splits < most ? splits : most;
+    splits = splits < 1 ? 1 : splits > 64 ? 64 : splits;
+    long keys = (range + splits - 1) / splits;
+    keys = (keys + step - 1) / step * step;
+    Cut c;
+    c.keys = (int)(keys < step ? step : keys);
+    c.splits = (int)((range + c.keys - 1) / c.keys);
+    c.splits = c.splits < 1 ? 1 : c.splits;
+    return c;
+}
 
 // Tiles and splits by the bounds that the host knows.
-Plan plan_few(const AttnArgs &a) {
+Plan plan_attn(int dtype, int d, const AttnArgs &a) {
     const int G = a.r.Hq / a.r.Hkv;
+    const long most = (long)a.max_q * G, rows = (long)a.r.T * G, N = a.c.N;
     Plan p;
-    p.tiles = (int)(((long)a.max_q * G + kFewTile - 1) / kFewTile);
+    p.few_rows = dtype == 0 ? 0x7fffffff : kFewMost;
+    const long few = most < p.few_rows ? most : p.few_rows;
+    p.tiles = (int)((few + kFewTile - 1) / kFewTile);
     if (p.tiles < 1) p.tiles = 1;
-    const long range = a.window > 0 ? (a.c.max_kv < (long)a.window + a.max_q + kFewKeys ? a.c.max_kv : (long)a.window + a.max_q + kFewKeys) : a.c.max_kv;
-    const long base = (long)(a.c.N > 0 ? a.c.N : 1) * p.tiles * a.r.Hkv;
-    long splits = 1024 / base, most = (range + 255) / 256;
-    if (splits > most) splits = most;
-    if (splits < 1) splits = 1;
-    if (splits > 64) splits = 64;
-    long keys = (range + splits - 1) / splits;
-    keys = (keys + 127) / 128 * 128;
-    if (keys < 128) keys = 128;
-    p.split_keys = (int)keys;
-    p.splits = (int)((range + keys - 1) / keys);
-    if (p.splits < 1) p.splits = 1;
+    p.slots = 0;
+    if (most > p.few_rows) { // sum of ceil(R / 128) over the sequences
+        const long by_rows = rows / kWideRows + N, by_most = N * ((most + kWideRows - 1) / kWideRows);
+        p.slots = (int)(by_rows < by_most ? by_rows : by_most);
+    }
+    auto range = [&](int step) {
+        const long seen = a.window > 0 ? (long)a.window + a.max_q + step : a.c.max_kv;
+        return seen < a.c.max_kv ? seen : (long)a.c.max_kv;
+    };
+    p.few = cut_keys(range(kFewKeys), (N > 0 ? N : 1) * p.tiles * a.r.Hkv, 1024, 256, kFewWaves * kFewKeys);
+    const long full = rows / kWideRows;
+    p.wide = p.slots ? cut_keys(range(wide_keys(d)), (full > 0 ? full : 1) * a.r.Hkv, 512, 512, wide_keys(d)) : Cut{1, 64};
     return p;
 }
 
-size_t workspace_of(const AttnArgs &a, int d, int splits) {
-    if (splits == 1) return 0;
+int most_splits(const Plan &p) { return p.few.splits > p.wide.splits ? p.few.splits : p.wide.splits; }
+size_t workspace_of(const AttnArgs &a, int d, const Plan &p) {
+    const int splits = most_splits(p);
+    if (splits == 1 || a.r.T == 0) return 0;
     const size_t rows = (size_t)splits * a.r.T * a.r.Hq;
     return (((2 * rows + 3) & ~size_t(3)) + rows * d) * sizeof(float);
 }
 
-template <typename T, typename CT, int D> int launch_attn(AttnArgs a, hipStream_t stream) {
-    Plan p = plan_few(a);
-    int max_rows = 1 << 30;
-    constexpr int lds = kFewWaves * kFewTile * (D + 4 + 2) * 4;
-    const void *fn = reinterpret_cast<const void *>(k_attn_few<T, CT, D>);
-    if constexpr (lds > 64 * 1024)
-        if (const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds)) return (int)e;
-    void *args[] = {&a, &p.tiles, &p.splits, &p.split_keys, &max_rows};
-    const long blocks = ((long)a.c.N * p.tiles + 1) * p.splits * a.r.Hkv;
+int launch(const char *name, const void *fn, long blocks, int threads, int lds, void **args, hipStream_t stream) {
     if (blocks >= (1l << 31)) return (int)hipErrorInvalidConfiguration;
-    prof_begin("k_attn_few", stream);
-    hipError_t e = hipLaunchKernel(fn, dim3((unsigned)blocks), dim3(64 * kFewWaves), args, lds, stream);
-    prof_end(stream);
-    if (e != hipSuccess || p.splits == 1) return (int)e;
-    void *jargs[] = {&a, &p.splits, &p.split_keys};
-    const long rows = (long)a.r.T * a.r.Hq;
-    prof_begin("k_attn_join", stream);
-    e = hipLaunchKernel(reinterpret_cast<const void *>(k_attn_join<T, D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), jargs, 0, stream);
+    if (lds > 64 * 1024)
+        if (const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds)) return (int)e;
+    prof_begin(name, stream);
+    const hipError_t e = hipLaunchKernel(fn, dim3((unsigned)blocks), dim3(threads), args, lds, stream);
     prof_end(stream);
     return (int)e;
 }
 
+template <typename T, typename CT, int D> int launch_attn(int dtype, AttnArgs a, hipStream_t stream) {
+    Plan p = plan_attn(dtype, D, a);
+    a.splits = most_splits(p);
+    if constexpr (sizeof(T) == 2)
+        if (p.slots) {
+            void *args[] = {&a, &p.wide, &p.few_rows};
+            if (const int e = launch("k_attn_wide", reinterpret_cast<const void *>(k_attn_wide<CT, D>), (long)p.slots * p.wide.splits * a.r.Hkv, 64 * kWideWaves,
+                                     2 * WideTile<CT, D>::SIZE, args, stream)) return e;
+        }
+    {
+        void *args[] = {&a, &p.tiles, &p.few, &p.few_rows};
+        if (const int e = launch("k_attn_few", reinterpret_cast<const void *>(k_attn_few<T, CT, D>), ((long)a.c.N * p.tiles + 1) * p.few.splits * a.r.Hkv,
+                                 64 * kFewWaves, kFewWaves * kFewTile * (D + 4 + 2) * 4, args, stream)) return e;
+    }
+    if (a.splits == 1) return 0;
+    void *args[] = {&a, &p.few, &p.wide, &p.few_rows};
+    return launch("k_attn_join", reinterpret_cast<const void *>(k_attn_join<T, D>), ((long)a.r.T * a.r.Hq + 3) / 4, 256, 0, args, stream);
+}
+
 } // namespace
 
-size_t paged_attn_workspace(int, int d, const AttnArgs &a) { return a.r.T == 0 ? 0 : workspace_of(a, d, plan_few(a).splits); }
+size_t paged_attn_workspace(int dtype, int d, const AttnArgs &a) { return workspace_of(a, d, plan_attn(dtype, d, a)); }
 
 int run_paged_attn(int dtype, int d, bool fp8_pages, const AttnArgs &a, hipStream_t stream) {
     if (a.r.T == 0) return 0;
     if (dtype == 0) {
-        if (d == 32) return launch_attn<float, float, 32>(a, stream);
-        if (d == 64) return launch_attn<float, float, 64>(a, stream);
-        if (d == 128) return launch_attn<float, float, 128>(a, stream);
+        if (d == 32) return launch_attn<float, float, 32>(dtype, a, stream);
+        if (d == 64) return launch_attn<float, float, 64>(dtype, a, stream);
+        if (d == 128) return launch_attn<float, float, 128>(dtype, a, stream);
     } else if (fp8_pages) {
-        if (d == 64) return launch_attn<bf16, fp8, 64>(a, stream);
-        if (d == 128) return launch_attn<bf16, fp8, 128>(a, stream);
-        if (d == 256) return launch_attn<bf16, fp8, 256>(a, stream);
+        if (d == 64) return launch_attn<bf16, fp8, 64>(dtype, a, stream);
+        if (d == 128) return launch_attn<bf16, fp8, 128>(dtype, a, stream);
+        if (d == 256) return launch_attn<bf16, fp8, 256>(dtype, a, stream);
     } else {
-        if (d == 64) return launch_attn<bf16, bf16, 64>(a, stream);
-        if (d == 128) return launch_attn<bf16, bf16, 128>(a, stream);
-        if (d == 256) return launch_attn<bf16, bf16, 256>(a, stream);
+        if (d == 64) return launch_attn<bf16, bf16, 64>(dtype, a, stream);
+        if (d == 128) return launch_attn<bf16, bf16, 128>(dtype, a, stream);
+        if (d == 256) return launch_attn<bf16, bf16, 256>(dtype, a, stream);
     }
     return (int)hipErrorInvalidValue;
 }
