@@ -76,14 +76,18 @@ constexpr int kFewTile = 16, kFewKeys = 32, kFewWaves = 4;
 template <typename T, typename CT> struct PageElem { typedef CT type; static constexpr int bytes = (int)sizeof(CT); };
 template <typename T> struct PageElem<T, fp8> { typedef unsigned char type; static constexpr int bytes = 1; };
 
-template <int W> __device__ inline void load_words(unsigned (&w)[W], const void *p) {
-    if constexpr (W == 1) w[0] = *static_cast<const unsigned *>(p);
-    else if constexpr (W == 2) { const uint2 x = *static_cast<const uint2 *>(p); w[0] = x.x; w[1] = x.y; }
+// W words at `off` bytes behind a descriptor's base.  (Buffer loads: the base, the same for the whole wave, stays in scalar registers, where a global load
+// would have a 64-bit address per lane and load.)
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+template <int W> __device__ inline void load_words(unsigned (&w)[W], __amdgpu_buffer_rsrc_t rs, int off) {
+    if constexpr (W == 1) w[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0);
+    else if constexpr (W == 2) { const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0); w[0] = x[0]; w[1] = x[1]; }
     else {
 #pragma unroll
         for (int i = 0; i < W / 4; ++i) {
-            const uint4 x = static_cast<const uint4 *>(p)[i];
-            w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+            const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rs, off + 16 * i, 0, 0);
+            w[4 * i] = x[0]; w[4 * i + 1] = x[1]; w[4 * i + 2] = x[2]; w[4 * i + 3] = x[3];
         }
     }
 }
@@ -93,7 +97,6 @@ __device__ inline unsigned bf16_pair(unsigned w, bool hi) {
     const bf16x2 v = hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false);
     return __builtin_bit_cast(unsigned, v);
 }
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 // eight e4m3 numbers as bf16
 __device__ inline u32x4 widen(unsigned lo, unsigned hi) { return u32x4{bf16_pair(lo, false), bf16_pair(lo, true), bf16_pair(hi, false), bf16_pair(hi, true)}; }
 
@@ -132,7 +135,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_attn_few(AttnArgs a, int til
 
     // the query: elements g KE .. g KE + KE - 1
     unsigned qw[KE * sizeof(T) / 4];
-    load_words(qw, static_cast<const T *>(a.r.q) + (long)(s.r0 + tok) * a.r.q_stride + head * D + g * KE);
+    {
+        const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const T *>(a.r.q) + (long)(s.r0 + tok) * a.r.q_stride + head * D + g * KE);
+#pragma unroll
+        for (int i = 0; i < (int)(KE * sizeof(T) / 16); ++i) { const uint4 x = src[i]; qw[4 * i] = x.x; qw[4 * i + 1] = x.y; qw[4 * i + 2] = x.z; qw[4 * i + 3] = x.w; }
+    }
     const float c = a.scale * 1.4426950408889634f;
 
     const char *kp = static_cast<const char *>(a.c.kp), *vp = static_cast<const char *>(a.c.vp);
@@ -142,7 +149,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_attn_few(AttnArgs a, int til
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const long row = row_of(a.c, page[h], k0 + 16 * h, kvh, Hkv);
-            load_words(kw[h], kp + (row * D * EB + (col * D + g * KE) * EB));
+            load_words(kw[h], make_rsrc(kp + row * (D * EB)), (col * D + g * KE) * EB);
             if constexpr (FP8) ks[h] = *reinterpret_cast<const float4 *>(a.c.ks + row + 4 * g);
         }
     };
@@ -150,8 +157,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_attn_few(AttnArgs a, int til
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const long row = row_of(a.c, page[h], k0 + 16 * h, kvh, Hkv);
+            const __amdgpu_buffer_rsrc_t va = make_rsrc(vp + row * (D * EB));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) load_words(vw[4 * h + i], vp + (row * D * EB + ((4 * g + i) * D + col * VE) * EB));
+            for (int i = 0; i < 4; ++i) load_words(vw[4 * h + i], va, ((4 * g + i) * D + col * VE) * EB);
             if constexpr (FP8) vs[h] = *reinterpret_cast<const float4 *>(a.c.vs + row + 4 * g);
         }
     };
@@ -340,7 +348,7 @@ template <typename CT, int D> struct WideTile {
 
 // The sequence and the row tile that a slot stands for: slots count the tiles of 128 rows of the sequences with more than `few` rows.
 // Later tiles see more keys and come first, so that the workgroups that start last are short: of each 64 sequences the last tiles, then the ones
-// before those, and so on (in the order of the sequences, prompts of 4 x 2048 tokens took 160 us instead of TIMEHERE).  False past the last slot.
+// before those, and so on (in the order of the sequences, prompts of 4 x 2048 tokens took 160 us instead of 126).  False past the last slot.
 __device__ inline bool tile_of_slot(const AttnArgs &a, int G, int few, int slot, int *seq, int *tile) {
     const int lane = threadIdx.x & 63;
     for (int base = 0; base < a.c.N; base += 64) {
@@ -373,7 +381,7 @@ __device__ inline bool tile_of_slot(const AttnArgs &a, int G, int few, int slot,
 }
 
 template <typename CT, int D>
-__global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(AttnArgs a, Cut cut, int few) {
+__global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(AttnArgs a, Cut cut, int few, int zero) {
     const int splits = cut.splits, split_keys = cut.keys;
     using W = WideTile<CT, D>;
     constexpr bool FP8 = W::FP8;
@@ -385,6 +393,7 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(
     const int kvh = b % Hkv; b /= Hkv;
     const int split = b % splits, slot = b / splits;
     int n, tile;
+    if (zero && split == 0 && (slot + 1) * splits * Hkv == gridDim.x) zero_rest<bf16, D>(a, kvh, G);
     if (!tile_of_slot(a, G, few, slot, &n, &tile)) return;
     n = __builtin_amdgcn_readfirstlane(n);
     tile = __builtin_amdgcn_readfirstlane(tile);
@@ -433,9 +442,9 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(
         for (int i = 0; i < W::NL; ++i) {
             const int r0 = (i * 256 + wave * 64) / W::LPR, kk = k0 + (r0 & ~15); // the wave's rows lie in one group of 16 keys
             const long at = row_of(a.c, __builtin_amdgcn_readfirstlane(page_id(a.c, page[i])), kk, kvh, Hkv) * (D * EB);
-            const int off = ((r0 & 15) + lane / W::LPR) * (D * EB) + piece * 16;
-            rk[i] = *reinterpret_cast<const u32x4 *>(kp + at + off);
-            rv[i] = *reinterpret_cast<const u32x4 *>(vp + at + off);
+            const unsigned off = ((r0 & 15) + lane / W::LPR) * (D * EB) + piece * 16;
+            rk[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(kp + at), off, 0, 0);
+            rv[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(vp + at), off, 0, 0);
         }
         if constexpr (FP8)
             if (wave < 2 && lane < KEYS) rs = (wave ? a.c.vs : a.c.ks)[row_of(a.c, page_id(a.c, spage), k0 + (lane & 48), kvh, Hkv) + (lane & 15)];
@@ -591,64 +600,93 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(
     }
 }
 
-// Joins the splits of every row (a wave per row and head).  Where a launch splits the rows of one kind only, the others' outputs are there.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, Cut few, Cut wide, int few_rows) {
+// Joins the splits of a row (token and head).  FEW: of the sequences that k_attn_few takes, a workgroup per row, since there are few rows and up to
+// kMostSplits splits (1 x 16 heads, 64 splits of 128: a wave per row took 17 us, one load after the other); else a wave per row of the others.
+template <typename T, int D, bool FEW>
+__global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, Cut cut, int few_rows, int per_seq) {
+    constexpr int LPR = D / 4, TPR = FEW ? 256 : 64, SIDE = TPR / LPR; // lanes of a row, threads of a row, splits side by side
+    __shared__ float part[FEW ? 4 : 1][D + 4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const long row = (long)blockIdx.x * 4 + wave;
-    if (row >= (long)a.r.T * a.r.Hq) return;
-    const int t = (int)(row / a.r.Hq), h = (int)(row % a.r.Hq), G = a.r.Hq / a.r.Hkv;
-    const int n = seq_of_row(a.c.cu, a.c.N, t);
-    if (n >= a.c.N) return; // (zeroed)
+    const int G = a.r.Hq / a.r.Hkv;
+    int n, kvh, r;
     SeqRows s;
-    s.load(a, n);
-    const int R = (s.r1 - s.r0) * G, r = max(t - s.r0, 0) * G + h % G;
-    const Cut cut = R > few_rows ? wide : few;
-    if (cut.splits == 1) return;
-    const int rows = R > few_rows ? kWideRows : kFewTile, row0 = r / rows * rows;
+    if (FEW) {
+        int b = blockIdx.x;
+        r = b % per_seq; b /= per_seq;
+        kvh = b % a.r.Hkv; n = b / a.r.Hkv;
+        s.load(a, n);
+        const int R = (s.r1 - s.r0) * G;
+        if (r >= R || R > few_rows) return;
+    } else {
+        const long row = (long)blockIdx.x * 4 + wave;
+        if (row >= (long)a.r.T * a.r.Hq) return;
+        const int t = (int)(row / a.r.Hq), h = (int)(row % a.r.Hq);
+        n = seq_of_row(a.c.cu, a.c.N, t);
+        if (n >= a.c.N) return; // (zeroed)
+        s.load(a, n);
+        kvh = h / G; r = max(t - s.r0, 0) * G + h % G;
+        if ((s.r1 - s.r0) * G <= few_rows) return;
+    }
+    constexpr int ROWS = FEW ? kFewTile : kWideRows;
     int lo, hi;
-    key_range(a, s, G, row0, min(row0 + rows, R), R > few_rows ? wide_keys(D) : kFewKeys, lo, hi);
+    key_range(a, s, G, r / ROWS * ROWS, min(r / ROWS * ROWS + ROWS, (s.r1 - s.r0) * G), FEW ? kFewKeys : wide_keys(D), lo, hi);
     const int live = hi > lo ? min((hi - lo + cut.keys - 1) / cut.keys, cut.splits) : 0;
-    constexpr int E = D >= 64 ? D / 64 : 1;
-    const bool on = lane * E < D;
-    float M = kNoScore, L = 0.f, acc[E];
+    const long row = (long)(s.r0 + r / G) * a.r.Hq + kvh * G + r % G;
+    const int in = FEW ? threadIdx.x : lane, e0 = in % LPR * 4, side = in / LPR;
     float *ml, *po;
+    float M = kNoScore;
     for (int i = lane; i < live; i += 64) {
         partial_of(a, i, row, D, &ml, &po);
         M = fmaxf(M, ml[0]);
     }
     M = lanes_max<64>(M);
-#pragma unroll
-    for (int j = 0; j < E; ++j) acc[j] = 0.f;
-    for (int i = 0; i < live; ++i) {
+    float L = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = side; i < live; i += SIDE) {
         partial_of(a, i, row, D, &ml, &po);
         const float f = __builtin_amdgcn_exp2f(ml[0] - M);
         L = fmaf(ml[1], f, L);
-        if (on) {
+        acc += *reinterpret_cast<const f32x4 *>(po + e0) * f;
+    }
 #pragma unroll
-            for (int j = 0; j < E; ++j) acc[j] = fmaf(po[lane * E + j], f, acc[j]);
+    for (int m = LPR; m < 64; m <<= 1) {
+        L += __shfl_xor(L, m);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], m);
+    }
+    if (FEW) {
+        if (lane < LPR) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) part[wave][e0 + j] = acc[j];
+            if (lane == 0) part[wave][D] = L;
         }
-    }
-    const float inv = inverse_sum(L);
-    T *to = static_cast<T *>(a.r.q_out) + row * D + lane * E;
-    if (on) {
+        __syncthreads();
+        if (threadIdx.x >= LPR) return;
+        L = (part[0][D] + part[1][D]) + (part[2][D] + part[3][D]);
 #pragma unroll
-        for (int j = 0; j < E; ++j) to[j] = (T)(acc[j] * inv);
-    }
+        for (int j = 0; j < 4; ++j) acc[j] = (part[0][e0 + j] + part[1][e0 + j]) + (part[2][e0 + j] + part[3][e0 + j]);
+    } else if (lane >= LPR) return;
+    const float inv = inverse_sum(L);
+    typedef T out4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<out4 *>(static_cast<T *>(a.r.q_out) + row * D + e0) = out4{(T)(acc[0] * inv), (T)(acc[1] * inv), (T)(acc[2] * inv), (T)(acc[3] * inv)};
 }
 
 namespace {
 
 // Rows of a sequence and key/value head up to which the kernel for few rows takes them (fp32: always).
 constexpr int kFewMost = 32;
+constexpr int kMostSplits = 128;
 
-struct Plan { int few_rows, tiles, slots; Cut few, wide; };
+// per_seq: most rows of a sequence and key/value head that k_attn_few has (0: it is not launched); slots: row tiles of k_attn_wide, one more if it
+// zeroes the rows that lie in no sequence
+struct Plan { int few_rows, per_seq, tiles, slots; Cut few, wide; };
 
-// `range` keys at most, in `blocks` workgroups without a cut: as many splits as make `want` workgroups, each of `least` keys or more.
+// `range` keys at most, in `blocks` workgroups without a cut: as many splits as make about `want` workgroups, each of `least` keys or more.
 Cut cut_keys(long range, long blocks, long want, int least, int step) {
-    long splits = blocks > 0 ? want / blocks : want, most = (range + least - 1) / least;
+    long splits = (want + blocks / 2) / blocks, most = (range + least - 1) / least;
     splits = splits < most ? splits : most;
-    splits = splits < 1 ? 1 : splits > 64 ? 64 : splits;
+    splits = splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits;
     long keys = (range + splits - 1) / splits;
     keys = (keys + step - 1) / step * step;
     Cut c;
@@ -663,22 +701,24 @@ Plan plan_attn(int dtype, int d, const AttnArgs &a) {
     const int G = a.r.Hq / a.r.Hkv;
     const long most = (long)a.max_q * G, rows = (long)a.r.T * G, N = a.c.N;
     Plan p;
-    p.few_rows = dtype == 0 ? 0x7fffffff : kFewMost;
-    const long few = most < p.few_rows ? most : p.few_rows;
-    p.tiles = (int)((few + kFewTile - 1) / kFewTile);
-    if (p.tiles < 1) p.tiles = 1;
+    // A batch of equal chunks has none of few rows where the bounds are exact; should they not be (padded rows), k_attn_wide is right for those too.
+    const bool equal = dtype != 0 && most > kFewMost && N * a.max_q == a.r.T;
+    p.few_rows = dtype == 0 ? 0x7fffffff : equal ? 0 : kFewMost;
+    p.per_seq = (int)(most < p.few_rows ? most : p.few_rows);
+    p.tiles = (p.per_seq + kFewTile - 1) / kFewTile;
     p.slots = 0;
     if (most > p.few_rows) { // sum of ceil(R / 128) over the sequences
         const long by_rows = rows / kWideRows + N, by_most = N * ((most + kWideRows - 1) / kWideRows);
-        p.slots = (int)(by_rows < by_most ? by_rows : by_most);
+        p.slots = (int)(by_rows < by_most ? by_rows : by_most) + (equal ? 1 : 0);
     }
+    if (p.tiles < 1 && !p.slots) p.tiles = 1; // (it also zeroes the rows that lie in no sequence)
     auto range = [&](int step) {
         const long seen = a.window > 0 ? (long)a.window + a.max_q + step : a.c.max_kv;
         return seen < a.c.max_kv ? seen : (long)a.c.max_kv;
     };
-    p.few = cut_keys(range(kFewKeys), (N > 0 ? N : 1) * p.tiles * a.r.Hkv, 1024, 256, kFewWaves * kFewKeys);
+    p.few = p.tiles ? cut_keys(range(kFewKeys), (N > 0 ? N : 1) * p.tiles * a.r.Hkv, 1024, 256, kFewWaves * kFewKeys) : Cut{1, 128};
     const long full = rows / kWideRows;
-    p.wide = p.slots ? cut_keys(range(wide_keys(d)), (full > 0 ? full : 1) * a.r.Hkv, 512, 512, wide_keys(d)) : Cut{1, 64};
+    p.wide = p.slots ? cut_keys(range(wide_keys(d)), (full > 0 ? full : 1) * a.r.Hkv, d > 128 ? 256 : d > 64 ? 512 : 768, 512, wide_keys(d)) : Cut{1, 64};
     return p;
 }
 
@@ -705,18 +745,21 @@ template <typename T, typename CT, int D> int launch_attn(int dtype, AttnArgs a,
     a.splits = most_splits(p);
     if constexpr (sizeof(T) == 2)
         if (p.slots) {
-            void *args[] = {&a, &p.wide, &p.few_rows};
+            int zero = p.tiles == 0;
+            void *args[] = {&a, &p.wide, &p.few_rows, &zero};
             if (const int e = launch("k_attn_wide", reinterpret_cast<const void *>(k_attn_wide<CT, D>), (long)p.slots * p.wide.splits * a.r.Hkv, 64 * kWideWaves,
                                      2 * WideTile<CT, D>::SIZE, args, stream)) return e;
+            void *join[] = {&a, &p.wide, &p.few_rows, &p.per_seq};
+            if (p.wide.splits > 1)
+                if (const int e = launch("k_attn_join", reinterpret_cast<const void *>(k_attn_join<T, D, false>), ((long)a.r.T * a.r.Hq + 3) / 4, 256, 0, join, stream)) return e;
         }
-    {
-        void *args[] = {&a, &p.tiles, &p.few, &p.few_rows};
-        if (const int e = launch("k_attn_few", reinterpret_cast<const void *>(k_attn_few<T, CT, D>), ((long)a.c.N * p.tiles + 1) * p.few.splits * a.r.Hkv,
-                                 64 * kFewWaves, kFewWaves * kFewTile * (D + 4 + 2) * 4, args, stream)) return e;
-    }
-    if (a.splits == 1) return 0;
-    void *args[] = {&a, &p.few, &p.wide, &p.few_rows};
-    return launch("k_attn_join", reinterpret_cast<const void *>(k_attn_join<T, D>), ((long)a.r.T * a.r.Hq + 3) / 4, 256, 0, args, stream);
+    if (p.tiles == 0) return 0;
+    void *args[] = {&a, &p.tiles, &p.few, &p.few_rows};
+    if (const int e = launch("k_attn_few", reinterpret_cast<const void *>(k_attn_few<T, CT, D>), ((long)a.c.N * p.tiles + 1) * p.few.splits * a.r.Hkv,
+                             64 * kFewWaves, kFewWaves * kFewTile * (D + 4 + 2) * 4, args, stream)) return e;
+    if (p.few.splits == 1) return 0;
+    void *join[] = {&a, &p.few, &p.few_rows, &p.per_seq};
+    return launch("k_attn_join", reinterpret_cast<const void *>(k_attn_join<T, D, true>), (long)a.c.N * a.r.Hkv * p.per_seq, 256, 0, join, stream);
 }
 
 } // namespace
