@@ -1,4 +1,5 @@
-"""Builds libdeltanet_hip.so in-tree with hipcc for gfx950 (one object per .hip file, in parallel)."""
+"""Builds libdeltanet_hip.so in-tree with hipcc for gfx950 (one object per .hip file, in parallel), and the Python module that calls its
+attention operators with tensors (_attention.so, host code against torch's headers)."""
 from __future__ import annotations
 
 import os
@@ -9,6 +10,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libdeltanet_hip.so")
+BINDING = os.path.join(HERE, "_attention.so")
 SOURCES = ["dn_api.hip", "dn_inst_f32.hip", "dn_inst_bf16.hip", "dn_inst_bf16_wide.hip", "dn_recurrent.hip", "dn_noalloc.hip", "dn_lds_probe.hip",
            "dn_attn_api.hip", "dn_norm_rope.hip", "dn_paged_attn.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
@@ -29,9 +31,29 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _compile_binding() -> None:
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    tmp = BINDING + ".tmp.%d" % os.getpid()
+    r = subprocess.run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+                        "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+                        "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "dn_attention_binding.cpp"), "-o", tmp,
+                        "-L" + os.path.join(root, "lib"), "-Wl,-rpath," + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-ldl"],
+                       capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed on dn_attention_binding.cpp:\n" + r.stderr)
+    if r.stderr.strip():
+        sys.stderr.write(r.stderr)
+    os.replace(tmp, BINDING)
+
+
 def build(verbose: bool = True) -> str:
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        binding = ex.submit(_compile_binding)
         objs = list(ex.map(_compile, SOURCES))
+        binding.result()
     tmp = OUT + ".tmp.%d" % os.getpid()
     subprocess.check_call(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs)
     os.replace(tmp, OUT)

@@ -682,9 +682,9 @@ constexpr int kMostSplits = 128;
 // zeroes the rows that lie in no sequence
 struct Plan { int few_rows, per_seq, tiles, slots; Cut few, wide; };
 
-// `range` keys at most, in `blocks` workgroups without a cut: as many splits as make about `want` workgroups, each of `least` keys or more.
+// `range` keys at most, in `blocks` workgroups without a cut: as many splits as make up to `want` workgroups, each of `least` keys or more.
 Cut cut_keys(long range, long blocks, long want, int least, int step) {
-    long splits = (want + blocks / 2) / blocks, most = (range + least - 1) / least;
+    long splits = want / blocks, most = (range + least - 1) / least;
     splits = splits < most ? splits : most;
     splits = splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits;
     long keys = (range + splits - 1) / splits;
