@@ -72,21 +72,32 @@ template <typename T, int V> __device__ inline void load_weight(const void *w, i
     }
 }
 
-// Loads of up to NB heads' words are requested before the first is worked on.
+// Loads of up to this many steps (64 / lanes of a row heads each) are requested before the first is worked on.
 constexpr int kRowBatch = 4;
 
-// y of the words w[], in fp32
-template <typename T, int D> struct NormTurn {
+// The weight at the lane's elements and at their pairs' other ones.
+template <typename T, int D> struct Weights {
     using L = RowLayout<T, D>;
-    float w[L::V], wo[L::V]; // the weight at the lane's elements and at their pairs' other ones
-    Turn<L::V> turn;
-    __device__ inline void load_w(const RowArgs &a, const void *weight, int e0) {
+    float w[L::V], wo[L::V];
+    __device__ inline void load(const RowArgs &a, const void *weight, int e0) {
         load_weight<T>(weight, e0, w);
         if (e0 < a.rot && !a.interleaved) load_weight<T>(weight, e0 < (a.rot >> 1) ? e0 + (a.rot >> 1) : e0 - (a.rot >> 1), wo);
         else {
 #pragma unroll
             for (int i = 0; i < L::V; ++i) wo[i] = w[i ^ 1];
         }
+    }
+};
+
+// y of a row: r (x c w + other s wo), with the factors of a token's heads formed once (they are the same for all of a tensor's heads, and the
+// vector ALU, not only the memory, would bound a pass that forms them for each).
+template <typename T, int D> struct NormTurn {
+    using L = RowLayout<T, D>;
+    Turn<L::V> turn; // c w, s wo
+    __device__ inline void load(const RowArgs &a, const Weights<T, D> &w, int e0, int pos) {
+        turn.load(a, e0, pos);
+#pragma unroll
+        for (int i = 0; i < L::V; ++i) { turn.c[i] *= w.w[i]; turn.s[i] *= w.wo[i]; }
     }
     __device__ inline void apply(const RowArgs &a, const uint4 &x, float (&y)[L::V]) const {
         float own[L::V], oth[L::V], ss = 0.f;
@@ -96,10 +107,7 @@ template <typename T, int D> struct NormTurn {
         const float r = rsqrtf(lanes_sum<L::LPR>(ss) * (1.f / D) + a.eps);
         turn.template others<T>(a, x, own, oth);
 #pragma unroll
-        for (int i = 0; i < L::V; ++i) {
-            const float z = own[i] * r * w[i];
-            y[i] = fmaf(z, turn.c[i], oth[i] * r * wo[i] * turn.s[i]);
-        }
+        for (int i = 0; i < L::V; ++i) y[i] = r * fmaf(own[i], turn.c[i], oth[i] * turn.s[i]);
     }
 };
 
@@ -113,11 +121,12 @@ __global__ __launch_bounds__(256) void k_norm_rope_fwd(RowArgs a) {
     const T *in = static_cast<const T *>(is_q ? a.q : a.k);
     T *out = static_cast<T *>(is_q ? a.q_out : a.k_out);
     NormTurn<T, D> nt;
-    nt.load_w(a, is_q ? a.qw : a.kw, e0);
+    Weights<T, D> w;
+    w.load(a, is_q ? a.qw : a.kw, e0);
     for (int t = blockIdx.x * 4 + (threadIdx.x >> 6); t < a.T; t += gridDim.x * 4) {
         const T *row = in + t * stride;
         T *to = out + (long)t * H * D;
-        nt.turn.load(a, e0, a.positions ? a.positions[t] : t % a.seq_len);
+        nt.load(a, w, e0, a.positions ? a.positions[t] : t % a.seq_len);
         for (int h0 = 0; h0 < H; h0 += kRowBatch * L::RPW) {
             uint4 x[kRowBatch];
 #pragma unroll
@@ -127,6 +136,7 @@ __global__ __launch_bounds__(256) void k_norm_rope_fwd(RowArgs a) {
             }
 #pragma unroll
             for (int b = 0; b < kRowBatch; ++b) {
+                if (h0 + b * L::RPW >= H) break;
                 const int h = h0 + b * L::RPW + sub;
                 float y[L::V];
                 nt.apply(a, x[b], y);
@@ -166,6 +176,7 @@ __global__ __launch_bounds__(256) void k_norm_rope_bwd(RowArgs a) {
             }
 #pragma unroll
             for (int b = 0; b < kRowBatch; ++b) {
+                if (h0 + b * L::RPW >= H) break;
                 const int h = h0 + b * L::RPW + sub;
                 float xf[L::V], own[L::V], oth[L::V], ss = 0.f, gx = 0.f;
                 unpack16<T>(x[b], xf);
@@ -202,20 +213,21 @@ __global__ __launch_bounds__(256) void k_norm_rope_bwd(RowArgs a) {
         a.partial[((long)blockIdx.x * 2 + blockIdx.y) * D + e] = (part[0][e] + part[1][e]) + (part[2][e] + part[3][e]);
 }
 
-// Sums the workgroups' partial weight gradients: a workgroup takes 16 elements, 16 threads each, every sixteenth partial per thread.
-__global__ __launch_bounds__(256) void k_weight_grad(RowArgs a, int D, int blocks) {
-    __shared__ float part[16][17];
+// Sums the workgroups' partial weight gradients: 64 threads per element, each every 64th partial.
+__global__ __launch_bounds__(1024) void k_weight_grad(RowArgs a, int D, int blocks) {
+    __shared__ float part[64][17];
     const int e = blockIdx.x * 16 + (threadIdx.x & 15), of = threadIdx.x >> 4; // D is a multiple of 16
     float *to = blockIdx.y == 0 ? a.dqw : a.dkw;
     if (!to) return;
     float s = 0.f;
-    for (int b = of; b < blocks; b += 16) s += a.partial[((long)b * 2 + blockIdx.y) * D + e];
+#pragma unroll 8
+    for (int b = of; b < blocks; b += 64) s += a.partial[((long)b * 2 + blockIdx.y) * D + e];
     part[of][threadIdx.x & 15] = s;
     __syncthreads();
     if (of == 0) {
         s = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s += part[i][threadIdx.x];
+        for (int i = 0; i < 64; ++i) s += part[i][threadIdx.x];
         to[e] = s;
     }
 }
@@ -258,29 +270,36 @@ __device__ inline void cache_row(void *pages, float *scale, long row, int e0, co
     } else if (live) *reinterpret_cast<uint4 *>(static_cast<T *>(pages) + row * D + e0) = pack16<T>(y);
 }
 
-// New tokens: blockIdx.y = 0: k, 1: v, 2: q (only with NORM, which also normalises and rotates k).
+// New tokens, a wave per token (and, where there are few, per tensor and block of heads): k, v and, with NORM, which also normalises and rotates k, q.
+// Finding the token's place takes three loads in a row (its sequence, the context's length, the page), about as long as the rows' way
+// here, so the first rows are requested before and all tensors of a token share one search.
 template <typename T, typename CT, int D, bool NORM>
 __global__ __launch_bounds__(256) void k_paged_append(RowArgs a, PagedArgs c) {
     using L = RowLayout<T, D>;
+    constexpr int PER = kRowBatch * L::RPW; // heads of a batch
     const int lane = threadIdx.x & 63, e0 = (lane % L::LPR) * L::V, sub = lane / L::LPR;
-    const int t = blockIdx.x * 4 + (threadIdx.x >> 6), what = blockIdx.y;
+    const int t = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (t >= a.T) return;
-    const int H = what == 2 ? a.Hq : a.Hkv;
-    const long stride = what == 0 ? a.k_stride : what == 1 ? a.v_stride : a.q_stride;
-    const T *row = static_cast<const T *>(what == 0 ? a.k : what == 1 ? a.v : a.q) + t * stride;
+    // batches: those of q, then k, then v
+    const int bq = NORM ? (a.Hq + PER - 1) / PER : 0, bkv = (a.Hkv + PER - 1) / PER, all = bq + 2 * bkv;
+    int i = blockIdx.y;
     uint4 x[kRowBatch];
-    auto fetch = [&](int h0) {
+    auto heads_of = [&](int i, int &what, int &h0) { // 0: q, 1: k, 2: v
+        what = i < bq ? 0 : i < bq + bkv ? 1 : 2;
+        h0 = (i - (what == 0 ? 0 : what == 1 ? bq : bq + bkv)) * PER;
+    };
+    auto fetch = [&](int i) __attribute__((always_inline)) {
+        int what, h0;
+        heads_of(i, what, h0);
+        const T *row = static_cast<const T *>(what == 0 ? a.q : what == 1 ? a.k : a.v) + t * (what == 0 ? a.q_stride : what == 1 ? a.k_stride : a.v_stride);
+        const int H = what == 0 ? a.Hq : a.Hkv;
 #pragma unroll
         for (int b = 0; b < kRowBatch; ++b) {
             const int h = h0 + b * L::RPW + sub;
             x[b] = h < H ? *reinterpret_cast<const uint4 *>(row + h * D + e0) : make_uint4(0, 0, 0, 0);
         }
     };
-    const int hb = blockIdx.z * kRowBatch * L::RPW; // heads of this workgroup
-    if (hb >= H) return;
-    fetch(hb); // on its way while the row's place is looked up
-    NormTurn<T, D> nt;
-    if (NORM && what != 1) nt.load_w(a, what == 0 ? a.kw : a.qw, e0);
+    fetch(i);
     const int n = seq_of_row(c.cu, c.N, t);
     int pos = -1;
     Slot s{0, 0};
@@ -289,22 +308,35 @@ __global__ __launch_bounds__(256) void k_paged_append(RowArgs a, PagedArgs c) {
         pos = min(c.kv_len[n], c.max_kv) - c.cu[n + 1] + t;
         live = slot_of(c, n, pos, a.Hkv, false, &s);
     }
-    if (NORM && what != 1) nt.turn.load(a, e0, pos);
-    for (int h0 = hb;;) {
+    NormTurn<T, D> nt;
+    for (int with = -1;;) {
+        int what, h0;
+        heads_of(i, what, h0);
+        if (NORM && what != 2 && what != with) {
+            Weights<T, D> w;
+            w.load(a, what == 0 ? a.qw : a.kw, e0);
+            nt.load(a, w, e0, pos);
+            with = what;
+        }
+        const int H = what == 0 ? a.Hq : a.Hkv, next = i + gridDim.y;
+        uint4 now[kRowBatch];
+#pragma unroll
+        for (int b = 0; b < kRowBatch; ++b) now[b] = x[b];
+        if (next < all) fetch(next);
 #pragma unroll
         for (int b = 0; b < kRowBatch; ++b) {
+            if (h0 + b * L::RPW >= H) break;
             const int h = h0 + b * L::RPW + sub;
             float y[L::V];
-            if (NORM && what != 1) nt.apply(a, x[b], y);
-            else unpack16<T>(x[b], y);
-            if (what == 2) {
+            if (NORM && what != 2) nt.apply(a, now[b], y);
+            else unpack16<T>(now[b], y);
+            if (what == 0) {
                 if (h < H) *reinterpret_cast<uint4 *>(static_cast<T *>(a.q_out) + ((long)t * H + h) * D + e0) = pack16<T>(y);
             } else
-                cache_row<T, CT, D>(what == 0 ? c.kp : c.vp, what == 0 ? c.ks : c.vs, s.base + (long)h * s.stride, e0, y, live && h < H);
+                cache_row<T, CT, D>(what == 1 ? c.kp : c.vp, what == 1 ? c.ks : c.vs, s.base + (long)h * s.stride, e0, y, live && h < H);
         }
-        h0 += gridDim.z * kRowBatch * L::RPW;
-        if (h0 >= H) break;
-        fetch(h0);
+        if (next >= all) return;
+        i = next;
     }
 }
 
@@ -341,6 +373,7 @@ __global__ __launch_bounds__(256) void k_paged_read(RowArgs a, PagedArgs c) {
         }
 #pragma unroll
         for (int b = 0; b < kRowBatch; ++b) {
+            if (h0 + b * L::RPW >= a.Hkv) break;
             const int h = h0 + b * L::RPW + sub;
             if constexpr (__is_same(CT, fp8)) {
                 float y[8];
@@ -356,9 +389,9 @@ __global__ __launch_bounds__(256) void k_paged_read(RowArgs a, PagedArgs c) {
 
 namespace {
 
-int launch(const char *name, const void *fn, dim3 grid, void **args, hipStream_t stream) {
+int launch(const char *name, const void *fn, dim3 grid, void **args, hipStream_t stream, int threads = 256) {
     prof_begin(name, stream);
-    const hipError_t e = hipLaunchKernel(fn, grid, dim3(256), args, 0, stream);
+    const hipError_t e = hipLaunchKernel(fn, grid, dim3(threads), args, 0, stream);
     prof_end(stream);
     return (int)e;
 }
@@ -401,13 +434,13 @@ struct BwdLaunch {
         }
         if (!a.dqw && !a.dkw) return 0;
         void *args[] = {&a, &d, &blocks};
-        return launch("k_weight_grad", reinterpret_cast<const void *>(k_weight_grad), dim3(D / 16, 2), args, stream);
+        return launch("k_weight_grad", reinterpret_cast<const void *>(k_weight_grad), dim3(D / 16, 2), args, stream, 1024);
     }
 };
-// heads of one token are spread over workgroups where there are few tokens
-template <typename T, int D> int head_blocks(int T_rows, int H) {
-    const int per = kRowBatch * RowLayout<T, D>::RPW, most = (H + per - 1) / per;
-    return T_rows >= 1024 ? 1 : most;
+// The batches of a token are spread over waves where there are few tokens.
+template <typename T, int D> int batch_blocks(int tokens, int Hq, int Hkv) {
+    const int per = kRowBatch * RowLayout<T, D>::RPW, all = (Hq + per - 1) / per + 2 * ((Hkv + per - 1) / per);
+    return tokens >= 2048 ? 1 : all;
 }
 struct AppendLaunch {
     RowArgs a;
@@ -421,7 +454,7 @@ struct AppendLaunch {
             if (fp8_pages) fn = norm ? reinterpret_cast<const void *>(k_paged_append<T, fp8, D, true>) : reinterpret_cast<const void *>(k_paged_append<T, fp8, D, false>);
             else fn = norm ? reinterpret_cast<const void *>(k_paged_append<T, T, D, true>) : reinterpret_cast<const void *>(k_paged_append<T, T, D, false>);
         } else fn = norm ? reinterpret_cast<const void *>(k_paged_append<T, T, D, true>) : reinterpret_cast<const void *>(k_paged_append<T, T, D, false>);
-        return launch("k_paged_append", fn, dim3((a.T + 3) / 4, norm ? 3 : 2, head_blocks<T, D>(a.T, norm ? a.Hq : a.Hkv)), args, stream);
+        return launch("k_paged_append", fn, dim3((a.T + 3) / 4, batch_blocks<T, D>(a.T, norm ? a.Hq : 0, a.Hkv)), args, stream);
     }
 };
 struct ReadLaunch {
