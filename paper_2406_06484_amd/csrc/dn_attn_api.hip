@@ -51,6 +51,7 @@ int check_paged(const dn_paged_shape *s) {
     if (s->num_seqs < 0 || s->num_seqs > 65535 || s->num_pages < 0 || s->max_pages < 0 || s->max_q < 0 || s->max_kv < 0) return DN_ERR_SHAPE;
     if (s->max_q > s->T || (long long)s->max_kv > (long long)s->max_pages * ps) return DN_ERR_SHAPE;
     if (s->num_pages == 0 && s->max_kv > 0) return DN_ERR_SHAPE;
+    if ((long long)s->Hkv * ps * s->d * elem_bytes(s->dtype) >= (1ll << 30)) return DN_ERR_SHAPE; // a page lies within a buffer descriptor's range
     return DN_OK;
 }
 

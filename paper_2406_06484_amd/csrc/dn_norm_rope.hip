@@ -21,18 +21,18 @@ template <typename T, int D> struct RowLayout {
 
 // What a lane needs to turn its V elements: out_i = own_i c_i + other_i s_i, where `other` is the pair's other element and the
 // sign is in s; the transposed turn is own_i c_i - other_i s_i.  Elements past the rotated ones have c = 1, s = 0.
-template <int V> struct Turn {
+// IL: pairs are neighbours, else halves.
+template <int V, bool IL> struct Turn {
     float c[V], s[V];
     int from; // the lane that holds the others (halves); unused for neighbours
-    __device__ inline void load(const RowArgs &a, int e0, int pos) {
+    __device__ static inline const float *row_of(const RowArgs &a, int pos) { return a.cs + (long)min(max(pos, 0), a.max_pos - 1) * a.rot; }
+    __device__ inline void load(const RowArgs &a, int e0, const float *row) {
         const int lane = threadIdx.x & 63, half = a.rot >> 1;
         from = lane;
 #pragma unroll
         for (int i = 0; i < V; ++i) { c[i] = 1.f; s[i] = 0.f; }
         if (e0 >= a.rot) return;
-        pos = min(max(pos, 0), a.max_pos - 1);
-        const float *row = a.cs + (long)pos * a.rot;
-        if (a.interleaved) {
+        if constexpr (IL) {
 #pragma unroll
             for (int i = 0; i < V / 2; ++i) {
                 const float co = row[e0 / 2 + i], si = row[half + e0 / 2 + i];
@@ -52,15 +52,14 @@ template <int V> struct Turn {
         }
     }
     // the others of the elements in word w (the whole wave takes part)
-    template <typename T> __device__ inline void others(const RowArgs &a, const uint4 &w, const float (&own)[V], float (&o)[V]) const {
-        if (a.interleaved) {
+    template <typename T> __device__ inline void others(const uint4 &w, const float (&own)[V], float (&o)[V]) const {
+        if constexpr (IL) {
 #pragma unroll
             for (int i = 0; i < V; ++i) o[i] = own[i ^ 1];
             return;
         }
-        uint4 x;
-        x.x = __shfl(w.x, from); x.y = __shfl(w.y, from); x.z = __shfl(w.z, from); x.w = __shfl(w.w, from);
-        unpack16<T>(x, o);
+        auto get = [this](unsigned v) { return (unsigned)__builtin_amdgcn_ds_bpermute(4 * from, (int)v); };
+        unpack16<T>(make_uint4(get(w.x), get(w.y), get(w.z), get(w.w)), o);
     }
 };
 
@@ -76,12 +75,12 @@ template <typename T, int V> __device__ inline void load_weight(const void *w, i
 constexpr int kRowBatch = 4;
 
 // The weight at the lane's elements and at their pairs' other ones.
-template <typename T, int D> struct Weights {
+template <typename T, int D, bool IL> struct Weights {
     using L = RowLayout<T, D>;
     float w[L::V], wo[L::V];
     __device__ inline void load(const RowArgs &a, const void *weight, int e0) {
         load_weight<T>(weight, e0, w);
-        if (e0 < a.rot && !a.interleaved) load_weight<T>(weight, e0 < (a.rot >> 1) ? e0 + (a.rot >> 1) : e0 - (a.rot >> 1), wo);
+        if (!IL && e0 < a.rot) load_weight<T>(weight, e0 < (a.rot >> 1) ? e0 + (a.rot >> 1) : e0 - (a.rot >> 1), wo);
         else {
 #pragma unroll
             for (int i = 0; i < L::V; ++i) wo[i] = w[i ^ 1];
@@ -91,11 +90,11 @@ template <typename T, int D> struct Weights {
 
 // y of a row: r (x c w + other s wo), with the factors of a token's heads formed once (they are the same for all of a tensor's heads, and the
 // vector ALU, not only the memory, would bound a pass that forms them for each).
-template <typename T, int D> struct NormTurn {
+template <typename T, int D, bool IL> struct NormTurn {
     using L = RowLayout<T, D>;
-    Turn<L::V> turn; // c w, s wo
-    __device__ inline void load(const RowArgs &a, const Weights<T, D> &w, int e0, int pos) {
-        turn.load(a, e0, pos);
+    Turn<L::V, IL> turn; // c w, s wo
+    __device__ inline void load(const RowArgs &a, const Weights<T, D, IL> &w, int e0, const float *row) {
+        turn.load(a, e0, row);
 #pragma unroll
         for (int i = 0; i < L::V; ++i) { turn.c[i] *= w.w[i]; turn.s[i] *= w.wo[i]; }
     }
@@ -105,13 +104,13 @@ template <typename T, int D> struct NormTurn {
 #pragma unroll
         for (int i = 0; i < L::V; ++i) ss = fmaf(own[i], own[i], ss);
         const float r = rsqrtf(lanes_sum<L::LPR>(ss) * (1.f / D) + a.eps);
-        turn.template others<T>(a, x, own, oth);
+        turn.template others<T>(x, own, oth);
 #pragma unroll
         for (int i = 0; i < L::V; ++i) y[i] = r * fmaf(own[i], turn.c[i], oth[i] * turn.s[i]);
     }
 };
 
-template <typename T, int D>
+template <typename T, int D, bool IL>
 __global__ __launch_bounds__(256) void k_norm_rope_fwd(RowArgs a) {
     using L = RowLayout<T, D>;
     const int lane = threadIdx.x & 63, e0 = (lane % L::LPR) * L::V, sub = lane / L::LPR;
@@ -120,13 +119,13 @@ __global__ __launch_bounds__(256) void k_norm_rope_fwd(RowArgs a) {
     const long stride = is_q ? a.q_stride : a.k_stride;
     const T *in = static_cast<const T *>(is_q ? a.q : a.k);
     T *out = static_cast<T *>(is_q ? a.q_out : a.k_out);
-    NormTurn<T, D> nt;
-    Weights<T, D> w;
+    NormTurn<T, D, IL> nt;
+    Weights<T, D, IL> w;
     w.load(a, is_q ? a.qw : a.kw, e0);
     for (int t = blockIdx.x * 4 + (threadIdx.x >> 6); t < a.T; t += gridDim.x * 4) {
         const T *row = in + t * stride;
         T *to = out + (long)t * H * D;
-        nt.load(a, w, e0, a.positions ? a.positions[t] : t % a.seq_len);
+        nt.load(a, w, e0, nt.turn.row_of(a, a.positions ? a.positions[t] : t % a.seq_len));
         for (int h0 = 0; h0 < H; h0 += kRowBatch * L::RPW) {
             uint4 x[kRowBatch];
 #pragma unroll
@@ -147,7 +146,7 @@ __global__ __launch_bounds__(256) void k_norm_rope_fwd(RowArgs a) {
 }
 
 // Rows' gradients; every workgroup also leaves its sum of dz * xhat, which k_weight_grad adds up in the workgroups' order.
-template <typename T, int D>
+template <typename T, int D, bool IL>
 __global__ __launch_bounds__(256) void k_norm_rope_bwd(RowArgs a) {
     using L = RowLayout<T, D>;
     __shared__ float part[4][D];
@@ -161,11 +160,11 @@ __global__ __launch_bounds__(256) void k_norm_rope_bwd(RowArgs a) {
     load_weight<T>(is_q ? a.qw : a.kw, e0, w);
 #pragma unroll
     for (int i = 0; i < L::V; ++i) dw[i] = 0.f;
-    Turn<L::V> turn;
+    Turn<L::V, IL> turn;
     for (int t = blockIdx.x * 4 + wave; t < a.T; t += gridDim.x * 4) {
         const T *row = in + t * stride, *dy = grad + (long)t * H * D;
         T *to = out + (long)t * H * D;
-        turn.load(a, e0, a.positions ? a.positions[t] : t % a.seq_len);
+        turn.load(a, e0, turn.row_of(a, a.positions ? a.positions[t] : t % a.seq_len));
         for (int h0 = 0; h0 < H; h0 += kRowBatch * L::RPW) {
             uint4 x[kRowBatch], g[kRowBatch];
 #pragma unroll
@@ -181,7 +180,7 @@ __global__ __launch_bounds__(256) void k_norm_rope_bwd(RowArgs a) {
                 float xf[L::V], own[L::V], oth[L::V], ss = 0.f, gx = 0.f;
                 unpack16<T>(x[b], xf);
                 unpack16<T>(g[b], own);
-                turn.template others<T>(a, g[b], own, oth);
+                turn.template others<T>(g[b], own, oth);
 #pragma unroll
                 for (int i = 0; i < L::V; ++i) {
                     ss = fmaf(xf[i], xf[i], ss);
@@ -245,98 +244,123 @@ __device__ inline bool slot_of(const PagedArgs &c, int n, int pos, int Hkv, bool
     return true;
 }
 
+// Where the wave's rows of one tensor go: a descriptor from the token's first head on that ends behind its last one (stores past it, of heads that
+// are not there, and all stores of a token without a place are dropped; offsets stand in the vector operand alone, where the range is checked), this
+// lane's offset, and the step between `RPW` heads.
+struct Rows { __amdgpu_buffer_rsrc_t rs; int off, step; };
+
+__device__ inline void store16(const Rows &to, int step, const uint4 &w) {
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    __builtin_amdgcn_raw_buffer_store_b128(u32x4{w.x, w.y, w.z, w.w}, to.rs, to.off + step * to.step, 0, 0);
+}
+
 // Quantises the row that `y` is part of (LPR lanes) and writes it to the cache.
 template <typename T, typename CT, int D>
-__device__ inline void cache_row(void *pages, float *scale, long row, int e0, const float (&y)[RowLayout<T, D>::V], bool live) {
+__device__ inline void cache_row(const Rows &to, const Rows &scale, int step, int e0, const float (&y)[RowLayout<T, D>::V]) {
     using L = RowLayout<T, D>;
     if constexpr (__is_same(CT, fp8)) {
         float amax = 0.f;
 #pragma unroll
         for (int i = 0; i < L::V; ++i) amax = fmaxf(amax, fabsf(y[i]));
         amax = lanes_max<L::LPR>(amax);
-        const bool none = amax < 0x1p-100f; // (its factor would leave the range of normal numbers)
-        const float s = none ? 0.f : __fdiv_rn(amax, 448.f), inv = none ? 0.f : __fdiv_rn(1.f, s);
+        // Quotients to the last bit (the product with the reciprocal, corrected once: rows of bf16 values meet ties often): amax / 448, then y / s.  A row
+        // under 2^-100, whose factor would leave the range of normal numbers, is held as zeros.
+        constexpr float c = 1.f / 448.f;
+        float s = amax * c;
+        s = amax < INFINITY ? fmaf(fmaf(-s, 448.f, amax), c, s) : amax;
+        float inv = __builtin_amdgcn_rcpf(s);
+        inv = fmaf(fmaf(-s, inv, 1.f), inv, inv);
+        const bool none = amax < 0x1p-100f;
+        s = none ? 0.f : s;
+        inv = none || s == INFINITY ? 0.f : inv;
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            // y / s to the last bit (the product with the rounded reciprocal, corrected once): rows of bf16 values meet ties often
             const float x = y[i] * inv;
             v[i] = fmaf(fmaf(-x, s, y[i]), inv, x);
         }
-        if (live) {
-            *reinterpret_cast<uint2 *>(static_cast<unsigned char *>(pages) + row * D + e0) = to_fp8x8(v);
-            if (e0 == 0) scale[row] = s;
-        }
-    } else if (live) *reinterpret_cast<uint4 *>(static_cast<T *>(pages) + row * D + e0) = pack16<T>(y);
+        const uint2 w = to_fp8x8(v);
+        typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2{w.x, w.y}, to.rs, to.off + step * to.step, 0, 0);
+        if (e0 == 0) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(s), scale.rs, scale.off + step * scale.step, 0, 0);
+    } else store16(to, step, pack16<T>(y));
 }
 
-// New tokens, a wave per token (and, where there are few, per tensor and block of heads): k, v and, with NORM, which also normalises and rotates k, q.
-// Finding the token's place takes three loads in a row (its sequence, the context's length, the page), about as long as the rows' way
-// here, so the first rows are requested before and all tensors of a token share one search.
-template <typename T, typename CT, int D, bool NORM>
-__global__ __launch_bounds__(256) void k_paged_append(RowArgs a, PagedArgs c) {
+// New tokens: a wave takes up to kAppendSteps steps (a step: as many heads as a wave holds) of one token's q, k and v (q only with NORM, which also
+// normalises and rotates k).  Finding the token's place takes three loads in a row (its sequence, the context's length, the page),
+// and that latency, not the bytes, would be the time: all rows are requested before the search, and what the norm needs waits in the LDS, because a load
+// issued behind the first stores would wait for those.
+constexpr int kAppendSteps = 2;
+template <typename T, typename CT, int D, bool NORM, bool IL>
+__global__ __launch_bounds__(256) void k_paged_append(RowArgs a, PagedArgs c, int per) {
     using L = RowLayout<T, D>;
-    constexpr int PER = kRowBatch * L::RPW; // heads of a batch
-    const int lane = threadIdx.x & 63, e0 = (lane % L::LPR) * L::V, sub = lane / L::LPR;
-    const int t = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (t >= a.T) return;
-    // batches: those of q, then k, then v
-    const int bq = NORM ? (a.Hq + PER - 1) / PER : 0, bkv = (a.Hkv + PER - 1) / PER, all = bq + 2 * bkv;
-    int i = blockIdx.y;
-    uint4 x[kRowBatch];
-    auto heads_of = [&](int i, int &what, int &h0) { // 0: q, 1: k, 2: v
-        what = i < bq ? 0 : i < bq + bkv ? 1 : 2;
-        h0 = (i - (what == 0 ? 0 : what == 1 ? bq : bq + bkv)) * PER;
-    };
-    auto fetch = [&](int i) __attribute__((always_inline)) {
-        int what, h0;
-        heads_of(i, what, h0);
-        const T *row = static_cast<const T *>(what == 0 ? a.q : what == 1 ? a.k : a.v) + t * (what == 0 ? a.q_stride : what == 1 ? a.k_stride : a.v_stride);
-        const int H = what == 0 ? a.Hq : a.Hkv;
+    constexpr int ES = (int)sizeof(T), CB = __is_same(CT, fp8) ? 1 : ES; // bytes of an element, and in the cache
+    __shared__ __align__(16) float turns[NORM ? 4 : 1][NORM ? D : 4];
+    __shared__ __align__(16) T weight[NORM ? 2 : 1][NORM ? D : 8];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), e0 = (lane % L::LPR) * L::V, sub = lane / L::LPR;
+    const int t = blockIdx.x * 4 + wave;
+    // steps: those of q, then k, then v
+    const int sq = NORM ? (a.Hq + L::RPW - 1) / L::RPW : 0, skv = (a.Hkv + L::RPW - 1) / L::RPW;
+    const int first = blockIdx.y * per, last = min(first + per, sq + 2 * skv);
+    uint4 x[kAppendSteps];
+    if (t < a.T) {
 #pragma unroll
-        for (int b = 0; b < kRowBatch; ++b) {
-            const int h = h0 + b * L::RPW + sub;
-            x[b] = h < H ? *reinterpret_cast<const uint4 *>(row + h * D + e0) : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < kAppendSteps; ++i) {
+            const int at = min(first + i, last - 1), what = at < sq ? 0 : at < sq + skv ? 1 : 2, step = at - (what == 0 ? 0 : what == 1 ? sq : sq + skv);
+            const T *row = static_cast<const T *>(what == 0 ? a.q : what == 1 ? a.k : a.v) + t * (what == 0 ? a.q_stride : what == 1 ? a.k_stride : a.v_stride);
+            const auto w = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(row, (what == 0 ? a.Hq : a.Hkv) * D * ES), ((sub + step * L::RPW) * D + e0) * ES, 0, 0);
+            x[i] = make_uint4(w[0], w[1], w[2], w[3]);
         }
-    };
-    fetch(i);
-    const int n = seq_of_row(c.cu, c.N, t);
-    int pos = -1;
+    }
+    int n = c.N, pos = -1;
     Slot s{0, 0};
     bool live = false;
+    if (t < a.T) n = seq_of_row(c.cu, c.N, t);
     if (n < c.N) {
         pos = min(c.kv_len[n], c.max_kv) - c.cu[n + 1] + t;
         live = slot_of(c, n, pos, a.Hkv, false, &s);
     }
-    NormTurn<T, D> nt;
-    for (int with = -1;;) {
-        int what, h0;
-        heads_of(i, what, h0);
-        if (NORM && what != 2 && what != with) {
-            Weights<T, D> w;
-            w.load(a, what == 0 ? a.qw : a.kw, e0);
-            nt.load(a, w, e0, pos);
-            with = what;
+    if constexpr (NORM) {
+        if (first < sq + skv) {
+            for (int i = threadIdx.x; i < 2 * D / L::V; i += 256) {
+                const void *w = i < D / L::V ? a.qw : a.kw;
+                float f[L::V];
+                load_weight<T>(w, i % (D / L::V) * L::V, f);
+                *reinterpret_cast<uint4 *>(&weight[i / (D / L::V)][i % (D / L::V) * L::V]) = pack16<T>(f);
+            }
+            if (a.rot && 4 * lane < a.rot)
+                *reinterpret_cast<float4 *>(&turns[wave][4 * lane]) = *reinterpret_cast<const float4 *>(Turn<L::V, IL>::row_of(a, pos) + 4 * lane);
+            __syncthreads();
         }
-        const int H = what == 0 ? a.Hq : a.Hkv, next = i + gridDim.y;
-        uint4 now[kRowBatch];
+    }
+    if (t >= a.T) return;
+    NormTurn<T, D, IL> nt;
+    int with = -1;
 #pragma unroll
-        for (int b = 0; b < kRowBatch; ++b) now[b] = x[b];
-        if (next < all) fetch(next);
-#pragma unroll
-        for (int b = 0; b < kRowBatch; ++b) {
-            if (h0 + b * L::RPW >= H) break;
-            const int h = h0 + b * L::RPW + sub;
+    for (int i = 0; i < kAppendSteps; ++i) {
+        const int at = first + i;
+        if (at < last) {
+            const int what = at < sq ? 0 : at < sq + skv ? 1 : 2, step = at - (what == 0 ? 0 : what == 1 ? sq : sq + skv);
             float y[L::V];
-            if (NORM && what != 2) nt.apply(a, now[b], y);
-            else unpack16<T>(now[b], y);
+            if (NORM && what != 2) {
+                if (what != with) {
+                    Weights<T, D, IL> w;
+                    w.load(a, weight[what], e0);
+                    nt.load(a, w, e0, turns[wave]);
+                    with = what;
+                }
+                nt.apply(a, x[i], y);
+            } else unpack16<T>(x[i], y);
             if (what == 0) {
-                if (h < H) *reinterpret_cast<uint4 *>(static_cast<T *>(a.q_out) + ((long)t * H + h) * D + e0) = pack16<T>(y);
-            } else
-                cache_row<T, CT, D>(what == 1 ? c.kp : c.vp, what == 1 ? c.ks : c.vs, s.base + (long)h * s.stride, e0, y, live && h < H);
+                const Rows to{make_rsrc(static_cast<T *>(a.q_out) + (long)t * a.Hq * D, a.Hq * D * ES), (sub * D + e0) * ES, L::RPW * D * ES};
+                store16(to, step, pack16<T>(y));
+            } else { // head h of the token is row s.base + h s.stride
+                const int rows = live ? (a.Hkv - 1) * s.stride + 1 : 0;
+                const Rows to{make_rsrc(static_cast<char *>(what == 1 ? c.kp : c.vp) + s.base * (D * CB), rows * (D * CB)), (sub * s.stride * D + e0) * CB, L::RPW * s.stride * D * CB};
+                const Rows scale{make_rsrc((what == 1 ? c.ks : c.vs) + s.base, rows * 4), sub * s.stride * 4, L::RPW * s.stride * 4};
+                cache_row<T, CT, D>(to, scale, step, e0, y);
+            }
         }
-        if (next >= all) return;
-        i = next;
     }
 }
 
@@ -420,7 +444,7 @@ struct FwdLaunch {
     hipStream_t stream;
     template <typename T, int D> int operator()() {
         void *args[] = {&a};
-        return launch("k_norm_rope_fwd", reinterpret_cast<const void *>(k_norm_rope_fwd<T, D>), dim3(token_blocks(a.T), 2), args, stream);
+        return launch("k_norm_rope_fwd", a.interleaved ? reinterpret_cast<const void *>(k_norm_rope_fwd<T, D, true>) : reinterpret_cast<const void *>(k_norm_rope_fwd<T, D, false>), dim3(token_blocks(a.T), 2), args, stream);
     }
 };
 struct BwdLaunch {
@@ -430,31 +454,37 @@ struct BwdLaunch {
         int blocks = norm_rope_bwd_blocks(a.T), d = D;
         if (a.T > 0) {
             void *args[] = {&a};
-            if (const int e = launch("k_norm_rope_bwd", reinterpret_cast<const void *>(k_norm_rope_bwd<T, D>), dim3(blocks, 2), args, stream)) return e;
+            if (const int e = launch("k_norm_rope_bwd", a.interleaved ? reinterpret_cast<const void *>(k_norm_rope_bwd<T, D, true>) : reinterpret_cast<const void *>(k_norm_rope_bwd<T, D, false>), dim3(blocks, 2), args, stream)) return e;
         }
         if (!a.dqw && !a.dkw) return 0;
         void *args[] = {&a, &d, &blocks};
         return launch("k_weight_grad", reinterpret_cast<const void *>(k_weight_grad), dim3(D / 16, 2), args, stream, 1024);
     }
 };
-// The batches of a token are spread over waves where there are few tokens.
-template <typename T, int D> int batch_blocks(int tokens, int Hq, int Hkv) {
-    const int per = kRowBatch * RowLayout<T, D>::RPW, all = (Hq + per - 1) / per + 2 * ((Hkv + per - 1) / per);
-    return tokens >= 2048 ? 1 : all;
+// Steps of k_paged_append per wave: all of a token's, in equal parts of at most kAppendSteps; one where there are few tokens.
+template <typename T, int D> int steps_per_wave(int tokens, int Hq, int Hkv, int *waves) {
+    constexpr int RPW = RowLayout<T, D>::RPW;
+    const int all = (Hq + RPW - 1) / RPW + 2 * ((Hkv + RPW - 1) / RPW);
+    const int parts = tokens < 512 ? all : (all + kAppendSteps - 1) / kAppendSteps, per = (all + parts - 1) / parts;
+    *waves = (all + per - 1) / per;
+    return per;
 }
 struct AppendLaunch {
     RowArgs a;
     PagedArgs c;
     bool fp8_pages, norm;
     hipStream_t stream;
+    template <typename T, int D, typename CT> const void *of() const {
+        if (!norm) return reinterpret_cast<const void *>(k_paged_append<T, CT, D, false, false>);
+        return a.interleaved ? reinterpret_cast<const void *>(k_paged_append<T, CT, D, true, true>) : reinterpret_cast<const void *>(k_paged_append<T, CT, D, true, false>);
+    }
     template <typename T, int D> int operator()() {
-        void *args[] = {&a, &c};
-        const void *fn;
-        if constexpr (sizeof(T) == 2) {
-            if (fp8_pages) fn = norm ? reinterpret_cast<const void *>(k_paged_append<T, fp8, D, true>) : reinterpret_cast<const void *>(k_paged_append<T, fp8, D, false>);
-            else fn = norm ? reinterpret_cast<const void *>(k_paged_append<T, T, D, true>) : reinterpret_cast<const void *>(k_paged_append<T, T, D, false>);
-        } else fn = norm ? reinterpret_cast<const void *>(k_paged_append<T, T, D, true>) : reinterpret_cast<const void *>(k_paged_append<T, T, D, false>);
-        return launch("k_paged_append", fn, dim3((a.T + 3) / 4, batch_blocks<T, D>(a.T, norm ? a.Hq : 0, a.Hkv)), args, stream);
+        int waves, per = steps_per_wave<T, D>(a.T, norm ? a.Hq : 0, a.Hkv, &waves);
+        void *args[] = {&a, &c, &per};
+        const void *fn = of<T, D, T>();
+        if constexpr (sizeof(T) == 2)
+            if (fp8_pages) fn = of<T, D, fp8>();
+        return launch("k_paged_append", fn, dim3((a.T + 3) / 4, waves), args, stream);
     }
 };
 struct ReadLaunch {

@@ -335,6 +335,19 @@ constexpr int kWideRows = 128, kWideWaves = 4;
 // keys of a tile (at d = 256 twice as many would need more registers than there are)
 constexpr int wide_keys(int d) { return d > 128 ? 32 : 64; }
 
+// 64 lanes' 16 bytes from global memory to a kilobyte of the LDS, without registers in between: lane l's land 16 l behind `lds` (M0 holds it); lanes past
+// the descriptor's range leave zeros.  The compiler does not know of the transfer (told of it, it would have every read of the LDS wait for it): wait_moved
+// before the barrier that makes the tile readable.  Nor does it keep the hardware's distances inside the text: M0 needs one wait state, a scalar
+// register written on the vector unit (readfirstlane) five before a buffer access reads it.  tests/test_attention_dma_host.py reads both from the compiled code.
+__device__ __forceinline__ void move16(__amdgpu_buffer_rsrc_t rs, int off, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rs) : "memory");
+}
+__device__ inline unsigned lds_place(const unsigned char *p) {
+    typedef __attribute__((address_space(3))) const unsigned char lds_t;
+    return __builtin_amdgcn_readfirstlane((unsigned)(size_t)(lds_t *)p);
+}
+__device__ __forceinline__ void wait_moved() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 template <typename CT, int D> struct WideTile {
     static constexpr bool FP8 = __is_same(CT, fp8);
     static constexpr int KEYS = wide_keys(D);
@@ -426,7 +439,7 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(
         for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
     float m = kNoScore, l = 0.f;
 
-    // this thread's pieces of a tile on their way
+    // this thread's pieces of a tile on their way (8-bit pages; 16-bit ones go straight to the LDS)
     u32x4 rk[W::NL], rv[W::NL];
     float rs = 0.f;
     const char *kp = static_cast<const char *>(a.c.kp), *vp = static_cast<const char *>(a.c.vp);
@@ -437,14 +450,23 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(
         for (int i = 0; i < W::NL; ++i) page[i] = page_entry(a.c, n, k0 + ((i * 256 + wave * 64) / W::LPR & ~15));
         if constexpr (FP8) spage = page_entry(a.c, n, k0 + (lane & 48));
     };
-    auto fetch = [&](int k0) __attribute__((always_inline)) {
+    auto fetch = [&](unsigned char *buf, int k0) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < W::NL; ++i) {
             const int r0 = (i * 256 + wave * 64) / W::LPR, kk = k0 + (r0 & ~15); // the wave's rows lie in one group of 16 keys
             const long at = row_of(a.c, __builtin_amdgcn_readfirstlane(page_id(a.c, page[i])), kk, kvh, Hkv) * (D * EB);
-            const unsigned off = ((r0 & 15) + lane / W::LPR) * (D * EB) + piece * 16;
-            rk[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(kp + at), off, 0, 0);
-            rv[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(vp + at), off, 0, 0);
+            const int r = r0 + lane / W::LPR;
+            if constexpr (FP8) {
+                const int off = (r & 15) * (D * EB) + piece * 16;
+                rk[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(kp + at), off, 0, 0);
+                rv[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(vp + at), off, 0, 0);
+            } else {
+                // nothing past the last key that a row sees is read into a result, whatever stands there: such values arrive as zeros
+                const int off = (r & 15) * (D * EB) + ((piece ^ W::swizzle(r)) << 4);
+                const unsigned to = lds_place(buf) + (i * 256 + wave * 64) * 16;
+                move16(make_rsrc(kp + at), off, to);
+                move16(make_rsrc(vp + at), k0 + r < hi ? off : kBufRange, to + W::oV);
+            }
         }
         if constexpr (FP8)
             if (wave < 2 && lane < KEYS) rs = (wave ? a.c.vs : a.c.ks)[row_of(a.c, page_id(a.c, spage), k0 + (lane & 48), kvh, Hkv) + (lane & 15)];
@@ -457,21 +479,14 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(
             const int r = (i * 256 + t) / W::LPR;
             u32x4 v = rv[i];
             if (tail && k0 + r >= hi) v = u32x4{0, 0, 0, 0};
-            if constexpr (FP8) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    unsigned char *at = buf + r * W::ROWB + (((2 * piece + u) ^ W::swizzle(r)) << 4);
-                    *reinterpret_cast<u32x4 *>(at) = widen(rk[i][2 * u], rk[i][2 * u + 1]);
-                    *reinterpret_cast<u32x4 *>(at + W::oV) = widen(v[2 * u], v[2 * u + 1]);
-                }
-            } else {
-                unsigned char *at = buf + r * W::ROWB + ((piece ^ W::swizzle(r)) << 4);
-                *reinterpret_cast<u32x4 *>(at) = rk[i];
-                *reinterpret_cast<u32x4 *>(at + W::oV) = v;
+            for (int u = 0; u < 2; ++u) {
+                unsigned char *at = buf + r * W::ROWB + (((2 * piece + u) ^ W::swizzle(r)) << 4);
+                *reinterpret_cast<u32x4 *>(at) = widen(rk[i][2 * u], rk[i][2 * u + 1]);
+                *reinterpret_cast<u32x4 *>(at + W::oV) = widen(v[2 * u], v[2 * u + 1]);
             }
         }
-        if constexpr (FP8)
-            if (wave < 2 && lane < KEYS) reinterpret_cast<float *>(buf + (wave ? W::oVS : W::oKS))[lane] = tail && k0 + lane >= hi ? 0.f : rs;
+        if (wave < 2 && lane < KEYS) reinterpret_cast<float *>(buf + (wave ? W::oVS : W::oKS))[lane] = tail && k0 + lane >= hi ? 0.f : rs;
     };
     auto work = [&](const unsigned char *buf, int k0) __attribute__((always_inline)) {
         f32x16 st[NX];
@@ -558,18 +573,29 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(
         }
     };
 
+    // One barrier per tile: the other buffer was last read before the barrier in front of this tile.
+    auto seen = [&](int k0) { return k0 <= some_to && k0 + KEYS > some_from; };
     if (k_begin < k_end) {
         look_up(k_begin);
-        fetch(k_begin);
-        park(wsmem, k_begin);
-        if (k_begin + KEYS < k_end) fetch(k_begin + KEYS);
-        lds_barrier();
-        for (int k0 = k_begin, j = 0; k0 < k_end; k0 += KEYS, j ^= 1) {
-            // (the other buffer was last read before the barrier that ended the last tile)
-            if (k0 + KEYS < k_end) park(wsmem + (j ^ 1) * W::SIZE, k0 + KEYS);
-            if (k0 + 2 * KEYS < k_end) fetch(k0 + 2 * KEYS);
-            if (k0 <= some_to && k0 + KEYS > some_from) work(wsmem + j * W::SIZE, k0);
+        if constexpr (FP8) {
+            fetch(wsmem, k_begin);
+            park(wsmem, k_begin);
+            if (k_begin + KEYS < k_end) fetch(wsmem, k_begin + KEYS);
             lds_barrier();
+            for (int k0 = k_begin, j = 0; k0 < k_end; k0 += KEYS, j ^= 1) {
+                if (k0 + KEYS < k_end) park(wsmem + (j ^ 1) * W::SIZE, k0 + KEYS);
+                if (k0 + 2 * KEYS < k_end) fetch(wsmem, k0 + 2 * KEYS);
+                if (seen(k0)) work(wsmem + j * W::SIZE, k0);
+                lds_barrier();
+            }
+        } else {
+            fetch(wsmem, k_begin);
+            for (int k0 = k_begin, j = 0; k0 < k_end; k0 += KEYS, j ^= 1) {
+                wait_moved();
+                lds_barrier();
+                if (k0 + KEYS < k_end) fetch(wsmem + (j ^ 1) * W::SIZE, k0 + KEYS);
+                if (seen(k0)) work(wsmem + j * W::SIZE, k0);
+            }
         }
     }
     {
