@@ -490,22 +490,31 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(
     };
     auto work = [&](const unsigned char *buf, int k0) __attribute__((always_inline)) {
         f32x16 st[NX];
-#pragma unroll
-        for (int x = 0; x < NX; ++x) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) st[x][r] = 0.f;
-            const unsigned char *kr = buf + (32 * x + col) * W::ROWB;
-            const int sw = W::swizzle(col);
+        {
+            // all operands are requested before the first product: one LDS latency instead of one per product (the compiler's own order)
+            bf16x8 kf[NX][D / 16];
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
-                st[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(kr + (((2 * i + h) ^ sw) << 4)), q[i], st[x], 0, 0, 0);
-            if constexpr (FP8)
+#pragma unroll
+                for (int x = 0; x < NX; ++x) kf[x][i] = *reinterpret_cast<const bf16x8 *>(buf + (32 * x + col) * W::ROWB + (((2 * i + h) ^ W::swizzle(col)) << 4));
+#pragma unroll
+            for (int x = 0; x < NX; ++x)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) st[x][r] = 0.f;
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int x = 0; x < NX; ++x) st[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x][i], q[i], st[x], 0, 0, 0);
+        }
+        if constexpr (FP8)
+#pragma unroll
+            for (int x = 0; x < NX; ++x)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const float4 f = *reinterpret_cast<const float4 *>(buf + W::oKS + (32 * x + 8 * g + 4 * h) * 4);
                     st[x][4 * g] *= f.x; st[x][4 * g + 1] *= f.y; st[x][4 * g + 2] *= f.z; st[x][4 * g + 3] *= f.w;
                 }
-        }
         if (k0 < all_from || k0 + KEYS - 1 > all_to) {
 #pragma unroll
             for (int x = 0; x < NX; ++x)
