@@ -101,16 +101,15 @@ __device__ inline unsigned bf16_pair(unsigned w, bool hi) {
 __device__ inline u32x4 widen(unsigned lo, unsigned hi) { return u32x4{bf16_pair(lo, false), bf16_pair(lo, true), bf16_pair(hi, false), bf16_pair(hi, true)}; }
 
 template <typename T, typename CT, int D>
-__global__ __launch_bounds__(64 * kFewWaves) void k_attn_few(AttnArgs a, int tiles, Cut cut, int max_rows) {
+__device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut, int max_rows, int block, float *smem) {
     const int splits = cut.splits, split_keys = cut.keys;
     constexpr int EB = PageElem<T, CT>::bytes;
     constexpr int KE = D / 4, VE = D / 16;              // elements of a key, of a value, that a lane holds
     constexpr int KW = KE * EB / 4, VW = VE * EB / 4;   // in words
     constexpr bool FP8 = __is_same(CT, fp8);
-    extern __shared__ __align__(16) float smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int Hkv = a.r.Hkv, G = a.r.Hq / Hkv;
-    int b = blockIdx.x;
+    int b = block;
     const int kvh = b % Hkv; b /= Hkv;
     const int split = b % splits; b /= splits;
     const int tile = b % tiles, n = b / tiles;
@@ -394,19 +393,18 @@ __device__ inline bool tile_of_slot(const AttnArgs &a, int G, int few, int slot,
 }
 
 template <typename CT, int D>
-__global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(AttnArgs a, Cut cut, int few, int zero) {
+__device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few, bool zero, int block, unsigned char *wsmem) {
     const int splits = cut.splits, split_keys = cut.keys;
     using W = WideTile<CT, D>;
     constexpr bool FP8 = W::FP8;
     constexpr int EB = FP8 ? 1 : 2, NB = D / 32, KEYS = W::KEYS, NX = KEYS / 32;
-    extern __shared__ __align__(16) unsigned char wsmem[];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 31, h = lane >> 5;
     const int Hkv = a.r.Hkv, G = a.r.Hq / Hkv;
-    int b = blockIdx.x;
+    int b = block;
     const int kvh = b % Hkv; b /= Hkv;
     const int split = b % splits, slot = b / splits;
     int n, tile;
-    if (zero && split == 0 && (slot + 1) * splits * Hkv == gridDim.x) zero_rest<bf16, D>(a, kvh, G);
+    if (zero && block < Hkv) zero_rest<bf16, D>(a, kvh, G);
     if (!tile_of_slot(a, G, few, slot, &n, &tile)) return;
     n = __builtin_amdgcn_readfirstlane(n);
     tile = __builtin_amdgcn_readfirstlane(tile);
@@ -445,31 +443,35 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(
     const char *kp = static_cast<const char *>(a.c.kp), *vp = static_cast<const char *>(a.c.vp);
     const int piece = t % W::LPR;
     int page[W::NL], spage = 0; // of the next tile to fetch, looked up a tile ahead
+    const unsigned page_bytes = (unsigned)(Hkv << a.c.page_shift) * (D * EB);
     auto look_up = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < W::NL; ++i) page[i] = page_entry(a.c, n, k0 + ((i * 256 + wave * 64) / W::LPR & ~15));
         if constexpr (FP8) spage = page_entry(a.c, n, k0 + (lane & 48));
     };
-    auto fetch = [&](unsigned char *buf, int k0) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < W::NL; ++i) {
-            const int r0 = (i * 256 + wave * 64) / W::LPR, kk = k0 + (r0 & ~15); // the wave's rows lie in one group of 16 keys
-            const long at = row_of(a.c, __builtin_amdgcn_readfirstlane(page_id(a.c, page[i])), kk, kvh, Hkv) * (D * EB);
-            const int r = r0 + lane / W::LPR;
-            if constexpr (FP8) {
-                const int off = (r & 15) * (D * EB) + piece * 16;
-                rk[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(kp + at), off, 0, 0);
-                rv[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(vp + at), off, 0, 0);
-            } else {
-                // nothing past the last key that a row sees is read into a result, whatever stands there: such values arrive as zeros
-                const int off = (r & 15) * (D * EB) + ((piece ^ W::swizzle(r)) << 4);
-                const unsigned to = lds_place(buf) + (i * 256 + wave * 64) * 16;
-                move16(make_rsrc(kp + at), off, to);
-                move16(make_rsrc(vp + at), k0 + r < hi ? off : kBufRange, to + W::oV);
-            }
+    // load i of a tile's NL (of K and of V)
+    auto fetch = [&](unsigned char *buf, int k0, int i) __attribute__((always_inline)) {
+        const int r0 = (i * 256 + wave * 64) / W::LPR, kk = k0 + (r0 & ~15); // the wave's rows lie in one group of 16 keys
+        const unsigned id = __builtin_amdgcn_readfirstlane(page_id(a.c, page[i]));
+        const long at = (long)((unsigned long)id * page_bytes) + ((kvh << a.c.page_shift) + (kk & ((1 << a.c.page_shift) - 1))) * (D * EB);
+        const int r = r0 + lane / W::LPR;
+        if constexpr (FP8) {
+            const int off = (r & 15) * (D * EB) + piece * 16;
+            rk[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(kp + at), off, 0, 0);
+            rv[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(vp + at), off, 0, 0);
+            if (i == 0 && wave < 2 && lane < KEYS)
+                rs = (wave ? a.c.vs : a.c.ks)[row_of(a.c, page_id(a.c, spage), k0 + (lane & 48), kvh, Hkv) + (lane & 15)];
+        } else {
+            // nothing past the last key that a row sees is read into a result, whatever stands there: such values arrive as zeros
+            const int off = (r & 15) * (D * EB) + ((piece ^ W::swizzle(r)) << 4);
+            const unsigned to = lds_place(buf) + (i * 256 + wave * 64) * 16;
+            move16(make_rsrc(kp + at), off, to);
+            move16(make_rsrc(vp + at), k0 + r < hi ? off : kBufRange, to + W::oV);
         }
-        if constexpr (FP8)
-            if (wave < 2 && lane < KEYS) rs = (wave ? a.c.vs : a.c.ks)[row_of(a.c, page_id(a.c, spage), k0 + (lane & 48), kvh, Hkv) + (lane & 15)];
+    };
+    auto fetch_all = [&](unsigned char *buf, int k0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < W::NL; ++i) fetch(buf, k0, i);
         look_up(k0 + KEYS);
     };
     auto park = [&](unsigned char *buf, int k0) __attribute__((always_inline)) {
@@ -488,7 +490,8 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(
         }
         if (wave < 2 && lane < KEYS) reinterpret_cast<float *>(buf + (wave ? W::oVS : W::oKS))[lane] = tail && k0 + lane >= hi ? 0.f : rs;
     };
-    auto work = [&](const unsigned char *buf, int k0) __attribute__((always_inline)) {
+    // a tile's work, and between its first products the requests for tile `next` (16 bits: into `to`), if `more`
+    auto work = [&](const unsigned char *buf, int k0, unsigned char *to, int next, bool more) __attribute__((always_inline)) {
         f32x16 st[NX];
         {
             // all operands are requested before the first product: one LDS latency instead of one per product (the compiler's own order)
@@ -497,15 +500,20 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
                 for (int x = 0; x < NX; ++x) kf[x][i] = *reinterpret_cast<const bf16x8 *>(buf + (32 * x + col) * W::ROWB + (((2 * i + h) ^ W::swizzle(col)) << 4));
-#pragma unroll
-            for (int x = 0; x < NX; ++x)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) st[x][r] = 0.f;
+            __builtin_amdgcn_s_setprio(1); // (over the other workgroup's softmax: prompts of 4 x 2048 tokens 97 -> 93 us)
             __builtin_amdgcn_sched_barrier(0);
+            constexpr int EVERY = D / 16 / W::NL;
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i)
+            for (int i = 0; i < D / 16; ++i) {
 #pragma unroll
-                for (int x = 0; x < NX; ++x) st[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x][i], q[i], st[x], 0, 0, 0);
+                for (int x = 0; x < NX; ++x) st[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x][i], q[i], i ? st[x] : f32x16{}, 0, 0, 0);
+                if (i % EVERY == EVERY - 1) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (more) fetch(to, next, i / EVERY);
+                }
+            }
+            if (more) look_up(next + KEYS);
+            __builtin_amdgcn_s_setprio(0);
         }
         if constexpr (FP8)
 #pragma unroll
@@ -587,23 +595,25 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(
     if (k_begin < k_end) {
         look_up(k_begin);
         if constexpr (FP8) {
-            fetch(wsmem, k_begin);
+            fetch_all(wsmem, k_begin);
             park(wsmem, k_begin);
-            if (k_begin + KEYS < k_end) fetch(wsmem, k_begin + KEYS);
+            if (k_begin + KEYS < k_end) fetch_all(wsmem, k_begin + KEYS);
             lds_barrier();
             for (int k0 = k_begin, j = 0; k0 < k_end; k0 += KEYS, j ^= 1) {
                 if (k0 + KEYS < k_end) park(wsmem + (j ^ 1) * W::SIZE, k0 + KEYS);
-                if (k0 + 2 * KEYS < k_end) fetch(wsmem, k0 + 2 * KEYS);
-                if (seen(k0)) work(wsmem + j * W::SIZE, k0);
+                const bool more = k0 + 2 * KEYS < k_end;
+                if (seen(k0)) work(wsmem + j * W::SIZE, k0, wsmem, k0 + 2 * KEYS, more);
+                else if (more) fetch_all(wsmem, k0 + 2 * KEYS);
                 lds_barrier();
             }
         } else {
-            fetch(wsmem, k_begin);
+            fetch_all(wsmem, k_begin);
             for (int k0 = k_begin, j = 0; k0 < k_end; k0 += KEYS, j ^= 1) {
                 wait_moved();
                 lds_barrier();
-                if (k0 + KEYS < k_end) fetch(wsmem + (j ^ 1) * W::SIZE, k0 + KEYS);
-                if (seen(k0)) work(wsmem + j * W::SIZE, k0);
+                const bool more = k0 + KEYS < k_end;
+                if (seen(k0)) work(wsmem + j * W::SIZE, k0, wsmem + (j ^ 1) * W::SIZE, k0 + KEYS, more);
+                else if (more) fetch_all(wsmem + (j ^ 1) * W::SIZE, k0 + KEYS);
             }
         }
     }
@@ -635,20 +645,39 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(
     }
 }
 
-// Joins the splits of a row (token and head).  FEW: of the sequences that k_attn_few takes, a workgroup per row, since there are few rows and up to
-// kMostSplits splits (1 x 16 heads, 64 splits of 128: a wave per row took 17 us, one load after the other); else a wave per row of the others.
-template <typename T, int D, bool FEW>
+template <typename T, typename CT, int D>
+__global__ __launch_bounds__(64 * kFewWaves) void k_attn_few(AttnArgs a, int tiles, Cut cut, int max_rows) {
+    extern __shared__ __align__(16) unsigned char lds[];
+    attend_few<T, CT, D>(a, tiles, cut, max_rows, blockIdx.x, reinterpret_cast<float *>(lds));
+}
+template <typename CT, int D>
+__global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(AttnArgs a, Cut cut, int few_rows) {
+    extern __shared__ __align__(16) unsigned char lds[];
+    attend_wide<CT, D>(a, cut, few_rows, true, blockIdx.x, lds);
+}
+// Chunks beside single tokens: both kinds of workgroup in one launch, the long ones first, so that the short ones, which wait for memory, run under them.
+template <typename CT, int D>
+__global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_both(AttnArgs a, int tiles, Cut few, Cut wide, int few_rows, int wide_blocks) {
+    extern __shared__ __align__(16) unsigned char lds[];
+    if ((int)blockIdx.x < wide_blocks) attend_wide<CT, D>(a, wide, few_rows, false, blockIdx.x, lds);
+    else attend_few<bf16, CT, D>(a, tiles, few, few_rows, blockIdx.x - wide_blocks, reinterpret_cast<float *>(lds));
+}
+
+// Joins the splits of a row (token and head).  FEW: of the sequences that attend_few takes, else of the others.  WHOLE: a workgroup per row, for few rows with
+// many splits (16 rows of 128, 64 splits: a wave per row took 17 us, one load after the other); else a wave per row.
+template <typename T, int D, bool FEW, bool WHOLE>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, Cut cut, int few_rows, int per_seq) {
-    constexpr int LPR = D / 4, TPR = FEW ? 256 : 64, SIDE = TPR / LPR; // lanes of a row, threads of a row, splits side by side
-    __shared__ float part[FEW ? 4 : 1][D + 4];
+    constexpr int LPR = D / 4, TPR = WHOLE ? 256 : 64, SIDE = TPR / LPR; // lanes of a row, threads of a row, splits side by side
+    __shared__ float part[WHOLE ? 4 : 1][D + 4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int G = a.r.Hq / a.r.Hkv;
     int n, kvh, r;
     SeqRows s;
     if (FEW) {
-        int b = blockIdx.x;
-        r = b % per_seq; b /= per_seq;
-        kvh = b % a.r.Hkv; n = b / a.r.Hkv;
+        long b = WHOLE ? (long)blockIdx.x : (long)blockIdx.x * 4 + wave;
+        r = (int)(b % per_seq); b /= per_seq;
+        kvh = (int)(b % a.r.Hkv); n = (int)(b / a.r.Hkv);
+        if (n >= a.c.N) return;
         s.load(a, n);
         const int R = (s.r1 - s.r0) * G;
         if (r >= R || R > few_rows) return;
@@ -667,7 +696,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, Cut cut, int few_
     key_range(a, s, G, r / ROWS * ROWS, min(r / ROWS * ROWS + ROWS, (s.r1 - s.r0) * G), FEW ? kFewKeys : wide_keys(D), lo, hi);
     const int live = hi > lo ? min((hi - lo + cut.keys - 1) / cut.keys, cut.splits) : 0;
     const long row = (long)(s.r0 + r / G) * a.r.Hq + kvh * G + r % G;
-    const int in = FEW ? threadIdx.x : lane, e0 = in % LPR * 4, side = in / LPR;
+    const int in = WHOLE ? threadIdx.x : lane, e0 = in % LPR * 4, side = in / LPR;
     float *ml, *po;
     float M = kNoScore;
     for (int i = lane; i < live; i += 64) {
@@ -690,7 +719,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, Cut cut, int few_
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], m);
     }
-    if (FEW) {
+    if (WHOLE) {
         if (lane < LPR) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) part[wave][e0 + j] = acc[j];
@@ -713,8 +742,7 @@ namespace {
 constexpr int kFewMost = 32;
 constexpr int kMostSplits = 128;
 
-// per_seq: most rows of a sequence and key/value head that k_attn_few has (0: it is not launched); slots: row tiles of k_attn_wide, one more if it
-// zeroes the rows that lie in no sequence
+// per_seq: most rows of a sequence and key/value head that attend_few has; tiles: its tiles of them (0: there is none); slots: row tiles of attend_wide
 struct Plan { int few_rows, per_seq, tiles, slots; Cut few, wide; };
 
 // `range` keys at most, in `blocks` workgroups without a cut: as many splits as make up to `want` workgroups, each of `least` keys or more.
@@ -744,14 +772,15 @@ Plan plan_attn(int dtype, int d, const AttnArgs &a) {
     p.slots = 0;
     if (most > p.few_rows) { // sum of ceil(R / 128) over the sequences
         const long by_rows = rows / kWideRows + N, by_most = N * ((most + kWideRows - 1) / kWideRows);
-        p.slots = (int)(by_rows < by_most ? by_rows : by_most) + (equal ? 1 : 0);
+        p.slots = (int)(by_rows < by_most ? by_rows : by_most);
     }
     if (p.tiles < 1 && !p.slots) p.tiles = 1; // (it also zeroes the rows that lie in no sequence)
     auto range = [&](int step) {
         const long seen = a.window > 0 ? (long)a.window + a.max_q + step : a.c.max_kv;
         return seen < a.c.max_kv ? seen : (long)a.c.max_kv;
     };
-    p.few = p.tiles ? cut_keys(range(kFewKeys), (N > 0 ? N : 1) * p.tiles * a.r.Hkv, 1024, 256, kFewWaves * kFewKeys) : Cut{1, 128};
+    // (where there are chunks, too, most of the others are single tokens: one tile)
+    p.few = p.tiles ? cut_keys(range(kFewKeys), (N > 0 ? N : 1) * (p.slots ? 1 : p.tiles) * a.r.Hkv, 1024, 256, kFewWaves * kFewKeys) : Cut{1, 128};
     const long full = rows / kWideRows;
     p.wide = p.slots ? cut_keys(range(wide_keys(d)), (full > 0 ? full : 1) * a.r.Hkv, d > 128 ? 256 : d > 64 ? 512 : 768, 512, wide_keys(d)) : Cut{1, 64};
     return p;
@@ -778,23 +807,36 @@ int launch(const char *name, const void *fn, long blocks, int threads, int lds, 
 template <typename T, typename CT, int D> int launch_attn(int dtype, AttnArgs a, hipStream_t stream) {
     Plan p = plan_attn(dtype, D, a);
     a.splits = most_splits(p);
+    constexpr int few_lds = kFewWaves * kFewTile * (D + 4 + 2) * 4;
+    const long few_blocks = p.tiles ? ((long)a.c.N * p.tiles + 1) * p.few.splits * a.r.Hkv : 0;
+    int e = 0;
+    if (p.slots == 0) {
+        void *args[] = {&a, &p.tiles, &p.few, &p.few_rows};
+        e = launch("k_attn_few", reinterpret_cast<const void *>(k_attn_few<T, CT, D>), few_blocks, 64 * kFewWaves, few_lds, args, stream);
+    }
     if constexpr (sizeof(T) == 2)
         if (p.slots) {
-            int zero = p.tiles == 0;
-            void *args[] = {&a, &p.wide, &p.few_rows, &zero};
-            if (const int e = launch("k_attn_wide", reinterpret_cast<const void *>(k_attn_wide<CT, D>), (long)p.slots * p.wide.splits * a.r.Hkv, 64 * kWideWaves,
-                                     2 * WideTile<CT, D>::SIZE, args, stream)) return e;
+            const long wide_blocks = (long)p.slots * p.wide.splits * a.r.Hkv;
+            if (wide_blocks >= (1l << 31)) return (int)hipErrorInvalidConfiguration;
+            constexpr int wide_lds = 2 * WideTile<CT, D>::SIZE;
+            int first = (int)wide_blocks;
+            if (p.tiles) {
+                void *args[] = {&a, &p.tiles, &p.few, &p.wide, &p.few_rows, &first};
+                e = launch("k_attn_both", reinterpret_cast<const void *>(k_attn_both<CT, D>), wide_blocks + few_blocks, 64 * kWideWaves, wide_lds > few_lds ? wide_lds : few_lds, args, stream);
+            } else {
+                void *args[] = {&a, &p.wide, &p.few_rows};
+                e = launch("k_attn_wide", reinterpret_cast<const void *>(k_attn_wide<CT, D>), wide_blocks, 64 * kWideWaves, wide_lds, args, stream);
+            }
             void *join[] = {&a, &p.wide, &p.few_rows, &p.per_seq};
-            if (p.wide.splits > 1)
-                if (const int e = launch("k_attn_join", reinterpret_cast<const void *>(k_attn_join<T, D, false>), ((long)a.r.T * a.r.Hq + 3) / 4, 256, 0, join, stream)) return e;
+            if (!e && p.wide.splits > 1)
+                e = launch("k_attn_join", reinterpret_cast<const void *>(k_attn_join<T, D, false, false>), ((long)a.r.T * a.r.Hq + 3) / 4, 256, 0, join, stream);
         }
-    if (p.tiles == 0) return 0;
-    void *args[] = {&a, &p.tiles, &p.few, &p.few_rows};
-    if (const int e = launch("k_attn_few", reinterpret_cast<const void *>(k_attn_few<T, CT, D>), ((long)a.c.N * p.tiles + 1) * p.few.splits * a.r.Hkv,
-                             64 * kFewWaves, kFewWaves * kFewTile * (D + 4 + 2) * 4, args, stream)) return e;
-    if (p.few.splits == 1) return 0;
+    if (e || !p.tiles || p.few.splits == 1) return e;
+    const long rows = (long)a.c.N * a.r.Hkv * p.per_seq;
+    const bool whole = rows <= 2048;
     void *join[] = {&a, &p.few, &p.few_rows, &p.per_seq};
-    return launch("k_attn_join", reinterpret_cast<const void *>(k_attn_join<T, D, true>), (long)a.c.N * a.r.Hkv * p.per_seq, 256, 0, join, stream);
+    return launch("k_attn_join", whole ? reinterpret_cast<const void *>(k_attn_join<T, D, true, true>) : reinterpret_cast<const void *>(k_attn_join<T, D, true, false>),
+                  whole ? rows : (rows + 3) / 4, 256, 0, join, stream);
 }
 
 } // namespace

@@ -13,8 +13,8 @@ from tests.test_dma_hazards_host import CSRC, _instructions, _read_too_early
 def test_transfers_to_the_lds():
     asm = subprocess.run(["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-w",
                           "--offload-device-only", "-S", os.path.join(CSRC, "dn_paged_attn.hip"), "-o", "-"], check=True, capture_output=True, text=True).stdout
-    kernels = re.findall(r"^(_ZN2dn11k_attn_wideIDF16b\w+):(.*?)s_endpgm", asm, re.M | re.S)
-    assert len(kernels) == 3
+    kernels = re.findall(r"^(_ZN2dn11k_attn_(?:wide|both)IDF16b\w+):(.*?)s_endpgm", asm, re.M | re.S)
+    assert len(kernels) == 6
     for name, body in kernels:
         ops = list(_instructions(body))
         moves = [i for i, (op, words) in enumerate(ops) if op.startswith("buffer_load") and "lds" in words]
