@@ -67,26 +67,26 @@ __device__ inline void partial_of(const AttnArgs &a, int split, long row, int D,
 // --- Few rows: generation, and short chunks.
 //
 // Bound by the reading of the cache.  A wave takes 32 keys at a time straight from memory to its registers, in the order in which
-// the products want them: for S^T lane l holds a quarter (l / 16) of the elements of key l % 16 of each half; for O^T it holds a
-// sixteenth (l % 16) of the elements of the eight keys whose probabilities it has, which a 16-bit transposition among its own
-// registers turns into the operands of D / 16 products.  No LDS traffic and no barrier until the waves of a workgroup, which share out the
+// the products want them: for S^T lane l holds a quarter of the elements of key l % 16 of each half, every fourth 16-byte piece from l / 16 on; for O^T it
+// holds a sixteenth of the elements of the eight keys whose probabilities it has, one 16-byte piece (or less) of each 16, from l % 16 on, which a 16-bit
+// transposition among its own registers turns into the operands of D / 16 products.  (So the lanes of one load stand side by side.)  No LDS traffic and no barrier until the waves of a workgroup, which share out the
 // keys of one split, join their sums.
 constexpr int kFewTile = 16, kFewKeys = 32, kFewWaves = 4;
 
 template <typename T, typename CT> struct PageElem { typedef CT type; static constexpr int bytes = (int)sizeof(CT); };
 template <typename T> struct PageElem<T, fp8> { typedef unsigned char type; static constexpr int bytes = 1; };
 
-// W words at `off` bytes behind a descriptor's base.  (Buffer loads: the base, the same for the whole wave, stays in scalar registers, where a global load
+// W words, from `off` bytes behind a descriptor's base on, in pieces of 16 bytes that are `step` bytes apart.  (Buffer loads: the base, the same for the whole wave, stays in scalar registers, where a global load
 // would have a 64-bit address per lane and load.)
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-template <int W> __device__ inline void load_words(unsigned (&w)[W], __amdgpu_buffer_rsrc_t rs, int off) {
+template <int W> __device__ inline void load_words(unsigned (&w)[W], __amdgpu_buffer_rsrc_t rs, int off, int step = 16) {
     if constexpr (W == 1) w[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0);
     else if constexpr (W == 2) { const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0); w[0] = x[0]; w[1] = x[1]; }
     else {
 #pragma unroll
         for (int i = 0; i < W / 4; ++i) {
-            const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rs, off + 16 * i, 0, 0);
+            const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rs, off + step * i, 0, 0);
             w[4 * i] = x[0]; w[4 * i + 1] = x[1]; w[4 * i + 2] = x[2]; w[4 * i + 3] = x[3];
         }
     }
@@ -106,6 +106,8 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
     constexpr int EB = PageElem<T, CT>::bytes;
     constexpr int KE = D / 4, VE = D / 16;              // elements of a key, of a value, that a lane holds
     constexpr int KW = KE * EB / 4, VW = VE * EB / 4;   // in words
+    constexpr int KV = 16 / EB;                         // elements of a piece of a key: (4 piece + g) KV ..
+    constexpr int VV = VE * EB > 16 ? 16 / EB : VE;     // ... and of a value: (16 piece + col) VV ..
     constexpr bool FP8 = __is_same(CT, fp8);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int Hkv = a.r.Hkv, G = a.r.Hq / Hkv;
@@ -132,12 +134,16 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
     const int p_lo = a.window > 0 ? p - a.window + 1 : 0;                   // first key it sees
     const int all_from = a.window > 0 ? before + (row1 - 1) / G - a.window + 1 : 0, all_to = before + row0 / G; // keys in [all_from, all_to] are seen by every row
 
-    // the query: elements g KE .. g KE + KE - 1
+    // the query, in the same order as a key
     unsigned qw[KE * sizeof(T) / 4];
     {
-        const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const T *>(a.r.q) + (long)(s.r0 + tok) * a.r.q_stride + head * D + g * KE);
+        const T *src = static_cast<const T *>(a.r.q) + (long)(s.r0 + tok) * a.r.q_stride + head * D;
+        constexpr int PW = KV * (int)sizeof(T) / 16; // 16-byte words of a piece
 #pragma unroll
-        for (int i = 0; i < (int)(KE * sizeof(T) / 16); ++i) { const uint4 x = src[i]; qw[4 * i] = x.x; qw[4 * i + 1] = x.y; qw[4 * i + 2] = x.z; qw[4 * i + 3] = x.w; }
+        for (int i = 0; i < KE / KV * PW; ++i) {
+            const uint4 x = reinterpret_cast<const uint4 *>(src + (4 * (i / PW) + g) * KV)[i % PW];
+            qw[4 * i] = x.x; qw[4 * i + 1] = x.y; qw[4 * i + 2] = x.z; qw[4 * i + 3] = x.w;
+        }
     }
     const float c = a.scale * 1.4426950408889634f;
 
@@ -148,7 +154,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const long row = row_of(a.c, page[h], k0 + 16 * h, kvh, Hkv);
-            load_words(kw[h], make_rsrc(kp + row * (D * EB)), (col * D + g * KE) * EB);
+            load_words(kw[h], make_rsrc(kp + row * (D * EB)), col * D * EB + 16 * g, 64);
             if constexpr (FP8) ks[h] = *reinterpret_cast<const float4 *>(a.c.ks + row + 4 * g);
         }
     };
@@ -158,7 +164,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
             const long row = row_of(a.c, page[h], k0 + 16 * h, kvh, Hkv);
             const __amdgpu_buffer_rsrc_t va = make_rsrc(vp + row * (D * EB));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) load_words(vw[4 * h + i], va, ((4 * g + i) * D + col * VE) * EB);
+            for (int i = 0; i < 4; ++i) load_words(vw[4 * h + i], va, ((4 * g + i) * D + col * VV) * EB, 256);
             if constexpr (FP8) vs[h] = *reinterpret_cast<const float4 *>(a.c.vs + row + 4 * g);
         }
     };
@@ -279,7 +285,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
         }
     }
 
-    // the waves' sums: o of element (4 g + r) VE + j and query col stands at o[j][r]
+    // the waves' sums: o of element (16 piece + 4 g + r) VV + j and query col stands at o[piece VV + j][r]
     constexpr int LD = D + 4;
     float *so = smem, *sm = smem + kFewWaves * kFewTile * LD, *sl = sm + kFewWaves * kFewTile;
     {
@@ -293,7 +299,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int j = 0; j < VE; ++j) so[(wave * kFewTile + col) * LD + (4 * g + r) * VE + j] = o[j][r];
+        for (int j = 0; j < VE; ++j) so[(wave * kFewTile + col) * LD + (16 * (j / VV) + 4 * g + r) * VV + j % VV] = o[j][r];
     __syncthreads();
     const int q = threadIdx.x >> 4, e0 = (threadIdx.x & 15) * VE; // sixteen threads per query
     if (row0 + q >= row1) return;
@@ -780,7 +786,7 @@ Plan plan_attn(int dtype, int d, const AttnArgs &a) {
         return seen < a.c.max_kv ? seen : (long)a.c.max_kv;
     };
     // (where there are chunks, too, most of the others are single tokens: one tile)
-    p.few = p.tiles ? cut_keys(range(kFewKeys), (N > 0 ? N : 1) * (p.slots ? 1 : p.tiles) * a.r.Hkv, 1024, 256, kFewWaves * kFewKeys) : Cut{1, 128};
+    p.few = p.tiles ? cut_keys(range(kFewKeys), (N > 0 ? N : 1) * (p.slots ? 1 : p.tiles) * a.r.Hkv, 512, 256, kFewWaves * kFewKeys) : Cut{1, 128};
     const long full = rows / kWideRows;
     p.wide = p.slots ? cut_keys(range(wide_keys(d)), (full > 0 ? full : 1) * a.r.Hkv, d > 128 ? 256 : d > 64 ? 512 : 768, 512, wide_keys(d)) : Cut{1, 64};
     return p;
