@@ -291,7 +291,7 @@ typedef struct {
     int32_t Hq, Hkv, d;
     int32_t dtype, cache_dtype;
     int32_t page_size, num_pages, max_pages; /* max_pages: columns of page_table */
-    int32_t max_q, max_kv;               /* no sequence has more new tokens or a longer context (bounds suffice) */
+    int32_t max_q, max_kv;               /* no sequence has more new tokens or a longer context (bounds suffice); T, max_kv <= 2^30 */
     const int32_t *cu_q;                 /* DEVICE int32 [num_seqs + 1] */
     const int32_t *kv_len;               /* DEVICE int32 [num_seqs] */
     const int32_t *page_table;           /* DEVICE int32 [num_seqs, max_pages] */

@@ -193,7 +193,7 @@ struct Paged {
         s.num_seqs = int32(N, "sequences"); s.max_pages = int32(table.size(1), "max_pages");
         s.num_pages = int32(pages, "num_pages"); s.Hkv = int32(H, "heads"); s.page_size = int32(ps, "page_size"); s.d = int32(kp.size(3), "d");
         s.dtype = dtype; s.cache_dtype = quantised ? DN_FP8 : dtype;
-        s.max_kv = (int32_t)std::min<int64_t>(table.size(1) * ps, INT32_MAX);
+        s.max_kv = (int32_t)std::min<int64_t>(table.size(1) * ps, 1 << 30); // (the most that a context may have)
         s.cu_q = offsets.data_ptr<int32_t>(); s.kv_len = lens.data_ptr<int32_t>(); s.page_table = table.data_ptr<int32_t>();
         c.k_pages = kp.data_ptr(); c.v_pages = vp.data_ptr(); c.k_scale = fptr(ks); c.v_scale = fptr(vs);
     }

@@ -9,6 +9,8 @@ namespace {
 
 using namespace dn;
 
+constexpr int kMostTokens = 1 << 30;
+
 bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 int elem_bytes(int dtype) { return dtype == DN_BF16 ? 2 : 4; }
 
@@ -50,6 +52,7 @@ int check_paged(const dn_paged_shape *s) {
     if (ps != 16 && ps != 32 && ps != 64 && ps != 128 && ps != 256) return DN_ERR_UNSUPPORTED;
     if (s->num_seqs < 0 || s->num_seqs > 65535 || s->num_pages < 0 || s->max_pages < 0 || s->max_q < 0 || s->max_kv < 0) return DN_ERR_SHAPE;
     if (s->max_q > s->T || (long long)s->max_kv > (long long)s->max_pages * ps) return DN_ERR_SHAPE;
+    if (s->T > kMostTokens || s->max_kv > kMostTokens) return DN_ERR_SHAPE; // 32-bit positions, and some tiles past the last
     if (s->num_pages == 0 && s->max_kv > 0) return DN_ERR_SHAPE;
     if ((long long)s->Hkv * ps * s->d * elem_bytes(s->dtype) >= (1ll << 30)) return DN_ERR_SHAPE; // a page lies within a buffer descriptor's range
     return DN_OK;
@@ -116,7 +119,9 @@ AttnArgs attn_args(const dn_paged_shape *s, const dn_paged_cache *c, int window)
     a.r = row_args(s->T, s->Hq, s->Hkv);
     a.r.q_stride = s->q_stride;
     a.c = paged_args(s, c);
-    a.scale = 0.f; a.window = window; a.max_q = s->max_q; a.splits = 1;
+    a.scale = 0.f;
+    a.window = window >= s->max_kv ? 0 : window; // (a window as long as any context hides nothing)
+    a.max_q = s->max_q; a.splits = 1;
     a.workspace = nullptr;
     return a;
 }

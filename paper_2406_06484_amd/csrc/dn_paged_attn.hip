@@ -369,13 +369,13 @@ template <typename CT, int D> struct WideTile {
 // before those, and so on (in the order of the sequences, prompts of 4 x 2048 tokens took 160 us instead of 126).  False past the last slot.
 __device__ inline bool tile_of_slot(const AttnArgs &a, int G, int few, int slot, int *seq, int *tile) {
     const int lane = threadIdx.x & 63;
+    int next0 = 0, next1 = 0; // offsets of the 64 sequences to come, on their way while the present ones are gone through
+    auto ahead = [&](int n) { if (n < a.c.N) { next0 = a.c.cu[n]; next1 = a.c.cu[n + 1]; } };
+    ahead(lane);
     for (int base = 0; base < a.c.N; base += 64) {
-        const int n = base + lane;
-        int tiles = 0;
-        if (n < a.c.N) {
-            const int r0 = min(max(a.c.cu[n], 0), a.r.T), r1 = min(max(a.c.cu[n + 1], r0), a.r.T), R = (r1 - r0) * G;
-            tiles = R > few ? (R + kWideRows - 1) / kWideRows : 0;
-        }
+        const int n = base + lane, r0 = min(max(next0, 0), a.r.T), r1 = min(max(next1, r0), a.r.T), R = (r1 - r0) * G;
+        const int tiles = n < a.c.N && R > few ? (R + kWideRows - 1) / kWideRows : 0;
+        ahead(n + 64);
         int rank = 0; // tiles behind this one in its sequence
         for (unsigned long long on = __ballot(tiles > 0); on; on = __ballot(tiles > rank)) {
             const int count = __builtin_popcountll(on);

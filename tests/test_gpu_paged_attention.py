@@ -166,3 +166,31 @@ def test_refusals():
         assert e.value.status == status, kw
     with pytest.raises(ValueError):
         b.attend(q, o=torch.empty_like(q)[:1])
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+def test_many_sequences_of_every_kind(cache):
+    """more sequences than the search for a workgroup's tile looks at together, chunks beside single tokens and empty ones"""
+    qs = [(0, 1, 40, 3, 17, 90)[(7 * n) % 6] for n in range(150)]
+    kvs = [q + (5 * n) % 37 for n, q in enumerate(qs)]
+    b = Batch(qs, kvs, 1, 64, "bf16", cache, 16, seed=4)
+    _run(b, 2, "many", max_q=90, max_kv=max(kvs))
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_bounds_that_promise_equal_chunks_and_padded_rows(d):
+    """as many rows as sequences times max_q, but shorter sequences and rows that lie in none"""
+    b = Batch([40, 1, 0, 33], [70, 9, 5, 33], 2, d, "bf16", "bf16", 16, seed=d)
+    q, qh = b.rows(4, rows=4 * 40)
+    o = b.attend(q, max_q=40, o=torch.full_like(q, float("nan")))
+    torch.cuda.synchronize()
+    b.check(o, qh, d ** -0.5, 0, "padded")
+    assert not o[b.T:].any()
+
+
+def test_a_window_longer_than_the_context_is_none():
+    b = Batch([3, 50], [80, 60], 1, 128, "bf16", "bf16", 16)
+    q, _ = b.rows(2)
+    want = b.attend(q)
+    for window in (b.table.shape[1] * 16, 2 ** 31 - 1):
+        assert torch.equal(b.attend(q, window=window), want)
