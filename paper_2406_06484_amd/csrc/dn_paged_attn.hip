@@ -257,9 +257,15 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
                 for (int i = 0; i < 8; ++i)
                     o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vw[i][j]), st[i >> 2][i & 3], o[j], 0, 0, 0);
         } else {
-            bf16x8 pt;
+            // Probabilities as two bf16 terms: the products wait for memory anyway, and the output then carries the one rounding of its own (in one
+            // term, 1.4 times its error).
+            bf16x8 pt, pl;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) pt[i] = (bf16)st[i >> 2][i & 3];
+            for (int i = 0; i < 8; ++i) {
+                const float x = st[i >> 2][i & 3];
+                pt[i] = (bf16)x;
+                pl[i] = (bf16)(x - (float)pt[i]);
+            }
 #pragma unroll
             for (int w = 0; w < VE / 2; ++w) { // a pair of elements of eight keys -> eight keys of each element
                 unsigned x[8];
@@ -276,6 +282,8 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
                 }
                 o[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), pt, o[2 * w], 0, 0, 0);
                 o[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), pt, o[2 * w + 1], 0, 0, 0);
+                o[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), pl, o[2 * w], 0, 0, 0);
+                o[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), pl, o[2 * w + 1], 0, 0, 0);
             }
         }
         if (more) {
