@@ -323,9 +323,9 @@ int deltanet_paged_read(const dn_paged_shape *shape, const dn_paged_cache *cache
  *
  * (window = 0: the whole past).  A row without a position in its context (p < 0), or in no sequence, becomes zero.  Scores, the running maximum and sum and the output
  * are held in fp32; in bf16 the probabilities, multiplied by the cache's factors, enter the product with v as bf16 (in chunks of many rows
- * rounded, for few rows as two terms).  scale > 0.  Nothing at or past kv_len reaches a result, whatever the pages hold there (keys that a row's window or
- * place hides are given the weight zero: an infinity or NaN among THOSE values reaches rows that are worked on together with one
- * that sees it).  Deterministic: the order of every sum depends on the sizes and lengths alone.
+ * rounded, for few rows as two terms).  scale > 0.  Nothing at or past kv_len, nor before the windows of all of a sequence's new tokens, reaches a
+ * result, whatever the pages hold there (values that one new token sees and another does not are given the weight zero in the other's row: an
+ * infinity or NaN among THOSE may reach both).  Deterministic: the order of every sum depends on the sizes and lengths alone.
  * Compiled: d = 64, 128, 256 in bf16, with bf16 or DN_FP8 pages; d = 32, 64, 128 in fp32 (the precision mode).
  * Workspace: deltanet_paged_attn_workspace_bytes (it depends on num_seqs, T, the heads, d, the types, max_q, max_kv and window).
  */

@@ -26,12 +26,14 @@ struct SeqRows {
     }
 };
 
-// The keys that rows [row0, row1) of a sequence see between them: [lo, hi), lo a multiple of `step`.
-__device__ inline void key_range(const AttnArgs &a, const SeqRows &s, int G, int row0, int row1, int step, int &lo, int &hi) {
+// The keys that rows [row0, row1) of a sequence see between them: [from, hi); lo is `from` rounded down to a multiple of `step`.  Values outside, which a
+// window may have left to other sequences, enter no product, whatever stands there.
+__device__ inline void key_range(const AttnArgs &a, const SeqRows &s, int G, int row0, int row1, int step, int &lo, int &from, int &hi) {
     const int before = s.kv - (s.r1 - s.r0); // position of the first new token
     hi = max(before + (row1 - 1) / G + 1, 0);
     const int first = max(before + row0 / G, 0);
-    lo = a.window > 0 ? max(first - a.window + 1, 0) / step * step : 0;
+    from = a.window > 0 ? max(first - a.window + 1, 0) : 0;
+    lo = from / step * step;
 }
 
 // The page table's entry for key kk, the page that it stands for, and (the wave's key kk, a multiple of 16: a page holds at least 16) the
@@ -124,8 +126,8 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
     const int R = (s.r1 - s.r0) * G, row0 = tile * kFewTile;
     if (R > max_rows || row0 >= R) return;
     const int row1 = min(row0 + kFewTile, R);
-    int lo, hi;
-    key_range(a, s, G, row0, row1, kFewKeys, lo, hi);
+    int lo, from, hi;
+    key_range(a, s, G, row0, row1, kFewKeys, lo, from, hi);
     const int k_begin = lo + split * split_keys, k_end = min(hi, k_begin + split_keys);
     if (splits > 1 && k_begin >= k_end) return; // (the rows' other splits know)
     const bool valid = row0 + col < row1;
@@ -236,12 +238,13 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
 #pragma unroll
             for (int i = 0; i < 4; ++i) { st[h][i] = __builtin_amdgcn_exp2f(fmaf(st[h][i], c, -m)); sum += st[h][i]; }
         l += sum;
-        if (k0 + kFewKeys > hi) { // nothing past the last key that a row sees is read into a result, whatever stands there
+        if (k0 + kFewKeys > hi || k0 < from) { // what no row sees enters no result
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const bool dead = k0 + 16 * h + 4 * g + i >= hi;
+                    const int key = k0 + 16 * h + 4 * g + i;
+                    const bool dead = key >= hi || key < from;
 #pragma unroll
                     for (int w = 0; w < VW; ++w) vw[4 * h + i][w] = dead ? 0u : vw[4 * h + i][w];
                     if constexpr (FP8) if (dead) reinterpret_cast<float *>(&vs[h])[i] = 0.f;
@@ -425,8 +428,8 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
     SeqRows s;
     s.load(a, n);
     const int R = (s.r1 - s.r0) * G, row0 = tile * kWideRows, row1 = min(row0 + kWideRows, R);
-    int lo, hi;
-    key_range(a, s, G, row0, row1, KEYS, lo, hi);
+    int lo, from, hi;
+    key_range(a, s, G, row0, row1, KEYS, lo, from, hi);
     const int k_begin = lo + split * split_keys, k_end = min(hi, k_begin + split_keys);
     if (splits > 1 && k_begin >= k_end) return; // (the rows' other splits know)
     const int wrow = row0 + 32 * wave, before = s.kv - (s.r1 - s.r0);
@@ -476,11 +479,11 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
             if (i == 0 && wave < 2 && lane < KEYS)
                 rs = (wave ? a.c.vs : a.c.ks)[row_of(a.c, page_id(a.c, spage), k0 + (lane & 48), kvh, Hkv) + (lane & 15)];
         } else {
-            // nothing past the last key that a row sees is read into a result, whatever stands there: such values arrive as zeros
+            // values that no row sees arrive as zeros
             const int off = (r & 15) * (D * EB) + ((piece ^ W::swizzle(r)) << 4);
             const unsigned to = lds_place(buf) + (i * 256 + wave * 64) * 16;
             move16(make_rsrc(kp + at), off, to);
-            move16(make_rsrc(vp + at), k0 + r < hi ? off : kBufRange, to + W::oV);
+            move16(make_rsrc(vp + at), (unsigned)(k0 + r - from) < (unsigned)(hi - from) ? off : kBufRange, to + W::oV);
         }
     };
     auto fetch_all = [&](unsigned char *buf, int k0) __attribute__((always_inline)) {
@@ -489,12 +492,13 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
         look_up(k0 + KEYS);
     };
     auto park = [&](unsigned char *buf, int k0) __attribute__((always_inline)) {
-        const bool tail = k0 + KEYS > hi; // nothing past the last key that a row sees is read into a result, whatever stands there
+        const bool ends = k0 + KEYS > hi || k0 < from; // values that no row sees become zeros
+        auto dead = [&](int key) { return key >= hi || key < from; };
 #pragma unroll
         for (int i = 0; i < W::NL; ++i) {
             const int r = (i * 256 + t) / W::LPR;
             u32x4 v = rv[i];
-            if (tail && k0 + r >= hi) v = u32x4{0, 0, 0, 0};
+            if (ends && dead(k0 + r)) v = u32x4{0, 0, 0, 0};
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 unsigned char *at = buf + r * W::ROWB + (((2 * piece + u) ^ W::swizzle(r)) << 4);
@@ -502,7 +506,7 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
                 *reinterpret_cast<u32x4 *>(at + W::oV) = widen(v[2 * u], v[2 * u + 1]);
             }
         }
-        if (wave < 2 && lane < KEYS) reinterpret_cast<float *>(buf + (wave ? W::oVS : W::oKS))[lane] = tail && k0 + lane >= hi ? 0.f : rs;
+        if (wave < 2 && lane < KEYS) reinterpret_cast<float *>(buf + (wave ? W::oVS : W::oKS))[lane] = ends && dead(k0 + lane) ? 0.f : rs;
     };
     // a tile's work, and between its first products the requests for tile `next` (16 bits: into `to`), if `more`
     auto work = [&](const unsigned char *buf, int k0, unsigned char *to, int next, bool more) __attribute__((always_inline)) {
@@ -706,8 +710,8 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, Cut cut, int few_
         if ((s.r1 - s.r0) * G <= few_rows) return;
     }
     constexpr int ROWS = FEW ? kFewTile : kWideRows;
-    int lo, hi;
-    key_range(a, s, G, r / ROWS * ROWS, min(r / ROWS * ROWS + ROWS, (s.r1 - s.r0) * G), FEW ? kFewKeys : wide_keys(D), lo, hi);
+    int lo, from, hi;
+    key_range(a, s, G, r / ROWS * ROWS, min(r / ROWS * ROWS + ROWS, (s.r1 - s.r0) * G), FEW ? kFewKeys : wide_keys(D), lo, from, hi);
     const int live = hi > lo ? min((hi - lo + cut.keys - 1) / cut.keys, cut.splits) : 0;
     const long row = (long)(s.r0 + r / G) * a.r.Hq + kvh * G + r % G;
     const int in = WHOLE ? threadIdx.x : lane, e0 = in % LPR * 4, side = in / LPR;

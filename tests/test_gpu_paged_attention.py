@@ -93,6 +93,22 @@ def test_sharp_and_flat_scores():
     _run(b, 2, "flat")
 
 
+@pytest.mark.parametrize("dtype,cache,d", [("bf16", "bf16", 64), ("bf16", "bf16", 256), ("bf16", "fp8", 128), ("f32", "f32", 64)])
+def test_what_the_windows_left_behind_reaches_no_result(dtype, cache, d):
+    """places in front of a sequence's windows may belong to other sequences by now, or hold nothing that was ever written"""
+    window = 21
+    b = Batch([1, 70, 5, 2], [333, 170, 90, 22], 2, d, dtype, cache, 16)
+    for n, (m, kv) in enumerate(zip(b.qs, b.kvs)):
+        at = torch.arange(max(kv - m - window + 1, 0))
+        ids, slots = b.table_host[n].long()[at // 16].cuda(), (at % 16).cuda()
+        for t in (b.k_pages, b.v_pages, b.k_scale, b.v_scale):
+            if t is not None:
+                x = t.float()
+                x[ids, :, slots] = float("nan")
+                t.copy_(x.to(t.dtype))
+    _run(b, 4, "windows", window=window)
+
+
 def test_a_querys_nan_stays_in_its_row():
     b = Batch([4, 50], [100, 90], 1, 128, "bf16", "bf16", 16)
     q, qh = b.rows(2)
