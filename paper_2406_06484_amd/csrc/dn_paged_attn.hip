@@ -681,25 +681,17 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_both(
     else attend_few<bf16, CT, D>(a, tiles, few, few_rows, blockIdx.x - wide_blocks, reinterpret_cast<float *>(lds));
 }
 
-// Joins the splits of a row (token and head).  FEW: of the sequences that attend_few takes, else of the others.  WHOLE: a workgroup per row, for few rows with
-// many splits (16 rows of 128, 64 splits: a wave per row took 17 us, one load after the other); else a wave per row.
-template <typename T, int D, bool FEW, bool WHOLE>
-__global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, Cut cut, int few_rows, int per_seq) {
+// Joins the splits of a row (token and head).  ALL: a wave for each row, of either kind; else of the sequences that attend_few takes, where there are no others.
+// WHOLE: a workgroup per row, for few rows with many splits (16 rows of 128, 64 splits: a wave per row took 17 us, one load after the other).
+template <typename T, int D, bool ALL, bool WHOLE>
+__global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, Cut few, Cut wide, int few_rows, int per_seq) {
     constexpr int LPR = D / 4, TPR = WHOLE ? 256 : 64, SIDE = TPR / LPR; // lanes of a row, threads of a row, splits side by side
     __shared__ float part[WHOLE ? 4 : 1][D + 4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int G = a.r.Hq / a.r.Hkv;
     int n, kvh, r;
     SeqRows s;
-    if (FEW) {
-        long b = WHOLE ? (long)blockIdx.x : (long)blockIdx.x * 4 + wave;
-        r = (int)(b % per_seq); b /= per_seq;
-        kvh = (int)(b % a.r.Hkv); n = (int)(b / a.r.Hkv);
-        if (n >= a.c.N) return;
-        s.load(a, n);
-        const int R = (s.r1 - s.r0) * G;
-        if (r >= R || R > few_rows) return;
-    } else {
+    if (ALL) {
         const long row = (long)blockIdx.x * 4 + wave;
         if (row >= (long)a.r.T * a.r.Hq) return;
         const int t = (int)(row / a.r.Hq), h = (int)(row % a.r.Hq);
@@ -707,11 +699,21 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, Cut cut, int few_
         if (n >= a.c.N) return; // (zeroed)
         s.load(a, n);
         kvh = h / G; r = max(t - s.r0, 0) * G + h % G;
-        if ((s.r1 - s.r0) * G <= few_rows) return;
+    } else {
+        long b = WHOLE ? (long)blockIdx.x : (long)blockIdx.x * 4 + wave;
+        r = (int)(b % per_seq); b /= per_seq;
+        kvh = (int)(b % a.r.Hkv); n = (int)(b / a.r.Hkv);
+        if (n >= a.c.N) return;
+        s.load(a, n);
     }
-    constexpr int ROWS = FEW ? kFewTile : kWideRows;
+    const int R = (s.r1 - s.r0) * G;
+    if (!ALL && (r >= R || R > few_rows)) return;
+    const bool is_few = !ALL || R <= few_rows;
+    const Cut cut = is_few ? few : wide;
+    if (cut.splits == 1) return; // (stored as they are)
+    const int rows = is_few ? kFewTile : kWideRows;
     int lo, from, hi;
-    key_range(a, s, G, r / ROWS * ROWS, min(r / ROWS * ROWS + ROWS, (s.r1 - s.r0) * G), FEW ? kFewKeys : wide_keys(D), lo, from, hi);
+    key_range(a, s, G, r / rows * rows, min(r / rows * rows + rows, R), is_few ? kFewKeys : wide_keys(D), lo, from, hi);
     const int live = hi > lo ? min((hi - lo + cut.keys - 1) / cut.keys, cut.splits) : 0;
     const long row = (long)(s.r0 + r / G) * a.r.Hq + kvh * G + r % G;
     const int in = WHOLE ? threadIdx.x : lane, e0 = in % LPR * 4, side = in / LPR;
@@ -764,7 +766,7 @@ constexpr int kMostSplits = 128;
 struct Plan { int few_rows, per_seq, tiles, slots; Cut few, wide; };
 
 // `range` keys at most, in `blocks` workgroups without a cut: as many splits as make up to `want` workgroups, each of `least` keys or more.
-Cut cut_keys(long range, long blocks, long want, int least, int step) {
+Cut cut_keys(long range, long blocks, long want, long least, int step) {
     long splits = want / blocks, most = (range + least - 1) / least;
     splits = splits < most ? splits : most;
     splits = splits < 1 ? 1 : splits > kMostSplits ? kMostSplits : splits;
@@ -797,10 +799,12 @@ Plan plan_attn(int dtype, int d, const AttnArgs &a) {
         const long seen = a.window > 0 ? (long)a.window + a.max_q + step : a.c.max_kv;
         return seen < a.c.max_kv ? seen : (long)a.c.max_kv;
     };
-    // (where there are chunks, too, most of the others are single tokens: one tile)
-    p.few = p.tiles ? cut_keys(range(kFewKeys), (N > 0 ? N : 1) * (p.slots ? 1 : p.tiles) * a.r.Hkv, 512, 256, kFewWaves * kFewKeys) : Cut{1, 128};
     const long full = rows / kWideRows;
     p.wide = p.slots ? cut_keys(range(wide_keys(d)), (full > 0 ? full : 1) * a.r.Hkv, d > 128 ? 256 : d > 64 ? 512 : 768, 512, wide_keys(d)) : Cut{1, 64};
+    // Beside chunks, whose walks take longer per key, rows are cut no finer than twice as long as those, and not at all where those are not: the join would cost more
+    // than it brought.  (Most of these sequences are single tokens: one tile.)
+    const long seen = range(kFewKeys), least = !p.slots ? 256 : p.wide.splits == 1 ? seen : 2l * p.wide.keys;
+    p.few = p.tiles ? cut_keys(seen, (N > 0 ? N : 1) * (p.slots ? 1 : p.tiles) * a.r.Hkv, 512, least > 256 ? least : 256, kFewWaves * kFewKeys) : Cut{1, 128};
     return p;
 }
 
@@ -845,15 +849,15 @@ template <typename T, typename CT, int D> int launch_attn(int dtype, AttnArgs a,
                 void *args[] = {&a, &p.wide, &p.few_rows};
                 e = launch("k_attn_wide", reinterpret_cast<const void *>(k_attn_wide<CT, D>), wide_blocks, 64 * kWideWaves, wide_lds, args, stream);
             }
-            void *join[] = {&a, &p.wide, &p.few_rows, &p.per_seq};
-            if (!e && p.wide.splits > 1)
-                e = launch("k_attn_join", reinterpret_cast<const void *>(k_attn_join<T, D, false, false>), ((long)a.r.T * a.r.Hq + 3) / 4, 256, 0, join, stream);
+            if (e || a.splits == 1) return e;
+            void *join[] = {&a, &p.few, &p.wide, &p.few_rows, &p.per_seq};
+            return launch("k_attn_join", reinterpret_cast<const void *>(k_attn_join<T, D, true, false>), ((long)a.r.T * a.r.Hq + 3) / 4, 256, 0, join, stream);
         }
-    if (e || !p.tiles || p.few.splits == 1) return e;
+    if (e || a.splits == 1) return e;
     const long rows = (long)a.c.N * a.r.Hkv * p.per_seq;
     const bool whole = rows <= 2048;
-    void *join[] = {&a, &p.few, &p.few_rows, &p.per_seq};
-    return launch("k_attn_join", whole ? reinterpret_cast<const void *>(k_attn_join<T, D, true, true>) : reinterpret_cast<const void *>(k_attn_join<T, D, true, false>),
+    void *join[] = {&a, &p.few, &p.wide, &p.few_rows, &p.per_seq};
+    return launch("k_attn_join", whole ? reinterpret_cast<const void *>(k_attn_join<T, D, false, true>) : reinterpret_cast<const void *>(k_attn_join<T, D, false, false>),
                   whole ? rows : (rows + 3) / 4, 256, 0, join, stream);
 }
 
