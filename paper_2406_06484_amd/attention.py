@@ -78,11 +78,14 @@ def _module():
     return _ext
 
 
-def _stream(stream) -> Optional[int]:
-    return None if stream is None else stream.cuda_stream
-
-
-def _done(r):
+def _call(name: str, stream, *args):
+    fn = getattr(_ext or _module(), name)
+    if stream is None:
+        r = fn(*args)
+    else:
+        import torch
+        with torch.cuda.stream(stream):     # what the call allocates belongs to the stream that works on it
+            r = fn(*args)
     if type(r) is int:
         _check(r)
     return r
@@ -94,7 +97,7 @@ def deltanet_qk_norm_rope_fwd(q, k, q_weight=None, k_weight=None, rope=None, pos
     q [T, Hq, d] or [B, L, Hq, d] and k may be column blocks of one projection's output (rows apart).  rope: fp32 [max_pos, rot],
     the rot / 2 cosines and then the rot / 2 sines of every position, or None for no rotation.  positions: int32, one per
     row; without it a row's place in its sequence (dense) or in the tensor (packed)."""
-    return _done((_ext or _module()).norm_rope_fwd(q, k, q_weight, k_weight, rope, positions, eps, interleaved, q_out, k_out, _stream(stream)))
+    return _call("norm_rope_fwd", stream, q, k, q_weight, k_weight, rope, positions, eps, interleaved, q_out, k_out)
 
 
 def deltanet_qk_norm_rope_bwd(q, k, dq_out, dk_out, q_weight=None, k_weight=None, rope=None, positions=None, *, eps: float = 1e-6,
@@ -102,8 +105,8 @@ def deltanet_qk_norm_rope_bwd(q, k, dq_out, dk_out, q_weight=None, k_weight=None
                               stream=None):
     """Gradient of deltanet_qk_norm_rope_fwd; returns (dq, dk, dq_weight, dk_weight), the last two in fp32 and None where there is no
     weight.  dq and dk may be dq_out and dk_out themselves."""
-    return _done((_ext or _module()).norm_rope_bwd(q, k, dq_out, dk_out, q_weight, k_weight, rope, positions, eps, interleaved, dq, dk,
-                                                   dq_weight, dk_weight, workspace, _stream(stream)))
+    return _call("norm_rope_bwd", stream, q, k, dq_out, dk_out, q_weight, k_weight, rope, positions, eps, interleaved, dq, dk,
+                 dq_weight, dk_weight, workspace)
 
 
 def deltanet_paged_cache(num_pages: int, page_size: int, heads: int, d: int, dtype=None, device="cuda"):
@@ -123,7 +126,7 @@ def deltanet_paged_append(k, v, k_pages, v_pages, page_table, kv_len, cu_q, *, k
     """Writes the new tokens' k and v [T, Hkv, d] to the paged cache (8-bit pages: quantised on the way).  Sequence n's new tokens are
     rows cu_q[n] .. cu_q[n + 1] - 1, the last of them token kv_len[n] - 1 of its context; its token p stands in page
     page_table[n, p // page_size], slot p % page_size."""
-    return _done((_ext or _module()).append(k, v, k_pages, v_pages, page_table, kv_len, cu_q, k_scale, v_scale, _stream(stream)))
+    return _call("append", stream, k, v, k_pages, v_pages, page_table, kv_len, cu_q, k_scale, v_scale)
 
 
 def deltanet_paged_norm_rope_append(q, k, v, k_pages, v_pages, page_table, kv_len, cu_q, q_weight=None, k_weight=None, rope=None, *,
@@ -131,8 +134,8 @@ def deltanet_paged_norm_rope_append(q, k, v, k_pages, v_pages, page_table, kv_le
                                     stream=None) -> "torch.Tensor":
     """The serving form of deltanet_qk_norm_rope_fwd, in one pass with deltanet_paged_append: k normalised and rotated, and v, go to the
     cache; returns q normalised and rotated.  Positions are the tokens' places in their contexts."""
-    return _done((_ext or _module()).norm_rope_append(q, k, v, k_pages, v_pages, page_table, kv_len, cu_q, q_weight, k_weight, rope,
-                                                      k_scale, v_scale, eps, interleaved, q_out, _stream(stream)))
+    return _call("norm_rope_append", stream, q, k, v, k_pages, v_pages, page_table, kv_len, cu_q, q_weight, k_weight, rope,
+                 k_scale, v_scale, eps, interleaved, q_out)
 
 
 def deltanet_paged_read(k_pages, v_pages, page_table, kv_len, cu_out, rows: int, *, dtype=None, k_scale=None, v_scale=None, k_out=None,
@@ -147,8 +150,7 @@ def deltanet_paged_read(k_pages, v_pages, page_table, kv_len, cu_out, rows: int,
         code = DN_F32
     else:
         raise TypeError("dtype must be float32 or bfloat16, got %s" % held)
-    return _done((_ext or _module()).read(k_pages, v_pages, page_table, kv_len, cu_out, rows, code, k_scale, v_scale, k_out, v_out,
-                                          _stream(stream)))
+    return _call("read", stream, k_pages, v_pages, page_table, kv_len, cu_out, rows, code, k_scale, v_scale, k_out, v_out)
 
 
 def deltanet_paged_attn_workspace_bytes(shape: dn_paged_shape, window: int = 0) -> int:
@@ -164,5 +166,5 @@ def deltanet_paged_attn_fwd(q, k_pages, v_pages, page_table, kv_len, cu_q, *, k_
     [T, Hq, d].  The row at position p sees keys max(0, p - window + 1) .. p (window 0: its whole past); scale is d ** -0.5 by
     default.  max_q and max_kv: bounds on the longest chunk and the longest context (T and the page table's width by default; close bounds
     make for better-sized launches)."""
-    return _done((_ext or _module()).attn(q, k_pages, v_pages, page_table, kv_len, cu_q, k_scale, v_scale, scale, window, max_q, max_kv, o,
-                                          workspace, _stream(stream)))
+    return _call("attn", stream, q, k_pages, v_pages, page_table, kv_len, cu_q, k_scale, v_scale, scale, window, max_q, max_kv, o,
+                 workspace)

@@ -87,9 +87,8 @@ int type_of(const at::Tensor &t, const char *name) {
 void *ptr(const at::Tensor *t) { return t ? t->data_ptr() : nullptr; }
 float *fptr(const at::Tensor *t) { return static_cast<float *>(ptr(t)); }
 
-// the given stream's handle, or that of the current stream of t's device
-void *stream_of(PyObject *given, const at::Tensor &t) {
-    if (given != Py_None) return reinterpret_cast<void *>(integer(given, "stream"));
+// handle of the current stream of t's device
+void *stream_of(const at::Tensor &t) {
     PyObject *at = PyLong_FromLong(t.get_device());
     PyObject *h = at ? PyObject_CallFunctionObjArgs(g_raw_stream, at, nullptr) : nullptr;
     Py_XDECREF(at);
@@ -227,7 +226,7 @@ PyObject *norm_rope_fwd(Args a) {
     weights(qw, kw, x.type, x.s.d);
     const at::Tensor qo = out(maybe(a[8], "q_out"), "q_out", q.sizes(), q, x.type), ko = out(maybe(a[9], "k_out"), "k_out", k.sizes(), q, x.type);
     const int rc = lib.norm_rope_fwd(&x.s, &r, x.q.data_ptr(), x.k.data_ptr(), ptr(qw), ptr(kw), fptr(table), static_cast<int32_t *>(ptr(pos)), qo.data_ptr(),
-                                     ko.data_ptr(), stream_of(a[10], q));
+                                     ko.data_ptr(), stream_of(q));
     return rc ? PyLong_FromLong(rc) : tuple_of({&qo, &ko});
 }
 
@@ -250,7 +249,7 @@ PyObject *norm_rope_bwd(Args a) {
     if (rc) return PyLong_FromLong(rc);
     const Scratch ws(maybe(a[14], "workspace"), qw || kw ? need : 0, q);
     rc = lib.norm_rope_bwd(&x.s, &r, x.q.data_ptr(), x.k.data_ptr(), dqo.data_ptr(), dko.data_ptr(), ptr(qw), ptr(kw), fptr(table), static_cast<int32_t *>(ptr(pos)),
-                           dq.data_ptr(), dk.data_ptr(), qw ? fptr(&dqw) : nullptr, kw ? fptr(&dkw) : nullptr, ws.p(), ws.bytes, stream_of(a[15], q));
+                           dq.data_ptr(), dk.data_ptr(), qw ? fptr(&dqw) : nullptr, kw ? fptr(&dkw) : nullptr, ws.p(), ws.bytes, stream_of(q));
     return rc ? PyLong_FromLong(rc) : tuple_of({&dq, &dk, qw ? &dqw : nullptr, kw ? &dkw : nullptr});
 }
 
@@ -261,7 +260,7 @@ PyObject *append(Args a) {
     p.s.T = int32(T, "T"); p.s.Hq = p.s.Hkv;
     p.s.k_stride = rows(k, "k", k.scalar_type(), T, p.s.Hkv, p.s.d);
     p.s.v_stride = rows(v, "v", k.scalar_type(), T, p.s.Hkv, p.s.d);
-    const int rc = lib.append(&p.s, k.data_ptr(), v.data_ptr(), &p.c, stream_of(a[9], k));
+    const int rc = lib.append(&p.s, k.data_ptr(), v.data_ptr(), &p.c, stream_of(k));
     if (rc) return PyLong_FromLong(rc);
     Py_RETURN_NONE;
 }
@@ -279,7 +278,7 @@ PyObject *norm_rope_append(Args a) {
     const dn_rope r = rope_of(table, a[13], a[14]);
     weights(qw, kw, type, p.s.d);
     const at::Tensor qo = out(maybe(a[15], "q_out"), "q_out", q.sizes(), q, type);
-    const int rc = lib.norm_rope_append(&p.s, &r, q.data_ptr(), k.data_ptr(), v.data_ptr(), ptr(qw), ptr(kw), fptr(table), qo.data_ptr(), &p.c, stream_of(a[16], q));
+    const int rc = lib.norm_rope_append(&p.s, &r, q.data_ptr(), k.data_ptr(), v.data_ptr(), ptr(qw), ptr(kw), fptr(table), qo.data_ptr(), &p.c, stream_of(q));
     return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(qo);
 }
 
@@ -292,7 +291,7 @@ PyObject *read(Args a) { // dtype as a dn_dtype
     p.s.Hq = p.s.Hkv;
     const at::ScalarType type = dtype == DN_F32 ? at::kFloat : at::kBFloat16;
     const at::Tensor ko = out(maybe(a[9], "k_out"), "k_out", {T, p.s.Hkv, p.s.d}, kp, type), vo = out(maybe(a[10], "v_out"), "v_out", {T, p.s.Hkv, p.s.d}, kp, type);
-    const int rc = lib.read(&p.s, &p.c, p.s.cu_q, T, ko.data_ptr(), vo.data_ptr(), stream_of(a[11], kp));
+    const int rc = lib.read(&p.s, &p.c, p.s.cu_q, T, ko.data_ptr(), vo.data_ptr(), stream_of(kp));
     return rc ? PyLong_FromLong(rc) : tuple_of({&ko, &vo});
 }
 
@@ -311,7 +310,7 @@ PyObject *attn(Args a) {
     const at::Tensor o = out(maybe(a[12], "o"), "o", q.sizes(), q, q.scalar_type());
     const Scratch ws(maybe(a[13], "workspace"), need, q);
     const float scale = a[8] == Py_None ? 1.f / std::sqrt((float)p.s.d) : (float)number(a[8], "scale");
-    rc = lib.attn(&p.s, q.data_ptr(), &p.c, scale, window, o.data_ptr(), ws.p(), ws.bytes, stream_of(a[14], q));
+    rc = lib.attn(&p.s, q.data_ptr(), &p.c, scale, window, o.data_ptr(), ws.p(), ws.bytes, stream_of(q));
     return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(o);
 }
 
@@ -348,12 +347,12 @@ PyObject *open_library(PyObject *, PyObject *args) {
 
 #define ENTRY(NAME, F, N) {NAME, (PyCFunction)(void (*)(void))(PyObject * (*)(PyObject *, PyObject *const *, Py_ssize_t))entry<F, N>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"open", open_library, METH_VARARGS, nullptr},
-                         ENTRY("norm_rope_fwd", norm_rope_fwd, 11),
-                         ENTRY("norm_rope_bwd", norm_rope_bwd, 16),
-                         ENTRY("append", append, 10),
-                         ENTRY("norm_rope_append", norm_rope_append, 17),
-                         ENTRY("read", read, 12),
-                         ENTRY("attn", attn, 15),
+                         ENTRY("norm_rope_fwd", norm_rope_fwd, 10),
+                         ENTRY("norm_rope_bwd", norm_rope_bwd, 15),
+                         ENTRY("append", append, 9),
+                         ENTRY("norm_rope_append", norm_rope_append, 16),
+                         ENTRY("read", read, 11),
+                         ENTRY("attn", attn, 14),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_attention", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

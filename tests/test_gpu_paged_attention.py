@@ -138,6 +138,22 @@ def test_strided_queries_other_streams_and_the_same_bits_again():
     b.check(want, q.double().cpu(), 128 ** -0.5, 0, "strided")
 
 
+def test_a_given_stream_owns_what_the_call_allocates():
+    """the workspace of a call on another stream is not handed to this stream's tensors while the call is still to run"""
+    b = Batch([1], [4000], 2, 128, "bf16", "bf16", 64)
+    q, _ = b.rows(8)
+    want = b.attend(q)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(2_000_000)
+    o = b.attend(q, stream=side)
+    taken = [torch.zeros(1 << n, dtype=torch.uint8, device="cuda") for n in range(9, 22) for _ in range(3)]
+    side.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(o, want) and not any(bool(t.any()) for t in taken)
+
+
 def test_chunks_in_pieces_equal_one_call():
     """a prompt processed in chunks over the cache gives what one call gives, to rounding"""
     b = Batch([300], [300], 2, 64, "f32", "f32", 16)
