@@ -761,6 +761,7 @@ namespace {
 // Rows of a sequence and key/value head up to which the kernel for few rows takes them (fp32: always).
 constexpr int kFewMost = 32;
 constexpr int kMostSplits = 128;
+constexpr int kUncut = 640 * 128;
 
 // per_seq: most rows of a sequence and key/value head that attend_few has; tiles: its tiles of them (0: there is none); slots: row tiles of attend_wide
 struct Plan { int few_rows, per_seq, tiles, slots; Cut few, wide; };
@@ -801,10 +802,13 @@ Plan plan_attn(int dtype, int d, const AttnArgs &a) {
     };
     const long full = rows / kWideRows;
     p.wide = p.slots ? cut_keys(range(wide_keys(d)), (full > 0 ? full : 1) * a.r.Hkv, d > 128 ? 256 : d > 64 ? 512 : 768, 512, wide_keys(d)) : Cut{1, 64};
-    // Beside chunks, whose walks take longer per key, rows are cut no finer than twice as long as those, and not at all where those are not: the join would cost more
-    // than it brought.  (Most of these sequences are single tokens: one tile.)
-    const long seen = range(kFewKeys), least = !p.slots ? 256 : p.wide.splits == 1 ? seen : 2l * p.wide.keys;
-    p.few = p.tiles ? cut_keys(seen, (N > 0 ? N : 1) * (p.slots ? 1 : p.tiles) * a.r.Hkv, 512, least > 256 ? least : 256, kFewWaves * kFewKeys) : Cut{1, 128};
+    // A second launch for the join and the splits' way through memory cost 4 to 5 us, a walk 1 us for each 128 keys of d = 128: contexts up to kUncut / d are not cut
+    // (one token over 300 keys, d = 128: 7.5 us instead of 10.5; over 500, 8.8 instead of 10.6; over 1000 it would take 13.0 instead of 11.0), and never into more
+    // than 64 (32768 keys, e4m3, 4 heads: 15.1 us, in 128 pieces 16.4).  Beside chunks, whose walks take longer per key, no finer than twice as long as those, and not at
+    // all where those are not: the join would cost more than it brought.  (Most of these sequences are single tokens: one tile.)
+    const long seen = range(kFewKeys), blocks = (N > 0 ? N : 1) * (p.slots ? 1 : p.tiles) * a.r.Hkv, uncut = kUncut / (dtype == 0 ? 2 * d : d);
+    const long least = p.slots ? (p.wide.splits == 1 ? seen : 2l * p.wide.keys) : seen <= (uncut < 1024 ? uncut : 1024) ? seen : 256;
+    p.few = p.tiles ? cut_keys(seen, blocks, 64 * blocks < 512 ? 64 * blocks : 512, least > 256 ? least : 256, kFewWaves * kFewKeys) : Cut{1, 128};
     return p;
 }
 
