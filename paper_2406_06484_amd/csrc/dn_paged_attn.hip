@@ -74,6 +74,8 @@ __device__ inline void partial_of(const AttnArgs &a, int split, long row, int D,
 // transposition among its own registers turns into the operands of D / 16 products.  (So the lanes of one load stand side by side.)  No LDS traffic and no barrier until the waves of a workgroup, which share out the
 // keys of one split, join their sums.
 constexpr int kFewTile = 16, kFewKeys = 32, kFewWaves = 4;
+// Twice as many waves per workgroup where there are few workgroups, if their registers allow it.
+template <typename T> constexpr bool few_twice(int d) { return d * sizeof(T) <= 256; }
 
 template <typename T, typename CT> struct PageElem { typedef CT type; static constexpr int bytes = (int)sizeof(CT); };
 template <typename T> struct PageElem<T, fp8> { typedef unsigned char type; static constexpr int bytes = 1; };
@@ -102,7 +104,7 @@ __device__ inline unsigned bf16_pair(unsigned w, bool hi) {
 // eight e4m3 numbers as bf16
 __device__ inline u32x4 widen(unsigned lo, unsigned hi) { return u32x4{bf16_pair(lo, false), bf16_pair(lo, true), bf16_pair(hi, false), bf16_pair(hi, true)}; }
 
-template <typename T, typename CT, int D>
+template <typename T, typename CT, int D, int WAVES>
 __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut, int max_rows, int block, float *smem) {
     const int splits = cut.splits, split_keys = cut.keys;
     constexpr int EB = PageElem<T, CT>::bytes;
@@ -176,7 +178,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
     for (int j = 0; j < VE; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = kNoScore, l = 0.f;
 
-    constexpr int STEP = kFewWaves * kFewKeys;
+    constexpr int STEP = WAVES * kFewKeys;
     int k0 = k_begin + wave * kFewKeys;
     int page[2], next[2];
     if (k0 < k_end) {
@@ -298,7 +300,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
 
     // the waves' sums: o of element (16 piece + 4 g + r) VV + j and query col stands at o[piece VV + j][r]
     constexpr int LD = D + 4;
-    float *so = smem, *sm = smem + kFewWaves * kFewTile * LD, *sl = sm + kFewWaves * kFewTile;
+    float *so = smem, *sm = smem + WAVES * kFewTile * LD, *sl = sm + WAVES * kFewTile;
     {
         const unsigned u = __float_as_uint(l);
         const auto x = __builtin_amdgcn_permlane16_swap(u, u, false, false);
@@ -313,14 +315,14 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
         for (int j = 0; j < VE; ++j) so[(wave * kFewTile + col) * LD + (16 * (j / VV) + 4 * g + r) * VV + j % VV] = o[j][r];
     __syncthreads();
     const int q = threadIdx.x >> 4, e0 = (threadIdx.x & 15) * VE; // sixteen threads per query
-    if (row0 + q >= row1) return;
+    if (q >= kFewTile || row0 + q >= row1) return;
     float M = kNoScore, L = 0.f, acc[VE];
 #pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) M = fmaxf(M, sm[w * kFewTile + q]);
+    for (int w = 0; w < WAVES; ++w) M = fmaxf(M, sm[w * kFewTile + q]);
 #pragma unroll
     for (int j = 0; j < VE; ++j) acc[j] = 0.f;
 #pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         const float f = __builtin_amdgcn_exp2f(sm[w * kFewTile + q] - M);
         L = fmaf(sl[w * kFewTile + q], f, L);
 #pragma unroll
@@ -663,10 +665,10 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
     }
 }
 
-template <typename T, typename CT, int D>
-__global__ __launch_bounds__(64 * kFewWaves) void k_attn_few(AttnArgs a, int tiles, Cut cut, int max_rows) {
+template <typename T, typename CT, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_attn_few(AttnArgs a, int tiles, Cut cut, int max_rows) {
     extern __shared__ __align__(16) unsigned char lds[];
-    attend_few<T, CT, D>(a, tiles, cut, max_rows, blockIdx.x, reinterpret_cast<float *>(lds));
+    attend_few<T, CT, D, WAVES>(a, tiles, cut, max_rows, blockIdx.x, reinterpret_cast<float *>(lds));
 }
 template <typename CT, int D>
 __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(AttnArgs a, Cut cut, int few_rows) {
@@ -678,7 +680,7 @@ template <typename CT, int D>
 __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_both(AttnArgs a, int tiles, Cut few, Cut wide, int few_rows, int wide_blocks) {
     extern __shared__ __align__(16) unsigned char lds[];
     if ((int)blockIdx.x < wide_blocks) attend_wide<CT, D>(a, wide, few_rows, false, blockIdx.x, lds);
-    else attend_few<bf16, CT, D>(a, tiles, few, few_rows, blockIdx.x - wide_blocks, reinterpret_cast<float *>(lds));
+    else attend_few<bf16, CT, D, kFewWaves>(a, tiles, few, few_rows, blockIdx.x - wide_blocks, reinterpret_cast<float *>(lds));
 }
 
 // Joins the splits of a row (token and head).  ALL: a wave for each row, of either kind; else of the sequences that attend_few takes, where there are no others.
@@ -739,7 +741,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, Cut few, Cut wide
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], m);
     }
-    if (WHOLE) {
+    if constexpr (WHOLE) {
         if (lane < LPR) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) part[wave][e0 + j] = acc[j];
@@ -763,8 +765,8 @@ constexpr int kFewMost = 32;
 constexpr int kMostSplits = 128;
 constexpr int kUncut = 640 * 128;
 
-// per_seq: most rows of a sequence and key/value head that attend_few has; tiles: its tiles of them (0: there is none); slots: row tiles of attend_wide
-struct Plan { int few_rows, per_seq, tiles, slots; Cut few, wide; };
+// waves: of a workgroup of attend_few; per_seq: most rows of a sequence and key/value head that attend_few has; tiles: its tiles of them (0: there is none); slots: row tiles of attend_wide
+struct Plan { int few_rows, per_seq, tiles, slots, waves; Cut few, wide; };
 
 // `range` keys at most, in `blocks` workgroups without a cut: as many splits as make up to `want` workgroups, each of `least` keys or more.
 Cut cut_keys(long range, long blocks, long want, long least, int step) {
@@ -803,12 +805,18 @@ Plan plan_attn(int dtype, int d, const AttnArgs &a) {
     const long full = rows / kWideRows;
     p.wide = p.slots ? cut_keys(range(wide_keys(d)), (full > 0 ? full : 1) * a.r.Hkv, d > 128 ? 256 : d > 64 ? 512 : 768, 512, wide_keys(d)) : Cut{1, 64};
     // A second launch for the join and the splits' way through memory cost 4 to 5 us, a walk 1 us for each 128 keys of d = 128: contexts up to kUncut / d are not cut
-    // (one token over 300 keys, d = 128: 7.5 us instead of 10.5; over 500, 8.8 instead of 10.6; over 1000 it would take 13.0 instead of 11.0), and never into more
+    // (one token over 300 keys, d = 128: 7.5 us instead of 10.5; over 500, 8.9 instead of 10.6; over 1000 it would take 13.0 instead of 11.0), and never into more
     // than 64 (32768 keys, e4m3, 4 heads: 15.1 us, in 128 pieces 16.4).  Beside chunks, whose walks take longer per key, no finer than twice as long as those, and not at
     // all where those are not: the join would cost more than it brought.  (Most of these sequences are single tokens: one tile.)
     const long seen = range(kFewKeys), blocks = (N > 0 ? N : 1) * (p.slots ? 1 : p.tiles) * a.r.Hkv, uncut = kUncut / (dtype == 0 ? 2 * d : d);
-    const long least = p.slots ? (p.wide.splits == 1 ? seen : 2l * p.wide.keys) : seen <= (uncut < 1024 ? uncut : 1024) ? seen : 256;
-    p.few = p.tiles ? cut_keys(seen, blocks, 64 * blocks < 512 ? 64 * blocks : 512, least > 256 ? least : 256, kFewWaves * kFewKeys) : Cut{1, 128};
+    const long least = !p.slots ? (seen <= uncut ? seen : 256) : p.wide.splits == 1 ? seen : 2l * p.wide.keys;
+    // Workgroups of eight waves, one per CU: a CU has more loads under way and rounds end closer together (12 x 16 heads over 1000 keys, d = 128: 18.9 us instead of 23.8; 2 x 2 of 64
+    // in e4m3, 7.6 instead of 9.6; 32 x 16 over up to 2048, 72.8 instead of 75.2), except where two of four waves fit a CU and one round takes all of them (20 x 16 equal contexts of 1500 e4m3
+    // keys: 30.7 us instead of 35.2).
+    const bool twice = !p.slots && (dtype == 0 ? few_twice<float>(d) : few_twice<bf16>(d)) && (blocks <= 256 || blocks >= 512) && seen > kFewWaves * kFewKeys;
+    p.waves = twice ? 2 * kFewWaves : kFewWaves;
+    const long want = twice ? 256 : 512;
+    p.few = p.tiles ? cut_keys(seen, blocks, 64 * blocks < want ? 64 * blocks : want, least > 256 ? least : 256, kFewKeys * p.waves) : Cut{1, 128};
     return p;
 }
 
@@ -833,12 +841,15 @@ int launch(const char *name, const void *fn, long blocks, int threads, int lds, 
 template <typename T, typename CT, int D> int launch_attn(int dtype, AttnArgs a, hipStream_t stream) {
     Plan p = plan_attn(dtype, D, a);
     a.splits = most_splits(p);
-    constexpr int few_lds = kFewWaves * kFewTile * (D + 4 + 2) * 4;
+    const int few_lds = p.waves * kFewTile * (D + 4 + 2) * 4;
     const long few_blocks = p.tiles ? ((long)a.c.N * p.tiles + 1) * p.few.splits * a.r.Hkv : 0;
     int e = 0;
     if (p.slots == 0) {
         void *args[] = {&a, &p.tiles, &p.few, &p.few_rows};
-        e = launch("k_attn_few", reinterpret_cast<const void *>(k_attn_few<T, CT, D>), few_blocks, 64 * kFewWaves, few_lds, args, stream);
+        const void *fn = reinterpret_cast<const void *>(k_attn_few<T, CT, D, kFewWaves>);
+        if constexpr (few_twice<T>(D))
+            if (p.waves != kFewWaves) fn = reinterpret_cast<const void *>(k_attn_few<T, CT, D, 2 * kFewWaves>);
+        e = launch("k_attn_few", fn, few_blocks, 64 * p.waves, few_lds, args, stream);
     }
     if constexpr (sizeof(T) == 2)
         if (p.slots) {

@@ -93,6 +93,15 @@ def test_sharp_and_flat_scores():
     _run(b, 2, "flat")
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("qs,kvs,Hq,Hkv,window", [([128], [128], 4, 2, 0), ([257], [257], 1, 1, 0), ([300], [1000], 2, 1, 0), ([130, 130, 130], [130, 777, 4000], 4, 2, 0),
+                                                  ([64], [3333], 8, 2, 0), ([300], [900], 2, 2, 1), ([300], [900], 2, 2, 40), ([512, 512], [512, 1500], 1, 1, 333), ([1000], [1001], 3, 1, 64),
+                                                  ([256, 256], [256, 200], 1, 1, 0)])
+def test_equal_chunks_of_many_rows(qs, kvs, Hq, Hkv, window, d):
+    b = Batch(qs, kvs, Hkv, d, "bf16", "bf16", 32, seed=d + len(qs))
+    _run(b, Hq, "chunks", window=window, max_q=max(qs), max_kv=max(max(kvs), 1))
+
+
 @pytest.mark.parametrize("dtype,cache,d", [("bf16", "bf16", 64), ("bf16", "bf16", 256), ("bf16", "fp8", 128), ("f32", "f32", 64)])
 def test_what_the_windows_left_behind_reaches_no_result(dtype, cache, d):
     """places in front of a sequence's windows may belong to other sequences by now, or hold nothing that was ever written"""
