@@ -72,7 +72,8 @@ __device__ inline void partial_of(const AttnArgs &a, int split, long row, int D,
 // the products want them: for S^T lane l holds a quarter of the elements of key l % 16 of each half, every fourth 16-byte piece from l / 16 on; for O^T it
 // holds a sixteenth of the elements of the eight keys whose probabilities it has, one 16-byte piece (or less) of each 16, from l % 16 on, which a 16-bit
 // transposition among its own registers turns into the operands of D / 16 products.  (So the lanes of one load stand side by side.)  No LDS traffic and no barrier until the waves of a workgroup, which share out the
-// keys of one split, join their sums.
+// keys of one split, join their sums.  32 sequences of 16 heads of 128 over up to 2048 keys in bf16 (374 MB): 72 us, 5.2 TB/s; one over 32768 e4m3 keys of 4 heads (34 MB):
+// 11 us and 4 for the join.
 constexpr int kFewTile = 16, kFewKeys = 32, kFewWaves = 4;
 // Twice as many waves per workgroup where there are few workgroups, if their registers allow it.
 template <typename T> constexpr bool few_twice(int d) { return d * sizeof(T) <= 256; }
@@ -345,9 +346,11 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
 
 // --- Many rows: prompts and long chunks.
 //
-// Bound by the matrix cores.  A workgroup has 128 rows, 32 per wave, and walks over its keys 64 at a time: K and V travel through
-// registers (8-bit pages become bf16 on the way, exactly) into one of two LDS buffers while the other is worked on, so that a tile costs one
-// barrier.  Rows of a tile are not padded: their 16-byte pieces are permuted by an XOR with the row, which spreads both the row
+// Bound by the matrix cores and the vector ALU (softmax) one after the other: prompts of 4 x 2048 tokens, 16 heads of 128, 90 us (763 TFLOP/s of the 1195 of a large matrix
+// product); 512 tokens of 16 heads (4 of keys) behind 15872, 77 us and 10 for the join, the matrix pipes busy for 0.37 of it, the vector ALU for 0.47, the LDS for 0.2: the two waves of a SIMD
+// overlap little, and without the requests, the exponentials or half of the products it would still take 90 % (80 %).  A workgroup has 128
+// rows, 32 per wave, and walks over its keys 64 at a time: K and V travel straight, 8-bit pages through registers (they become bf16 on the way, exactly), into one of two LDS buffers while the other
+// is worked on, so that a tile costs one barrier.  Rows of a tile are not padded: their 16-byte pieces are permuted by an XOR with the row, which spreads both the row
 // reads (K) and the transposing reads (V, four rows at a time) over the banks.
 constexpr int kWideRows = 128, kWideWaves = 4;
 // keys of a tile (at d = 256 twice as many would need more registers than there are)
@@ -520,7 +523,7 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
                 for (int x = 0; x < NX; ++x) kf[x][i] = *reinterpret_cast<const bf16x8 *>(buf + (32 * x + col) * W::ROWB + (((2 * i + h) ^ W::swizzle(col)) << 4));
-            __builtin_amdgcn_s_setprio(1); // (over the other workgroup's softmax: prompts of 4 x 2048 tokens 97 -> 93 us)
+            __builtin_amdgcn_s_setprio(1); // (over the other workgroup's softmax: a chunk of 512 behind 15872 keys 88.6 -> 85.2 us)
             __builtin_amdgcn_sched_barrier(0);
             constexpr int EVERY = D / 16 / W::NL;
 #pragma unroll
@@ -582,6 +585,7 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
         const int i = lane & 15;
         const int sw[2] = {W::swizzle((i >> 2) + 4 * h), W::swizzle((i >> 2) + 4 * h + 8)};
         const int c0 = ((lane & 16) >> 3) + ((i & 3) >> 1);
+        if constexpr (FP8) __builtin_amdgcn_s_setprio(1); // (mixed batch, d = 64: 42.3 -> 39.6 us; with 16-bit pages a chunk behind 15872 keys 85.2 -> 88.7)
 #pragma unroll
         for (int x = 0; x < NX; ++x) {
             if constexpr (FP8) {
@@ -675,7 +679,8 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(
     extern __shared__ __align__(16) unsigned char lds[];
     attend_wide<CT, D>(a, cut, few_rows, true, blockIdx.x, lds);
 }
-// Chunks beside single tokens: both kinds of workgroup in one launch, the long ones first, so that the short ones, which wait for memory, run under them.
+// Chunks beside single tokens: both kinds of workgroup in one launch, the long ones first, so that the short ones, which wait for memory, run under them.  12 chunks of up to 256 tokens
+// and 12 single ones, 32 heads (8 of keys) of 64, e4m3, window 1024: 41 us, bound by the vector ALU (the softmax and the factors of K and V, 1600 clocks a tile against 512 of products).
 template <typename CT, int D>
 __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_both(AttnArgs a, int tiles, Cut few, Cut wide, int few_rows, int wide_blocks) {
     extern __shared__ __align__(16) unsigned char lds[];
@@ -683,7 +688,7 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_both(
     else attend_few<bf16, CT, D, kFewWaves>(a, tiles, few, few_rows, blockIdx.x - wide_blocks, reinterpret_cast<float *>(lds));
 }
 
-// Joins the splits of a row (token and head).  ALL: a wave for each row, of either kind; else of the sequences that attend_few takes, where there are no others.
+// Joins the splits of a row (token and head): 8192 rows of 128 in eight pieces (36 MB) 10 us, 16 rows in 64 pieces 4 us.  ALL: a wave for each row, of either kind; else of the sequences that attend_few takes, where there are no others.
 // WHOLE: a workgroup per row, for few rows with many splits (16 rows of 128, 64 splits: a wave per row took 17 us, one load after the other).
 template <typename T, int D, bool ALL, bool WHOLE>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, Cut few, Cut wide, int few_rows, int per_seq) {
