@@ -71,11 +71,11 @@ template <typename T, int V> __device__ inline void load_weight(const void *w, i
     }
 }
 
-// Waves of the workgroup that has all of a tensor's gradient to itself, and the steps (of kRowBatch) per wave and the bytes of the tensor up to which it has.  It saves
-// a launch, 3.6 us of the host's; forward and backward of 16 tokens of 16 heads of 128 (64 KB) take 15.0 us instead of 18.9, of 128 tokens of 2 heads
-// of 64 in fp32 (8 steps) 16.0 instead of 19.2; of 60 tokens of 16 heads (245 KB) they would take 21.8 instead of 19.0, of 250 of 2 (16 steps) 20.7 instead of 19.0.
-constexpr int kAloneWaves = 16, kAloneSteps = 8;
-constexpr long kAloneBytes = 64 * 1024;
+// Waves of the workgroup that has all of a tensor's gradient to itself, its steps (of a wave's rows) under way together, and the rounds of those and the bytes of the tensor up to
+// which it has.  It saves a launch, 3.6 us of the host's: forward and backward of 256 tokens of 2 heads of 64 in fp32 (4 rounds, 128 KB) take 14.7 us instead of 18.0, of 16 tokens of 16 heads of
+// 128 in bf16 15.5 instead of 18.9; of 2000 tokens of one head of 64 (8 rounds) they would take 27.9 instead of 18.5, of 60 of 16 heads of 128 (245 KB) 25.1 instead of 17.9.
+constexpr int kAloneWaves = 16, kAloneBatch = 2, kAloneRounds = 4;
+constexpr long kAloneBytes = 128 * 1024;
 
 // Loads of up to this many steps (64 / lanes of a row heads each) are requested before the first is worked on.
 constexpr int kRowBatch = 4;
@@ -152,13 +152,37 @@ __global__ __launch_bounds__(256) void k_norm_rope_fwd(RowArgs a) {
     }
 }
 
-// Rows' gradients: 403 MB for the same tokens in 78 us, 5.2 TB/s.  The norm is formed again from x, which has to be read anyway.  Every workgroup also leaves its sum of dz * xhat,
-// which k_weight_grad adds up in the workgroups' order (atomics would change the result from run to run); 512 workgroups, so that their sums are few.  A workgroup that is alone with its
-// tensor (kAloneWaves waves, few tokens) stores the weight's gradient itself.
-template <typename T, int D, bool IL, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void k_norm_rope_bwd(RowArgs a) {
+// dx of a row, and its dz * xhat added to dw if it is one.
+template <typename T, int D, bool IL>
+__device__ __forceinline__ void row_gradient(const RowArgs &a, const Turn<RowLayout<T, D>::V, IL> &turn, const float (&w)[RowLayout<T, D>::V], const uint4 &x, const uint4 &g, bool is_row,
+                                             float (&dw)[RowLayout<T, D>::V], float (&dx)[RowLayout<T, D>::V]) {
     using L = RowLayout<T, D>;
-    __shared__ float part[WAVES][D];
+    float xf[L::V], own[L::V], oth[L::V], ss = 0.f, gx = 0.f;
+    unpack16<T>(x, xf);
+    unpack16<T>(g, own);
+    turn.template others<T>(g, own, oth);
+#pragma unroll
+    for (int i = 0; i < L::V; ++i) {
+        ss = fmaf(xf[i], xf[i], ss);
+        own[i] = fmaf(own[i], turn.c[i], -oth[i] * turn.s[i]); // dz
+        gx = fmaf(own[i] * w[i], xf[i], gx);
+    }
+    const float r = rsqrtf(lanes_sum<L::LPR>(ss) * (1.f / D) + a.eps);
+    const float m = lanes_sum<L::LPR>(gx) * r * (1.f / D);
+#pragma unroll
+    for (int i = 0; i < L::V; ++i) {
+        const float xh = xf[i] * r;
+        if (is_row) dw[i] = fmaf(own[i], xh, dw[i]);
+        dx[i] = r * fmaf(-xh, m, own[i] * w[i]);
+    }
+}
+
+// Rows' gradients: 403 MB for the same tokens in 78 us, 5.2 TB/s.  The norm is formed again from x, which has to be read anyway.  Every workgroup also leaves its sum of dz * xhat,
+// which k_weight_grad adds up in the workgroups' order (atomics would change the result from run to run); 512 workgroups, so that their sums are few.
+template <typename T, int D, bool IL>
+__global__ __launch_bounds__(256) void k_norm_rope_bwd(RowArgs a) {
+    using L = RowLayout<T, D>;
+    __shared__ float part[4][D];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e0 = (lane % L::LPR) * L::V, sub = lane / L::LPR;
     const bool is_q = blockIdx.y == 0;
     const int H = is_q ? a.Hq : a.Hkv;
@@ -170,7 +194,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_norm_rope_bwd(RowArgs a) {
 #pragma unroll
     for (int i = 0; i < L::V; ++i) dw[i] = 0.f;
     Turn<L::V, IL> turn;
-    for (int t = blockIdx.x * WAVES + wave; t < a.T; t += gridDim.x * WAVES) {
+    for (int t = blockIdx.x * 4 + wave; t < a.T; t += gridDim.x * 4) {
         const T *row = in + t * stride, *dy = grad + (long)t * H * D;
         T *to = out + (long)t * H * D;
         turn.load(a, e0, turn.row_of(a, a.positions ? a.positions[t] : t % a.seq_len));
@@ -186,32 +210,14 @@ __global__ __launch_bounds__(64 * WAVES) void k_norm_rope_bwd(RowArgs a) {
             for (int b = 0; b < kRowBatch; ++b) {
                 if (h0 + b * L::RPW >= H) break;
                 const int h = h0 + b * L::RPW + sub;
-                float xf[L::V], own[L::V], oth[L::V], ss = 0.f, gx = 0.f;
-                unpack16<T>(x[b], xf);
-                unpack16<T>(g[b], own);
-                turn.template others<T>(g[b], own, oth);
-#pragma unroll
-                for (int i = 0; i < L::V; ++i) {
-                    ss = fmaf(xf[i], xf[i], ss);
-                    own[i] = fmaf(own[i], turn.c[i], -oth[i] * turn.s[i]); // dz
-                    gx = fmaf(own[i] * w[i], xf[i], gx);
-                }
-                const float r = rsqrtf(lanes_sum<L::LPR>(ss) * (1.f / D) + a.eps);
-                const float m = lanes_sum<L::LPR>(gx) * r * (1.f / D);
-#pragma unroll
-                for (int i = 0; i < L::V; ++i) {
-                    const float xh = xf[i] * r;
-                    if (h < H) dw[i] = fmaf(own[i], xh, dw[i]);
-                    own[i] = r * fmaf(-xh, m, own[i] * w[i]);
-                }
-                if (h < H) *reinterpret_cast<uint4 *>(to + h * D + e0) = pack16<T>(own);
+                float dx[L::V];
+                row_gradient<T, D, IL>(a, turn, w, x[b], g[b], h < H, dw, dx);
+                if (h < H) *reinterpret_cast<uint4 *>(to + h * D + e0) = pack16<T>(dx);
             }
         }
     }
-    constexpr bool ALONE = WAVES == kAloneWaves;
-    float *to = is_q ? a.dqw : a.dkw;
-    if (ALONE ? !to : !a.partial) return;
-    // the wave's rows side by side, then the waves
+    if (!a.partial) return;
+    // the wave's rows side by side, then the four waves
 #pragma unroll
     for (int i = 0; i < L::V; ++i) {
 #pragma unroll
@@ -219,12 +225,58 @@ __global__ __launch_bounds__(64 * WAVES) void k_norm_rope_bwd(RowArgs a) {
         if (sub == 0) part[wave][e0 + i] = dw[i];
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < D; e += 64 * WAVES) {
+    for (int e = threadIdx.x; e < D; e += 256)
+        a.partial[((long)blockIdx.x * 2 + blockIdx.y) * D + e] = (part[0][e] + part[1][e]) + (part[2][e] + part[3][e]);
+}
+
+// The same for few tokens, a workgroup per tensor (blockIdx.x), which so has the weight's gradient, too.  Rows (token and head) stand side by side in a wave, whatever
+// the number of heads.
+template <typename T, int D, bool IL>
+__global__ __launch_bounds__(64 * kAloneWaves) void k_norm_rope_bwd_alone(RowArgs a) {
+    using L = RowLayout<T, D>;
+    __shared__ float part[kAloneWaves][D];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e0 = (lane % L::LPR) * L::V, sub = lane / L::LPR;
+    const bool is_q = blockIdx.x == 0;
+    const int H = is_q ? a.Hq : a.Hkv, rows = a.T * H;
+    const long stride = is_q ? a.q_stride : a.k_stride;
+    const T *in = static_cast<const T *>(is_q ? a.q : a.k), *grad = static_cast<const T *>(is_q ? a.dq_out : a.dk_out);
+    T *out = static_cast<T *>(is_q ? a.q_out : a.k_out);
+    float w[L::V], dw[L::V];
+    load_weight<T>(is_q ? a.qw : a.kw, e0, w);
+#pragma unroll
+    for (int i = 0; i < L::V; ++i) dw[i] = 0.f;
+    for (int r0 = wave * kAloneBatch * L::RPW; r0 < rows; r0 += kAloneWaves * kAloneBatch * L::RPW) {
+        uint4 x[kAloneBatch], g[kAloneBatch];
+        Turn<L::V, IL> turn[kAloneBatch];
+#pragma unroll
+        for (int b = 0; b < kAloneBatch; ++b) {
+            const int r = min(r0 + b * L::RPW + sub, rows - 1), t = r / H;
+            x[b] = *reinterpret_cast<const uint4 *>(in + t * stride + (r - t * H) * D + e0);
+            g[b] = *reinterpret_cast<const uint4 *>(grad + (long)r * D + e0);
+            turn[b].load(a, e0, turn[b].row_of(a, a.positions ? a.positions[t] : t % a.seq_len));
+        }
+#pragma unroll
+        for (int b = 0; b < kAloneBatch; ++b) {
+            const int r = r0 + b * L::RPW + sub;
+            float dx[L::V];
+            row_gradient<T, D, IL>(a, turn[b], w, x[b], g[b], r < rows, dw, dx);
+            if (r < rows) *reinterpret_cast<uint4 *>(out + (long)r * D + e0) = pack16<T>(dx);
+        }
+    }
+    float *to = is_q ? a.dqw : a.dkw;
+    if (!to) return;
+#pragma unroll
+    for (int i = 0; i < L::V; ++i) {
+#pragma unroll
+        for (int m = L::LPR; m < 64; m <<= 1) dw[i] += __shfl_xor(dw[i], m);
+        if (sub == 0) part[wave][e0 + i] = dw[i];
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < D; e += 64 * kAloneWaves) {
         float s = 0.f;
 #pragma unroll
-        for (int i = 0; i < WAVES; ++i) s += part[i][e];
-        if (ALONE) to[e] = s;
-        else a.partial[((long)blockIdx.x * 2 + blockIdx.y) * D + e] = s;
+        for (int i = 0; i < kAloneWaves; ++i) s += part[i][e];
+        to[e] = s;
     }
 }
 
@@ -469,18 +521,18 @@ struct BwdLaunch {
     RowArgs a;
     hipStream_t stream;
     template <typename T, int D, bool IL> static const void *of(bool alone) {
-        return alone ? reinterpret_cast<const void *>(k_norm_rope_bwd<T, D, IL, kAloneWaves>) : reinterpret_cast<const void *>(k_norm_rope_bwd<T, D, IL, 4>);
+        return alone ? reinterpret_cast<const void *>(k_norm_rope_bwd_alone<T, D, IL>) : reinterpret_cast<const void *>(k_norm_rope_bwd<T, D, IL>);
     }
     template <typename T, int D> int operator()() {
         using L = RowLayout<T, D>;
         int blocks = norm_rope_bwd_blocks(a.T), d = D;
         const int H = a.Hq > a.Hkv ? a.Hq : a.Hkv;
-        const long steps = (long)((a.T + kAloneWaves - 1) / kAloneWaves) * ((H + kRowBatch * L::RPW - 1) / (kRowBatch * L::RPW));
-        const bool alone = a.T > 0 && steps <= kAloneSteps && (long)a.T * H * D * (long)sizeof(T) <= kAloneBytes && (a.dqw || a.dkw);
+        const long rows = (long)a.T * H, round = kAloneWaves * kAloneBatch * L::RPW;
+        const bool alone = a.T > 0 && rows <= kAloneRounds * round && rows * D * (long)sizeof(T) <= kAloneBytes && (a.dqw || a.dkw);
         if (a.T > 0) {
             void *args[] = {&a};
             const void *fn = a.interleaved ? of<T, D, true>(alone) : of<T, D, false>(alone);
-            const int e = launch("k_norm_rope_bwd", fn, dim3(alone ? 1 : blocks, 2), args, stream, alone ? 64 * kAloneWaves : 256);
+            const int e = alone ? launch("k_norm_rope_bwd", fn, dim3(2), args, stream, 64 * kAloneWaves) : launch("k_norm_rope_bwd", fn, dim3(blocks, 2), args, stream);
             if (e || alone) return e;
         }
         if (!a.dqw && !a.dkw) return 0;
