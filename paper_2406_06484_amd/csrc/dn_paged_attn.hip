@@ -724,7 +724,17 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, Cut few, Cut wide
     const int live = hi > lo ? min((hi - lo + cut.keys - 1) / cut.keys, cut.splits) : 0;
     const long row = (long)(s.r0 + r / G) * a.r.Hq + kvh * G + r % G;
     const int in = WHOLE ? threadIdx.x : lane, e0 = in % LPR * 4, side = in / LPR;
+    // the first pieces are on their way while the maximum is found
+    constexpr int AHEAD = 4;
     float *ml, *po;
+    float2 wl[AHEAD];
+    f32x4 w[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+        partial_of(a, min(side + u * SIDE, max(live - 1, 0)), row, D, &ml, &po);
+        wl[u] = *reinterpret_cast<const float2 *>(ml);
+        w[u] = *reinterpret_cast<const f32x4 *>(po + e0);
+    }
     float M = kNoScore;
     for (int i = lane; i < live; i += 64) {
         partial_of(a, i, row, D, &ml, &po);
@@ -733,8 +743,15 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, Cut few, Cut wide
     M = lanes_max<64>(M);
     float L = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+        if (side + u * SIDE < live) {
+            const float f = __builtin_amdgcn_exp2f(wl[u].x - M);
+            L = fmaf(wl[u].y, f, L);
+            acc += w[u] * f;
+        }
 #pragma unroll 4
-    for (int i = side; i < live; i += SIDE) {
+    for (int i = side + AHEAD * SIDE; i < live; i += SIDE) {
         partial_of(a, i, row, D, &ml, &po);
         const float f = __builtin_amdgcn_exp2f(ml[0] - M);
         L = fmaf(ml[1], f, L);
