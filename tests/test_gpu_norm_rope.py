@@ -54,6 +54,28 @@ def test_head_sizes_types_and_pairs(dtype, d, inter):
     _check(q, k, w, dy, ref.rope_table(64, d), None, 1e-6, inter, dtype, "d %d" % d)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [32, 64, 128, 256])
+@pytest.mark.parametrize("inter", [False, True])
+def test_more_tokens_than_one_workgroup_takes(dtype, d, inter):
+    q, k, w, dy, _ = _inputs(701, 6, 3, d, dtype, d + 1)
+    _check(q, k, w, dy, ref.rope_table(701, d), None, 1e-6, inter, dtype, "d %d" % d)
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,d", [(9, 3, 1, 128), (64, 8, 8, 64), (128, 4, 2, 64), (500, 1, 1, 64), (33, 7, 1, 256)])
+def test_few_tokens_in_place_and_with_one_weight(T, Hq, Hkv, d):
+    q, k, w, dy, _ = _inputs(T, Hq, Hkv, d, "bf16", T)
+    rope, pos = ref.rope_table(T, d), torch.arange(T).flip(0)
+    _check(q, k, w, dy, rope, pos, 1e-6, False, "bf16", "both weights")
+    _check(q, k, [w[0], None], dy, rope, pos, 1e-6, False, "bf16", "q's weight")
+    _check(q, k, [None, w[1]], dy, rope, pos, 1e-6, True, "bf16", "k's weight")
+    want = dn.deltanet_qk_norm_rope_bwd(q, k, *dy, *w, rope.cuda())
+    a, b = (t.clone() for t in dy)
+    got = dn.deltanet_qk_norm_rope_bwd(q, k, a, b, *w, rope.cuda(), dq=a, dk=b)
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+
+
 @pytest.mark.parametrize("T,Hq,Hkv,d,rot", [(1, 1, 1, 64, 64), (1, 16, 16, 128, 64), (3, 5, 1, 128, 16), (4, 33, 11, 64, 48), (2050, 4, 2, 128, 128), (301, 2, 2, 256, 112),
                                             (65, 7, 7, 32, 32), (9, 3, 1, 64, 0)])
 def test_sizes_and_partial_rotations(T, Hq, Hkv, d, rot):
