@@ -433,51 +433,53 @@ __global__ __launch_bounds__(256) void k_paged_append(RowArgs a, PagedArgs c, in
     }
 }
 
-// Tokens read back: blockIdx.y = 0: k, 1: v; a.T rows of output, c.cu their offsets.  8192 tokens of 4 heads of 128 from e4m3 pages (27 MB, just written): 8 us; a search
-// of three loads in a row, then one step of loads and stores.
+// Tokens read back: a.T rows of output, c.cu their offsets.  A wave takes up to `per` steps (kReadSteps at most) of one token's k and v: finding the token's place, three loads in a row, is
+// most of its time.  8192 tokens of 4 heads of 128 from e4m3 pages (27 MB, just written): 7 us.
+constexpr int kReadSteps = 4;
 template <typename T, typename CT, int D>
-__global__ __launch_bounds__(256) void k_paged_read(RowArgs a, PagedArgs c) {
+__global__ __launch_bounds__(256) void k_paged_read(RowArgs a, PagedArgs c, int per) {
     using L = RowLayout<T, D>;
     const int lane = threadIdx.x & 63, e0 = (lane % L::LPR) * L::V, sub = lane / L::LPR;
     const int t = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (t >= a.T) return;
-    const bool is_k = blockIdx.y == 0;
-    const void *pages = is_k ? c.kp : c.vp;
-    const float *scale = is_k ? c.ks : c.vs;
-    T *to = static_cast<T *>(is_k ? a.k_out : a.v_out) + (long)t * a.Hkv * D;
+    const int skv = (a.Hkv + L::RPW - 1) / L::RPW; // steps: those of k, then v
+    const int first = blockIdx.y * per, last = min(first + per, 2 * skv);
     const int n = seq_of_row(c.cu, c.N, t);
     Slot s{0, 0};
     const bool live = n < c.N && slot_of(c, n, min(c.kv_len[n], c.max_kv) - c.cu[n + 1] + t, a.Hkv, true, &s);
-    for (int h0 = 0; h0 < a.Hkv; h0 += kRowBatch * L::RPW) {
-        uint4 x[kRowBatch];
-        float f[kRowBatch];
+    uint4 x[kReadSteps];
+    float f[kReadSteps];
 #pragma unroll
-        for (int b = 0; b < kRowBatch; ++b) {
-            const int h = h0 + b * L::RPW + sub;
-            const long row = s.base + (long)h * s.stride;
-            x[b] = make_uint4(0, 0, 0, 0);
-            f[b] = 0.f;
-            if (live && h < a.Hkv) {
-                if constexpr (__is_same(CT, fp8)) {
-                    const uint2 w = *reinterpret_cast<const uint2 *>(static_cast<const unsigned char *>(pages) + row * D + e0);
-                    x[b].x = w.x; x[b].y = w.y;
-                    f[b] = scale[row];
-                } else x[b] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(pages) + row * D + e0);
-            }
-        }
-#pragma unroll
-        for (int b = 0; b < kRowBatch; ++b) {
-            if (h0 + b * L::RPW >= a.Hkv) break;
-            const int h = h0 + b * L::RPW + sub;
+    for (int b = 0; b < kReadSteps; ++b) {
+        const int at = first + b;
+        const bool is_k = at < skv;
+        const int h = (is_k ? at : at - skv) * L::RPW + sub;
+        const long row = s.base + (long)h * s.stride;
+        const void *pages = is_k ? c.kp : c.vp;
+        x[b] = make_uint4(0, 0, 0, 0);
+        f[b] = 0.f;
+        if (live && at < last && h < a.Hkv) {
             if constexpr (__is_same(CT, fp8)) {
-                float y[8];
-                from_fp8x8(make_uint2(x[b].x, x[b].y), y);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] *= f[b];
-                x[b] = pack16<T>(y);
-            }
-            if (h < a.Hkv) *reinterpret_cast<uint4 *>(to + h * D + e0) = x[b];
+                const uint2 w = *reinterpret_cast<const uint2 *>(static_cast<const unsigned char *>(pages) + row * D + e0);
+                x[b].x = w.x; x[b].y = w.y;
+                f[b] = (is_k ? c.ks : c.vs)[row];
+            } else x[b] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(pages) + row * D + e0);
         }
+    }
+#pragma unroll
+    for (int b = 0; b < kReadSteps; ++b) {
+        const int at = first + b;
+        if (at >= last) break;
+        const bool is_k = at < skv;
+        const int h = (is_k ? at : at - skv) * L::RPW + sub;
+        if constexpr (__is_same(CT, fp8)) {
+            float y[8];
+            from_fp8x8(make_uint2(x[b].x, x[b].y), y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] *= f[b];
+            x[b] = pack16<T>(y);
+        }
+        if (h < a.Hkv) *reinterpret_cast<uint4 *>(static_cast<T *>(is_k ? a.k_out : a.v_out) + ((long)t * a.Hkv + h) * D + e0) = x[b];
     }
 }
 
@@ -540,11 +542,11 @@ struct BwdLaunch {
         return launch("k_weight_grad", reinterpret_cast<const void *>(k_weight_grad), dim3(D / 16, 2), args, stream, 1024);
     }
 };
-// Steps of k_paged_append per wave: all of a token's, in equal parts of at most kAppendSteps; one where there are few tokens.
-template <typename T, int D> int steps_per_wave(int tokens, int Hq, int Hkv, int *waves) {
+// Steps of k_paged_append and k_paged_read per wave: all of a token's, in equal parts of at most `most`; one where there are few tokens.
+template <typename T, int D> int steps_per_wave(int tokens, int Hq, int Hkv, int most, int *waves) {
     constexpr int RPW = RowLayout<T, D>::RPW;
     const int all = (Hq + RPW - 1) / RPW + 2 * ((Hkv + RPW - 1) / RPW);
-    const int parts = tokens < 512 ? all : (all + kAppendSteps - 1) / kAppendSteps, per = (all + parts - 1) / parts;
+    const int parts = tokens < 512 ? all : (all + most - 1) / most, per = (all + parts - 1) / parts;
     *waves = (all + per - 1) / per;
     return per;
 }
@@ -558,7 +560,7 @@ struct AppendLaunch {
         return a.interleaved ? reinterpret_cast<const void *>(k_paged_append<T, CT, D, true, true>) : reinterpret_cast<const void *>(k_paged_append<T, CT, D, true, false>);
     }
     template <typename T, int D> int operator()() {
-        int waves, per = steps_per_wave<T, D>(a.T, norm ? a.Hq : 0, a.Hkv, &waves);
+        int waves, per = steps_per_wave<T, D>(a.T, norm ? a.Hq : 0, a.Hkv, kAppendSteps, &waves);
         void *args[] = {&a, &c, &per};
         const void *fn = of<T, D, T>();
         if constexpr (sizeof(T) == 2)
@@ -572,11 +574,15 @@ struct ReadLaunch {
     bool fp8_pages;
     hipStream_t stream;
     template <typename T, int D> int operator()() {
-        void *args[] = {&a, &c};
+        // Two waves per token, or one where k and v are a step each: 16384 tokens of 2 heads of 64 read back (with a small append) in 12.4 us instead of 15.0; of 8 heads
+        // of 128 by one wave 29.0 instead of 28.0.
+        const int skv = (a.Hkv + RowLayout<T, D>::RPW - 1) / RowLayout<T, D>::RPW;
+        int waves, per = steps_per_wave<T, D>(a.T, 0, a.Hkv, skv < 2 ? 2 : skv < kReadSteps ? skv : kReadSteps, &waves);
+        void *args[] = {&a, &c, &per};
         const void *fn = reinterpret_cast<const void *>(k_paged_read<T, T, D>);
         if constexpr (sizeof(T) == 2)
             if (fp8_pages) fn = reinterpret_cast<const void *>(k_paged_read<T, fp8, D>);
-        return launch("k_paged_read", fn, dim3((a.T + 3) / 4, 2), args, stream);
+        return launch("k_paged_read", fn, dim3((a.T + 3) / 4, waves), args, stream);
     }
 };
 
