@@ -281,7 +281,8 @@ int deltanet_qk_norm_rope_bwd(const dn_qk_shape *shape, const dn_rope *rope, con
  * 2^-100 is held as zeros, factor 0; one with an infinity reads back as NaN).  page_size is 16, 32, 64, 128 or 256.
  * Sequence n of the batch has kv_len[n] tokens in the cache, the new ones of this step included; its token p stands in page
  * page_table[n][p / page_size], slot p % page_size (entries past its last page are not read).  Its new tokens are rows
- * cu_q[n] .. cu_q[n + 1] - 1 of the packed tensors, the last of them at position kv_len[n] - 1.
+ * cu_q[n] .. cu_q[n + 1] - 1 of the packed tensors, the last of them at position kv_len[n] - 1.  Rows in front of cu_q[0] and from cu_q[num_seqs] on
+ * lie in no sequence (the arrays may be a part of a larger batch's).
  * These arrays live on the device and are not validated: kernels work on contexts held inside [0, max_kv] and on the rows that
  * lie in the tensors, drop writes to pages outside [0, num_pages) and read page 0 or num_pages - 1 in the place of such ones,
  * so that a malformed array gives meaningless results but no access outside the buffers.
@@ -300,7 +301,7 @@ typedef struct {
 
 typedef struct { void *k_pages, *v_pages; float *k_scale, *v_scale; } dn_paged_cache; /* scales: NULL unless DN_FP8 */
 
-/* Writes the new tokens' k and v to the cache.  Rows whose position is negative (a context shorter than the chunk) are not
+/* Writes the new tokens' k and v to the cache.  Rows whose position is negative (a context shorter than the chunk) and rows in no sequence are not
  * written.  q_stride, max_q and Hq are not used. d as for the attention below. */
 int deltanet_paged_append(const dn_paged_shape *shape, const void *k, const void *v, const dn_paged_cache *cache,
                           void *hip_stream);

@@ -65,9 +65,9 @@ template <int N> __device__ inline float lanes_sum(float x) { return lanes_join<
 template <int N> __device__ inline float lanes_max(float x) { return lanes_join<N>(x, [](float a, float b) { return fmaxf(a, b); }); }
 
 // The sequence that packed row t lies in: the number of n in [0, N) with cu[n + 1] <= t, by 64-way probes of the whole wave (t
-// is the wave's).  Returns N for a row past the last sequence; always in [0, N], whatever the array holds.
+// is the wave's).  Returns N for a row in front of the first sequence or past the last one; always in [0, N], whatever the array holds.
 __device__ inline int seq_of_row(const int32_t *cu, int N, int t) {
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, first = N > 0 ? cu[0] : 0; // (fetched beside the first probes)
     int lo = 0, hi = N; // the answer lies in [lo, hi]
     while (lo < hi) {
         const int step = (hi - lo + 63) >> 6, at = lo + lane * step; // probe lane asks whether the answer is over `at`
@@ -77,7 +77,7 @@ __device__ inline int seq_of_row(const int32_t *cu, int N, int t) {
         lo = min(hi, lo + (c - 1) * step + 1);
         if (c < 64) hi = min(hi, lo - 1 + step);
     }
-    return __builtin_amdgcn_readfirstlane(lo);
+    return __builtin_amdgcn_readfirstlane(t < first ? N : lo);
 }
 
 } // namespace dn

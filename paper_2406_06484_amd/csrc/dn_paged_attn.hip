@@ -45,12 +45,12 @@ __device__ inline long row_of(const PagedArgs &c, int page, int kk, int kvh, int
     return (((long)page * Hkv + kvh) << c.page_shift) + (kk & ((1 << c.page_shift) - 1));
 }
 
-// Zeroes the outputs of rows that lie in no sequence.
+// Zeroes the outputs of rows that lie in no sequence: those in front of the first one and those past the last one.
 template <typename T, int D> __device__ inline void zero_rest(const AttnArgs &a, int kvh, int G) {
-    const int from = min(max(a.c.N ? a.c.cu[a.c.N] : 0, 0), a.r.T);
+    const int front = a.c.N ? min(max(a.c.cu[0], 0), a.r.T) : 0, from = a.c.N ? min(max(a.c.cu[a.c.N], front), a.r.T) : 0;
     constexpr int W = D * (int)sizeof(T) / 16; // words of a row
-    for (long i = threadIdx.x; i < (long)(a.r.T - from) * G * W; i += blockDim.x) {
-        const long row = (from + i / (G * W)) * a.r.Hq + kvh * G + i / W % G;
+    for (long i = threadIdx.x; i < (long)(front + a.r.T - from) * G * W; i += blockDim.x) {
+        const long t = i / (G * W), row = (t < front ? t : from + t - front) * a.r.Hq + kvh * G + i / W % G;
         reinterpret_cast<uint4 *>(a.r.q_out)[row * W + i % W] = make_uint4(0, 0, 0, 0);
     }
 }
