@@ -283,7 +283,7 @@ int deltanet_qk_norm_rope_bwd(const dn_qk_shape *shape, const dn_rope *rope, con
  * page_table[n][p / page_size], slot p % page_size (entries past its last page are not read).  Its new tokens are rows
  * cu_q[n] .. cu_q[n + 1] - 1 of the packed tensors, the last of them at position kv_len[n] - 1.  Rows in front of cu_q[0] and from cu_q[num_seqs] on
  * lie in no sequence (the arrays may be a part of a larger batch's).
- * These arrays live on the device and are not validated: kernels work on contexts held inside [0, max_kv] and on the rows that
+ * These arrays live on the device and are not validated: kernels work on the first max_kv tokens of longer contexts (whose rows keep their positions) and on the rows that
  * lie in the tensors, drop writes to pages outside [0, num_pages) and read page 0 or num_pages - 1 in the place of such ones,
  * so that a malformed array gives meaningless results but no access outside the buffers.
  */
@@ -301,8 +301,8 @@ typedef struct {
 
 typedef struct { void *k_pages, *v_pages; float *k_scale, *v_scale; } dn_paged_cache; /* scales: NULL unless DN_FP8 */
 
-/* Writes the new tokens' k and v to the cache.  Rows whose position is negative (a context shorter than the chunk) and rows in no sequence are not
- * written.  q_stride, max_q and Hq are not used. d as for the attention below. */
+/* Writes the new tokens' k and v to the cache.  Rows whose position is negative (a context shorter than the chunk) or for which there is no room (max_kv and
+ * more), and rows in no sequence, are not written.  q_stride, max_q and Hq are not used. d as for the attention below. */
 int deltanet_paged_append(const dn_paged_shape *shape, const void *k, const void *v, const dn_paged_cache *cache,
                           void *hip_stream);
 
@@ -313,7 +313,7 @@ int deltanet_paged_norm_rope_append(const dn_paged_shape *shape, const dn_rope *
                                     void *q_out, const dn_paged_cache *cache, void *hip_stream);
 
 /* Reads tokens back: rows cu_out[n] .. cu_out[n + 1] - 1 of k_out, v_out [T_out, Hkv, d] (element type dtype) become the last ones of
- * sequence n's context (all of it, if that many).  A row in front of the context's start, or in no sequence, becomes zero. */
+ * sequence n's context (all of it, if that many).  A row in front of the context's start, past max_kv, or in no sequence, becomes zero. */
 int deltanet_paged_read(const dn_paged_shape *shape, const dn_paged_cache *cache, const int32_t *cu_out, int32_t T_out,
                         void *k_out, void *v_out, void *hip_stream);
 

@@ -299,12 +299,16 @@ __global__ __launch_bounds__(1024) void k_weight_grad(RowArgs a, int D, int bloc
     }
 }
 
-// Where the wave's packed row t stands in the cache; false for a row that is not written.
+// The position of the wave's packed row t of sequence n, counted back from the context's end whether or not the table has room for all of it.
+__device__ inline int position_of(const PagedArgs &c, int n, int t) {
+    const long pos = (long)c.kv_len[n] - c.cu[n + 1] + t;
+    return (int)(pos < -1 ? -1 : pos > 0x7fffffff ? 0x7fffffff : pos);
+}
+// Where it stands in the cache; false for a row that has no place there.
 struct Slot { long base; int stride; }; // of head 0, in rows of d elements; rows between heads
 __device__ inline bool slot_of(const PagedArgs &c, int n, int pos, int Hkv, bool clamp, Slot *s) {
-    const int page = pos >> c.page_shift;
-    if (pos < 0 || page >= c.max_pages) return false;
-    int id = c.table[(long)n * c.max_pages + page];
+    if (pos < 0 || pos >= c.max_kv) return false; // (max_kv tokens need max_pages pages at most)
+    int id = c.table[(long)n * c.max_pages + (pos >> c.page_shift)];
     if (clamp) id = min(max(id, 0), c.num_pages - 1);
     else if (id < 0 || id >= c.num_pages) return false;
     s->base = (((long)id * Hkv) << c.page_shift) + (pos & ((1 << c.page_shift) - 1));
@@ -386,7 +390,7 @@ __global__ __launch_bounds__(256) void k_paged_append(RowArgs a, PagedArgs c, in
     bool live = false;
     if (t < a.T) n = seq_of_row(c.cu, c.N, t);
     if (n < c.N) {
-        pos = min(c.kv_len[n], c.max_kv) - c.cu[n + 1] + t;
+        pos = position_of(c, n, t);
         live = slot_of(c, n, pos, a.Hkv, false, &s);
     }
     if constexpr (NORM) {
@@ -446,7 +450,7 @@ __global__ __launch_bounds__(256) void k_paged_read(RowArgs a, PagedArgs c, int 
     const int first = blockIdx.y * per, last = min(first + per, 2 * skv);
     const int n = seq_of_row(c.cu, c.N, t);
     Slot s{0, 0};
-    const bool live = n < c.N && slot_of(c, n, min(c.kv_len[n], c.max_kv) - c.cu[n + 1] + t, a.Hkv, true, &s);
+    const bool live = n < c.N && slot_of(c, n, position_of(c, n, t), a.Hkv, true, &s);
     uint4 x[kReadSteps];
     float f[kReadSteps];
 #pragma unroll

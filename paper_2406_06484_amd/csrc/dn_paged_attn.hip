@@ -16,23 +16,25 @@ struct Cut { int splits, keys; };
 
 constexpr float kNoScore = -1e30f; // the running maximum before the first key: finite, so that differences are never NaN
 
-// The rows of sequence n and its context, held inside the tensors whatever the arrays say.
+// The rows of sequence n, its context, held inside the tensors whatever the arrays say, and the position of its first row (tokens that the table has no room
+// for have theirs behind the context's end, and move nobody's).
 struct SeqRows {
-    int r0, r1, kv;
+    int r0, r1, kv, before;
     __device__ inline void load(const AttnArgs &a, int n) {
         r0 = min(max(a.c.cu[n], 0), a.r.T);
         r1 = min(max(a.c.cu[n + 1], r0), a.r.T);
-        kv = min(max(a.c.kv_len[n], 0), a.c.max_kv);
+        const int len = max(a.c.kv_len[n], 0);
+        kv = min(len, a.c.max_kv);
+        before = len - (r1 - r0);
     }
 };
 
 // The keys that rows [row0, row1) of a sequence see between them: [from, hi); lo is `from` rounded down to a multiple of `step`.  Values outside, which a
 // window may have left to other sequences, enter no product, whatever stands there.
 __device__ inline void key_range(const AttnArgs &a, const SeqRows &s, int G, int row0, int row1, int step, int &lo, int &from, int &hi) {
-    const int before = s.kv - (s.r1 - s.r0); // position of the first new token
-    hi = max(before + (row1 - 1) / G + 1, 0);
-    const int first = max(before + row0 / G, 0);
-    from = a.window > 0 ? max(first - a.window + 1, 0) : 0;
+    hi = min(max(s.before + (row1 - 1) / G + 1, 0), s.kv);
+    const int first = max(s.before + row0 / G, 0);
+    from = a.window > 0 ? min(max(first - a.window + 1, 0), hi) : 0;
     lo = from / step * step;
 }
 
@@ -135,9 +137,9 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
     if (splits > 1 && k_begin >= k_end) return; // (the rows' other splits know)
     const bool valid = row0 + col < row1;
     const int tok = (valid ? row0 + col : row0) / G, head = kvh * G + (valid ? row0 + col : row0) % G;
-    const int before = s.kv - (s.r1 - s.r0), p = before + tok;              // the lane's query's position
-    const int p_lo = a.window > 0 ? p - a.window + 1 : 0;                   // first key it sees
-    const int all_from = a.window > 0 ? before + (row1 - 1) / G - a.window + 1 : 0, all_to = before + row0 / G; // keys in [all_from, all_to] are seen by every row
+    const int pos = s.before + tok, p = min(pos, s.kv - 1);                 // the lane's query's position, and the last key it sees
+    const int p_lo = a.window > 0 ? pos - a.window + 1 : 0;                 // the first one
+    const int all_from = a.window > 0 ? s.before + (row1 - 1) / G - a.window + 1 : 0, all_to = min(s.before + row0 / G, s.kv - 1); // keys in [all_from, all_to] are seen by every row
 
     // the query, in the same order as a key
     unsigned qw[KE * sizeof(T) / 4];
@@ -437,13 +439,13 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
     key_range(a, s, G, row0, row1, KEYS, lo, from, hi);
     const int k_begin = lo + split * split_keys, k_end = min(hi, k_begin + split_keys);
     if (splits > 1 && k_begin >= k_end) return; // (the rows' other splits know)
-    const int wrow = row0 + 32 * wave, before = s.kv - (s.r1 - s.r0);
+    const int wrow = row0 + 32 * wave;
     const int row = min(wrow + col, row1 - 1), tok = row / G, head = kvh * G + row % G;
-    const int p = before + tok, p_lo = a.window > 0 ? p - a.window + 1 : 0;   // the lane's query's position, and the first key it sees
+    const int pos = s.before + tok, p = min(pos, s.kv - 1), p_lo = a.window > 0 ? pos - a.window + 1 : 0; // the lane's query's position, the last and the first key it sees
     // keys that some row, that every row of the wave sees
-    const int last = before + (min(wrow + 32, row1) - 1) / G, first = before + min(wrow, row1 - 1) / G;
-    const int some_from = a.window > 0 ? first - a.window + 1 : 0, some_to = wrow < row1 ? last : -1;
-    const int all_from = a.window > 0 ? last - a.window + 1 : 0, all_to = first;
+    const int last = s.before + (min(wrow + 32, row1) - 1) / G, first = s.before + min(wrow, row1 - 1) / G;
+    const int some_from = a.window > 0 ? first - a.window + 1 : 0, some_to = wrow < row1 ? min(last, s.kv - 1) : -1;
+    const int all_from = a.window > 0 ? last - a.window + 1 : 0, all_to = min(first, s.kv - 1);
     const float c = a.scale * 1.4426950408889634f;
 
     bf16x8 q[D / 16];
