@@ -323,7 +323,7 @@ int deltanet_paged_read(const dn_paged_shape *shape, const dn_paged_cache *cache
  *     o = sum_j exp(scale q . k_j) v_j / sum_j exp(scale q . k_j) ,   max(0, p - window + 1) <= j <= p
  *
  * (window = 0: the whole past).  A row without a position in its context (p < 0), or in no sequence, becomes zero.  Scores, the running maximum and sum and the output
- * are held in fp32; in bf16 the probabilities, multiplied by the cache's factors, enter the product with v as bf16 (in chunks of many rows
+ * are held in fp32, and scores of any size that fp32 holds are told apart (a row all of whose scores are -infinity becomes zero); in bf16 the probabilities, multiplied by the cache's factors, enter the product with v as bf16 (in chunks of many rows
  * rounded, for few rows as two terms).  scale > 0.  Nothing at or past kv_len, nor before the windows of all of a sequence's new tokens, reaches a
  * result, whatever the pages hold there (values that one new token sees and another does not are given the weight zero in the other's row: an
  * infinity or NaN among THOSE may reach both).  Deterministic: the order of every sum depends on the sizes and lengths alone.

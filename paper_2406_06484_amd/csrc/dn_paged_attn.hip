@@ -1,10 +1,11 @@
 // Attention of new tokens over the paged cache.  The rows of a sequence that read one key/value head, q_len tokens times
 // G = Hq / Hkv query heads, are taken together (row = token * G + head), so that each key and value is fetched once for all of them.
-// Softmax runs over the keys in one pass with the running maximum m and sum l per row (in powers of two, the scale folded in):
+// Softmax runs over the keys in one pass with the running maximum m and sum l per row (in powers of two, c = scale / log 2):
 //
-//     m' = max(m, max_j s_j) ,  l' = l 2^(m - m') + sum_j 2^(s_j - m') ,  o' = o 2^(m - m') + sum_j 2^(s_j - m') v_j
+//     m' = max(m, max_j s_j) ,  l' = l 2^(c (m - m')) + sum_j 2^(c (s_j - m')) ,  o' = o 2^(c (m - m')) + sum_j 2^(c (s_j - m')) v_j
 //
-// and splits of the key axis are joined by the same formula.  All products run transposed, S^T = K Q^T and O^T = V^T P^T: the
+// (m is a score, not its multiple: s_j - m is right to its last bits however large both are, where c s_j less a rounded c m may be off by more than the
+// exponential's range) and splits of the key axis are joined by the same formula.  All products run transposed, S^T = K Q^T and O^T = V^T P^T: the
 // matrix cores leave S^T with a lane's values all in one row (the lane's query) and at the keys that P^T's operand wants from
 // that lane, so that P never leaves its registers.
 #include "dn_attn_device.hpp"
@@ -14,7 +15,8 @@ namespace dn {
 // How the key axis is cut: `splits` pieces of `keys` keys from the first that a row tile sees.
 struct Cut { int splits, keys; };
 
-constexpr float kNoScore = -1e30f; // the running maximum before the first key: finite, so that differences are never NaN
+constexpr float kNoScore = -3.4028235e38f; // the running maximum before the first key: finite, so that differences are never NaN, and under every other score
+constexpr float kLog2e = 1.4426950408889634f;
 
 // The rows of sequence n, its context, held inside the tensors whatever the arrays say, and the position of its first row (tokens that the table has no room
 // for have theirs behind the context's end, and move nobody's).
@@ -152,7 +154,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
             qw[4 * i] = x.x; qw[4 * i + 1] = x.y; qw[4 * i + 2] = x.z; qw[4 * i + 3] = x.w;
         }
     }
-    const float c = a.scale * 1.4426950408889634f;
+    const float c = a.scale * kLog2e;
 
     const char *kp = static_cast<const char *>(a.c.kp), *vp = static_cast<const char *>(a.c.vp);
     unsigned kw[2][KW], vw[8][VW];
@@ -229,9 +231,9 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
             const auto y = __builtin_amdgcn_permlane32_swap(v, v, false, false);
             mt = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
         }
-        const float mn = fmaxf(m, mt * c);
+        const float mn = fmaxf(m, mt);
         if (__any(mn > m)) {
-            const float f = __builtin_amdgcn_exp2f(m - mn);
+            const float f = __builtin_amdgcn_exp2f((m - mn) * c);
             l *= f;
 #pragma unroll
             for (int j = 0; j < VE; ++j) o[j] *= f;
@@ -241,7 +243,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { st[h][i] = __builtin_amdgcn_exp2f(fmaf(st[h][i], c, -m)); sum += st[h][i]; }
+            for (int i = 0; i < 4; ++i) { st[h][i] = __builtin_amdgcn_exp2f((st[h][i] - m) * c); sum += st[h][i]; }
         l += sum;
         if (k0 + kFewKeys > hi || k0 < from) { // what no row sees enters no result
 #pragma unroll
@@ -326,7 +328,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
     for (int j = 0; j < VE; ++j) acc[j] = 0.f;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-        const float f = __builtin_amdgcn_exp2f(sm[w * kFewTile + q] - M);
+        const float f = __builtin_amdgcn_exp2f((sm[w * kFewTile + q] - M) * c);
         L = fmaf(sl[w * kFewTile + q], f, L);
 #pragma unroll
         for (int j = 0; j < VE; ++j) acc[j] = fmaf(so[(w * kFewTile + q) * LD + e0 + j], f, acc[j]);
@@ -355,6 +357,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
 // is worked on, so that a tile costs one barrier.  Rows of a tile are not padded: their 16-byte pieces are permuted by an XOR with the row, which spreads both the row
 // reads (K) and the transposing reads (V, four rows at a time) over the banks.
 constexpr int kWideRows = 128, kWideWaves = 4;
+constexpr float kFarScore = 0x1p20f; // (a number of this size is rounded by 2^-4 at most)
 // keys of a tile (at d = 256 twice as many would need more registers than there are)
 constexpr int wide_keys(int d) { return d > 128 ? 32 : 64; }
 
@@ -446,7 +449,7 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
     const int last = s.before + (min(wrow + 32, row1) - 1) / G, first = s.before + min(wrow, row1 - 1) / G;
     const int some_from = a.window > 0 ? first - a.window + 1 : 0, some_to = wrow < row1 ? min(last, s.kv - 1) : -1;
     const int all_from = a.window > 0 ? last - a.window + 1 : 0, all_to = min(first, s.kv - 1);
-    const float c = a.scale * 1.4426950408889634f;
+    const float c = a.scale * kLog2e;
 
     bf16x8 q[D / 16];
     {
@@ -459,7 +462,12 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
     for (int i = 0; i < NB; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
-    float m = kNoScore, l = 0.f;
+    // A score's exponent is c s - off, one operation, where c m is rounded by a small part of a power of two (the same for all of a row's scores); with a row
+    // whose scores are larger, the wave subtracts m first.  (off is finite also before the first key: masked scores are -infinity.)
+    float m = kNoScore, l = 0.f, off;
+    bool far;
+    auto set_off = [&]() __attribute__((always_inline)) { off = fmaxf(m * c, kNoScore); far = __any(m > kNoScore && fabsf(off) > kFarScore); };
+    set_off();
 
     // this thread's pieces of a tile on their way (8-bit pages; 16-bit ones go straight to the LDS)
     u32x4 rk[W::NL], rv[W::NL];
@@ -565,22 +573,30 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
         {
             const unsigned u = __float_as_uint(mt);
             const auto x = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-            mt = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) * c;
+            mt = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
         }
         // m need not be the maximum, only near it: sums are rescaled when a row's has grown by 2^8 or more
-        if (__any(mt > m + 8.f)) {
-            const float mn = fmaxf(m, mt), f = __builtin_amdgcn_exp2f(m - mn);
+        if (__any((mt - m) * c > 8.f)) {
+            const float mn = fmaxf(m, mt), f = __builtin_amdgcn_exp2f((m - mn) * c);
             l *= f;
 #pragma unroll
             for (int i = 0; i < NB; ++i) o[i] *= f;
             m = mn;
+            set_off();
         }
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        float sub = off, sum[4] = {0.f, 0.f, 0.f, 0.f};
+        if (far) {
+#pragma unroll
+            for (int x = 0; x < NX; ++x)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) st[x][r] -= m;
+            sub = 0.f;
+        }
 #pragma unroll
         for (int x = 0; x < NX; ++x)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                st[x][r] = __builtin_amdgcn_exp2f(fmaf(st[x][r], c, -m));
+                st[x][r] = __builtin_amdgcn_exp2f(fmaf(st[x][r], c, -sub));
                 sum[r & 3] += st[x][r];
             }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
@@ -743,19 +759,20 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, Cut few, Cut wide
         M = fmaxf(M, ml[0]);
     }
     M = lanes_max<64>(M);
+    const float c = a.scale * kLog2e;
     float L = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
         if (side + u * SIDE < live) {
-            const float f = __builtin_amdgcn_exp2f(wl[u].x - M);
+            const float f = __builtin_amdgcn_exp2f((wl[u].x - M) * c);
             L = fmaf(wl[u].y, f, L);
             acc += w[u] * f;
         }
 #pragma unroll 4
     for (int i = side + AHEAD * SIDE; i < live; i += SIDE) {
         partial_of(a, i, row, D, &ml, &po);
-        const float f = __builtin_amdgcn_exp2f(ml[0] - M);
+        const float f = __builtin_amdgcn_exp2f((ml[0] - M) * c);
         L = fmaf(ml[1], f, L);
         acc += *reinterpret_cast<const f32x4 *>(po + e0) * f;
     }
