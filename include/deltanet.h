@@ -251,7 +251,7 @@ typedef struct {
 } dn_rope;
 
 typedef struct {
-    int32_t T, Hq, Hkv, d;
+    int32_t T, Hq, Hkv, d;               /* T <= 2^30, T * Hq < 2^31 */
     int32_t dtype;                       /* DN_F32 or DN_BF16 */
     int32_t seq_len;                     /* without a positions array: row t has position t % seq_len */
     int64_t q_stride, k_stride;          /* elements between rows of q and k */
@@ -292,7 +292,7 @@ typedef struct {
     int32_t Hq, Hkv, d;
     int32_t dtype, cache_dtype;
     int32_t page_size, num_pages, max_pages; /* max_pages: columns of page_table */
-    int32_t max_q, max_kv;               /* no sequence has more new tokens or a longer context (bounds suffice); T, max_kv <= 2^30 */
+    int32_t max_q, max_kv;               /* no sequence has more new tokens or a longer context (bounds suffice); T, max_kv <= 2^30, T * Hq < 2^31 */
     const int32_t *cu_q;                 /* DEVICE int32 [num_seqs + 1] */
     const int32_t *kv_len;               /* DEVICE int32 [num_seqs] */
     const int32_t *page_table;           /* DEVICE int32 [num_seqs, max_pages] */
@@ -313,7 +313,7 @@ int deltanet_paged_norm_rope_append(const dn_paged_shape *shape, const dn_rope *
                                     void *q_out, const dn_paged_cache *cache, void *hip_stream);
 
 /* Reads tokens back: rows cu_out[n] .. cu_out[n + 1] - 1 of k_out, v_out [T_out, Hkv, d] (element type dtype) become the last ones of
- * sequence n's context (all of it, if that many).  A row in front of the context's start, past max_kv, or in no sequence, becomes zero. */
+ * sequence n's context (all of it, if that many); T_out <= 2^30, T_out * Hkv < 2^31.  A row in front of the context's start, past max_kv, or in no sequence, becomes zero. */
 int deltanet_paged_read(const dn_paged_shape *shape, const dn_paged_cache *cache, const int32_t *cu_out, int32_t T_out,
                         void *k_out, void *v_out, void *hip_stream);
 

@@ -9,7 +9,7 @@ namespace {
 
 using namespace dn;
 
-constexpr int kMostTokens = 1 << 30;
+constexpr int kMostTokens = 1 << 30; // 32-bit positions and rows, and some tiles or strides past the last
 
 bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 int elem_bytes(int dtype) { return dtype == DN_BF16 ? 2 : 4; }
@@ -21,7 +21,7 @@ int check_rows(int64_t stride, int H, int d, int es) {
 }
 
 int check_heads(int T, int Hq, int Hkv, int dtype) {
-    if (T < 0 || Hq <= 0 || Hkv <= 0 || Hq > 8192 || Hkv > Hq || Hq % Hkv) return DN_ERR_SHAPE;
+    if (T < 0 || T > kMostTokens || Hq <= 0 || Hkv <= 0 || Hq > 8192 || Hkv > Hq || Hq % Hkv) return DN_ERR_SHAPE;
     if ((long long)T * Hq >= (1ll << 31)) return DN_ERR_SHAPE; // 32-bit indices of rows and heads
     return dtype == DN_F32 || dtype == DN_BF16 ? DN_OK : DN_ERR_UNSUPPORTED;
 }
@@ -52,7 +52,7 @@ int check_paged(const dn_paged_shape *s) {
     if (ps != 16 && ps != 32 && ps != 64 && ps != 128 && ps != 256) return DN_ERR_UNSUPPORTED;
     if (s->num_seqs < 0 || s->num_seqs > 65535 || s->num_pages < 0 || s->max_pages < 0 || s->max_q < 0 || s->max_kv < 0) return DN_ERR_SHAPE;
     if (s->max_q > s->T || (long long)s->max_kv > (long long)s->max_pages * ps) return DN_ERR_SHAPE;
-    if (s->T > kMostTokens || s->max_kv > kMostTokens) return DN_ERR_SHAPE; // 32-bit positions, and some tiles past the last
+    if (s->max_kv > kMostTokens) return DN_ERR_SHAPE;
     if (s->num_pages == 0 && s->max_kv > 0) return DN_ERR_SHAPE;
     if ((long long)s->Hkv * ps * s->d * elem_bytes(s->dtype) >= (1ll << 30)) return DN_ERR_SHAPE; // a page lies within a buffer descriptor's range
     return DN_OK;
@@ -190,7 +190,7 @@ int deltanet_paged_norm_rope_append(const dn_paged_shape *shape, const dn_rope *
 int deltanet_paged_read(const dn_paged_shape *shape, const dn_paged_cache *cache, const int32_t *cu_out, int32_t T_out, void *k_out,
                         void *v_out, void *hip_stream) {
     if (int rc = check_paged(shape)) return rc;
-    if (T_out < 0 || (long long)T_out * shape->Hkv >= (1ll << 31)) return DN_ERR_SHAPE;
+    if (T_out < 0 || T_out > kMostTokens || (long long)T_out * shape->Hkv >= (1ll << 31)) return DN_ERR_SHAPE;
     if (int rc = check_cache(shape, cache)) return rc;
     if (T_out && (!k_out || !v_out)) return DN_ERR_NULL;
     if (shape->num_seqs && !cu_out) return DN_ERR_NULL;
