@@ -327,7 +327,7 @@ int deltanet_paged_read(const dn_paged_shape *shape, const dn_paged_cache *cache
  * rounded, for few rows as two terms).  scale > 0.  Nothing at or past kv_len, nor before the windows of all of a sequence's new tokens, reaches a
  * result, whatever the pages hold there (values that one new token sees and another does not are given the weight zero in the other's row: an
  * infinity or NaN among THOSE may reach both).  Deterministic: the order of every sum depends on the sizes and lengths alone.
- * Compiled: d = 64, 128, 256 in bf16, with bf16 or DN_FP8 pages; d = 32, 64, 128 in fp32 (the precision mode).
+ * Compiled: d = 64, 128, 256 in bf16, with bf16 or DN_FP8 pages; d = 32, 64, 128 in fp32 (the precision mode; max_q * Hq < 2^26 there).
  * Workspace: deltanet_paged_attn_workspace_bytes (it depends on num_seqs, T, the heads, d, the types, max_q, max_kv and window).
  */
 int deltanet_paged_attn_workspace_bytes(const dn_paged_shape *shape, int32_t window, size_t *out_bytes);

@@ -122,6 +122,7 @@ AttnArgs attn_args(const dn_paged_shape *s, const dn_paged_cache *c, int window)
     a.scale = 0.f;
     a.window = window >= s->max_kv ? 0 : window; // (a window as long as any context hides nothing)
     a.max_q = s->max_q; a.splits = 1;
+    a.zero_front = a.zero_rest = 1;
     a.workspace = nullptr;
     return a;
 }
@@ -207,6 +208,7 @@ int deltanet_paged_attn_workspace_bytes(const dn_paged_shape *shape, int32_t win
     if (!out_bytes) return DN_ERR_NULL;
     if (int rc = check_paged(shape)) return rc;
     if (window < 0) return DN_ERR_SHAPE;
+    if (shape->dtype == DN_F32 && (long long)shape->max_q * shape->Hq >= (1ll << 26)) return DN_ERR_SHAPE; // a sequence's tiles of 16 rows are one launch's
     const dn_paged_cache none = {nullptr, nullptr, nullptr, nullptr};
     *out_bytes = paged_attn_workspace(shape->dtype, shape->d, attn_args(shape, &none, window));
     return DN_OK;

@@ -34,6 +34,7 @@ struct AttnArgs {
     float scale;
     int window, max_q;
     int splits;                          // most splits of any row (the workspace's layout)
+    int zero_front, zero_rest;           // whether rows in front of the first sequence, past the last one, are this launch's to zero
     void *workspace;
 };
 

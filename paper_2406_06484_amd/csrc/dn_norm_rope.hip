@@ -358,6 +358,11 @@ __device__ inline void cache_row(const Rows &to, const Rows &scale, int step, in
     } else store16(to, step, pack16<T>(y));
 }
 
+// The workgroup's four tokens; its part of their steps is blockIdx.y.  (A launch of 2^32 threads or more along one dimension of its grid is cut to the low 32 bits
+// without an error, so workgroups past kGridRow stand in further rows.)
+constexpr int kGridRowShift = 22, kGridRow = 1 << kGridRowShift;
+__device__ inline int token_block() { return (blockIdx.z << kGridRowShift) + blockIdx.x; }
+
 // New tokens: a wave takes up to kAppendSteps steps (a step: as many heads as a wave holds) of one token's q, k and v (q only with NORM, which also
 // normalises and rotates k).  Finding the token's place takes three loads in a row (its sequence, the context's length, the page),
 // and that latency, not the bytes, would be the time: all rows are requested before the search, and what the norm needs waits in the LDS, because a load
@@ -371,7 +376,7 @@ __global__ __launch_bounds__(256) void k_paged_append(RowArgs a, PagedArgs c, in
     __shared__ __align__(16) float turns[NORM ? 4 : 1][NORM ? D : 4];
     __shared__ __align__(16) T weight[NORM ? 2 : 1][NORM ? D : 8];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), e0 = (lane % L::LPR) * L::V, sub = lane / L::LPR;
-    const int t = blockIdx.x * 4 + wave;
+    const int t = token_block() * 4 + wave;
     // steps: those of q, then k, then v
     const int sq = NORM ? (a.Hq + L::RPW - 1) / L::RPW : 0, skv = (a.Hkv + L::RPW - 1) / L::RPW;
     const int first = blockIdx.y * per, last = min(first + per, sq + 2 * skv);
@@ -444,7 +449,7 @@ template <typename T, typename CT, int D>
 __global__ __launch_bounds__(256) void k_paged_read(RowArgs a, PagedArgs c, int per) {
     using L = RowLayout<T, D>;
     const int lane = threadIdx.x & 63, e0 = (lane % L::LPR) * L::V, sub = lane / L::LPR;
-    const int t = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int t = token_block() * 4 + (threadIdx.x >> 6);
     if (t >= a.T) return;
     const int skv = (a.Hkv + L::RPW - 1) / L::RPW; // steps: those of k, then v
     const int first = blockIdx.y * per, last = min(first + per, 2 * skv);
@@ -546,6 +551,11 @@ struct BwdLaunch {
         return launch("k_weight_grad", reinterpret_cast<const void *>(k_weight_grad), dim3(D / 16, 2), args, stream, 1024);
     }
 };
+// The grid of token_block.
+dim3 token_grid(int T, int parts) {
+    const int blocks = (T + 3) / 4;
+    return dim3(blocks < kGridRow ? blocks : kGridRow, parts, (blocks + kGridRow - 1) / kGridRow);
+}
 // Steps of k_paged_append and k_paged_read per wave: all of a token's, in equal parts of at most `most`; one where there are few tokens.
 template <typename T, int D> int steps_per_wave(int tokens, int Hq, int Hkv, int most, int *waves) {
     constexpr int RPW = RowLayout<T, D>::RPW;
@@ -569,7 +579,7 @@ struct AppendLaunch {
         const void *fn = of<T, D, T>();
         if constexpr (sizeof(T) == 2)
             if (fp8_pages) fn = of<T, D, fp8>();
-        return launch("k_paged_append", fn, dim3((a.T + 3) / 4, waves), args, stream);
+        return launch("k_paged_append", fn, token_grid(a.T, waves), args, stream);
     }
 };
 struct ReadLaunch {
@@ -586,7 +596,7 @@ struct ReadLaunch {
         const void *fn = reinterpret_cast<const void *>(k_paged_read<T, T, D>);
         if constexpr (sizeof(T) == 2)
             if (fp8_pages) fn = reinterpret_cast<const void *>(k_paged_read<T, fp8, D>);
-        return launch("k_paged_read", fn, dim3((a.T + 3) / 4, waves), args, stream);
+        return launch("k_paged_read", fn, token_grid(a.T, waves), args, stream);
     }
 };
 

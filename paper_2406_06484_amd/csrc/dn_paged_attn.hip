@@ -51,7 +51,9 @@ __device__ inline long row_of(const PagedArgs &c, int page, int kk, int kvh, int
 
 // Zeroes the outputs of rows that lie in no sequence: those in front of the first one and those past the last one.
 template <typename T, int D> __device__ inline void zero_rest(const AttnArgs &a, int kvh, int G) {
-    const int front = a.c.N ? min(max(a.c.cu[0], 0), a.r.T) : 0, from = a.c.N ? min(max(a.c.cu[a.c.N], front), a.r.T) : 0;
+    int front = a.c.N ? min(max(a.c.cu[0], 0), a.r.T) : 0, from = a.c.N ? min(max(a.c.cu[a.c.N], front), a.r.T) : 0;
+    if (!a.zero_front) front = 0;
+    if (!a.zero_rest) from = a.r.T;
     constexpr int W = D * (int)sizeof(T) / 16; // words of a row
     for (long i = threadIdx.x; i < (long)(front + a.r.T - from) * G * W; i += blockDim.x) {
         const long t = i / (G * W), row = (t < front ? t : from + t - front) * a.r.Hq + kvh * G + i / W % G;
@@ -869,8 +871,10 @@ size_t workspace_of(const AttnArgs &a, int d, const Plan &p) {
     return (((2 * rows + 3) & ~size_t(3)) + rows * d) * sizeof(float);
 }
 
+// Workgroups of a launch: one of 2^32 threads or more is cut to the low 32 bits without an error.
+long most_blocks(int threads) { return ((1l << 32) - 1) / threads; }
 int launch(const char *name, const void *fn, long blocks, int threads, int lds, void **args, hipStream_t stream) {
-    if (blocks >= (1l << 31)) return (int)hipErrorInvalidConfiguration;
+    if (blocks > most_blocks(threads)) return (int)hipErrorInvalidConfiguration;
     if (lds > 64 * 1024)
         if (const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds)) return (int)e;
     prof_begin(name, stream);
@@ -883,8 +887,18 @@ template <typename T, typename CT, int D> int launch_attn(int dtype, AttnArgs a,
     Plan p = plan_attn(dtype, D, a);
     a.splits = most_splits(p);
     const int few_lds = p.waves * kFewTile * (D + 4 + 2) * 4;
-    const long few_blocks = p.tiles ? ((long)a.c.N * p.tiles + 1) * p.few.splits * a.r.Hkv : 0;
+    const long few_blocks = p.tiles ? ((long)a.c.N * p.tiles + 1) * p.few.splits * a.r.Hkv : 0, wide_blocks = (long)p.slots * p.wide.splits * a.r.Hkv;
     int e = 0;
+    if (few_blocks + wide_blocks > most_blocks(64 * p.waves) && a.c.N > 1) {
+        // One half of the sequences after the other.  (So many are not cut more finely by halves: the workspace suffices for each.)
+        AttnArgs b = a;
+        a.c.N /= 2;
+        a.zero_rest = 0;
+        b.c.cu += a.c.N; b.c.kv_len += a.c.N; b.c.table += (long)a.c.N * a.c.max_pages; b.c.N -= a.c.N;
+        b.zero_front = 0;
+        e = launch_attn<T, CT, D>(dtype, a, stream);
+        return e ? e : launch_attn<T, CT, D>(dtype, b, stream);
+    }
     if (p.slots == 0) {
         void *args[] = {&a, &p.tiles, &p.few, &p.few_rows};
         const void *fn = reinterpret_cast<const void *>(k_attn_few<T, CT, D, kFewWaves>);
@@ -894,8 +908,6 @@ template <typename T, typename CT, int D> int launch_attn(int dtype, AttnArgs a,
     }
     if constexpr (sizeof(T) == 2)
         if (p.slots) {
-            const long wide_blocks = (long)p.slots * p.wide.splits * a.r.Hkv;
-            if (wide_blocks >= (1l << 31)) return (int)hipErrorInvalidConfiguration;
             constexpr int wide_lds = 2 * WideTile<CT, D>::SIZE;
             int first = (int)wide_blocks;
             if (p.tiles) {

@@ -24,3 +24,12 @@ def test_the_largest_number_of_rows():
     out = ctypes.c_size_t(0)
     assert lib.deltanet_qk_norm_rope_workspace_bytes(qk_shape(T=MOST, Hq=1, Hkv=1), out) == 0
     assert out.value == 512 * 2 * 64 * 4
+
+
+@pytest.mark.parametrize("max_q,status", [((1 << 20) - 1, 0), (1 << 20, SHAPE)])
+def test_fp32_chunks_of_more_tiles_than_a_launch_has_room_for(max_q, status):
+    _, lib = _lib()
+    s, out = paged(dtype=0, cache_dtype=0, T=1 << 20, Hq=64, max_q=max_q, q_stride=64 * 64), ctypes.c_size_t(0)
+    assert lib.deltanet_paged_attn_workspace_bytes(s, 0, out) == status
+    s.dtype = s.cache_dtype = 1
+    assert lib.deltanet_paged_attn_workspace_bytes(s, 0, out) == 0
