@@ -859,7 +859,7 @@ Plan plan_attn(int dtype, int d, const AttnArgs &a) {
     const bool twice = !p.slots && (dtype == 0 ? few_twice<float>(d) : few_twice<bf16>(d)) && (blocks <= 256 || blocks >= 512) && seen > kFewWaves * kFewKeys;
     p.waves = twice ? 2 * kFewWaves : kFewWaves;
     const long want = twice ? 256 : 512;
-    p.few = p.tiles ? cut_keys(seen, blocks, 64 * blocks < want ? 64 * blocks : want, least > 256 ? least : 256, kFewKeys * p.waves) : Cut{1, 128};
+    p.few = p.per_seq && N ? cut_keys(seen, blocks, 64 * blocks < want ? 64 * blocks : want, least > 256 ? least : 256, kFewKeys * p.waves) : Cut{1, 128};
     return p;
 }
 
