@@ -32,17 +32,32 @@ def _compile(src: str) -> str:
 
 
 def _compile_binding() -> None:
+    """The module for calls with tensors.  It is left out, with a word on stderr, where there is no torch to serve or no host compiler; C callers need
+    neither."""
     import sysconfig
 
-    import torch
+    def left_out(why):
+        if os.path.exists(BINDING):     # (none is better than one of other sources)
+            os.remove(BINDING)
+        sys.stderr.write("_attention.so is not built: no %s\n" % why)
+
+    try:
+        import torch
+    except ImportError:
+        return left_out("torch")
     root = os.path.dirname(torch.__file__)
     tmp = BINDING + ".tmp.%d" % os.getpid()
-    r = subprocess.run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
-                        "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
-                        "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "dn_attention_binding.cpp"), "-o", tmp,
-                        "-L" + os.path.join(root, "lib"), "-Wl,-rpath," + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-ldl"],
-                       capture_output=True, text=True)
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+           "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+           "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "dn_attention_binding.cpp"), "-o", tmp,
+           "-L" + os.path.join(root, "lib"), "-Wl,-rpath," + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-ldl"]
+    try:
+        r = subprocess.run(cmd, capture_output=True, text=True)
+    except FileNotFoundError:
+        return left_out("g++")
     if r.returncode != 0:
+        if os.path.exists(BINDING):
+            os.remove(BINDING)
         raise RuntimeError("g++ failed on dn_attention_binding.cpp:\n" + r.stderr)
     if r.stderr.strip():
         sys.stderr.write(r.stderr)
@@ -53,10 +68,10 @@ def build(verbose: bool = True) -> str:
     with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
         binding = ex.submit(_compile_binding)
         objs = list(ex.map(_compile, SOURCES))
-        binding.result()
     tmp = OUT + ".tmp.%d" % os.getpid()
     subprocess.check_call(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs)
     os.replace(tmp, OUT)
+    binding.result()    # (the library is there for C callers by now)
     if verbose:
         print("built", OUT)
     return OUT
