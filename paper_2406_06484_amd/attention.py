@@ -1,6 +1,7 @@
 """Binding of the attention operators of ``libdeltanet_hip.so`` (declared in ``include/deltanet.h``): the norm and rotation of
 queries and keys with its gradient, the paged cache, and attention over it.  Argument marshalling only, as ``binding``; the calls go through the
-compiled module ``_attention`` (csrc/dn_attention_binding.cpp), which checks tensors and allocates what the caller did not bring.  A missing
+compiled module ``_attention`` (csrc/dn_attention_binding.cpp), which checks tensors and allocates what the caller did not bring (the library wants arrays of 16-byte
+alignment: offsets, lengths, tables and positions that are parts of larger ones are copied on the way where they need it).  A missing
 library or module raises; there is no fallback."""
 from __future__ import annotations
 

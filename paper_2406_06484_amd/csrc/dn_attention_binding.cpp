@@ -63,6 +63,13 @@ int64_t rows(const at::Tensor &t, const char *name, at::ScalarType type, int64_t
     return T > 1 ? t.stride(0) : H * d;
 }
 
+// The array of integers in t; one that begins inside a 16-byte word (a part of a larger batch's) as a copy that does not, made on the call's stream.
+const int32_t *ints(const at::Tensor &t, at::Tensor &copy) {
+    if (reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0) return t.data_ptr<int32_t>();
+    copy = t.clone();
+    return copy.data_ptr<int32_t>();
+}
+
 int32_t int32(int64_t v, const char *name) {
     if (v < INT32_MIN || v > INT32_MAX) throw Refusal{PyExc_ValueError, std::string(name) + " does not fit 32 bits"};
     return (int32_t)v;
@@ -144,10 +151,11 @@ at::Tensor flat(const at::Tensor &t, const char *name) {
 }
 
 struct QK {
-    at::Tensor q, k;
+    at::Tensor q, k, copy;
+    const int32_t *positions = nullptr;
     dn_qk_shape s;
     at::ScalarType type;
-    QK(const at::Tensor &q_, const at::Tensor &k_, const at::Tensor *positions) : q(q_), k(k_) {
+    QK(const at::Tensor &q_, const at::Tensor &k_, const at::Tensor *pos) : q(q_), k(k_) {
         s.dtype = type_of(q, "q");
         type = q.scalar_type();
         int64_t seq = q.dim() ? q.size(0) : 0;
@@ -163,13 +171,17 @@ struct QK {
         s.k_stride = rows(k, "k", type, T, k.size(1), d);
         s.T = int32(T, "T"); s.Hq = int32(q.size(1), "heads"); s.Hkv = int32(k.size(1), "heads"); s.d = int32(d, "d");
         s.seq_len = int32(std::max<int64_t>(seq, 1), "L");
-        if (positions) whole(*positions, "positions", at::kInt, {T});
+        if (pos) {
+            whole(*pos, "positions", at::kInt, {T});
+            positions = ints(*pos, copy);
+        }
     }
 };
 
 struct Paged {
     dn_paged_shape s = {};
     dn_paged_cache c = {};
+    at::Tensor copies[3];
     Paged(PyObject *k_pages, PyObject *v_pages, PyObject *page_table, PyObject *kv_len, PyObject *cu, PyObject *k_scale, PyObject *v_scale, int dtype) {
         const at::Tensor &kp = tensor(k_pages, "k_pages"), &vp = tensor(v_pages, "v_pages"), &table = tensor(page_table, "page_table");
         const at::Tensor &lens = tensor(kv_len, "kv_len"), &offsets = tensor(cu, "cu_q"), *ks = maybe(k_scale, "k_scale"), *vs = maybe(v_scale, "v_scale");
@@ -193,7 +205,7 @@ struct Paged {
         s.num_pages = int32(pages, "num_pages"); s.Hkv = int32(H, "heads"); s.page_size = int32(ps, "page_size"); s.d = int32(kp.size(3), "d");
         s.dtype = dtype; s.cache_dtype = quantised ? DN_FP8 : dtype;
         s.max_kv = (int32_t)std::min<int64_t>(table.size(1) * ps, 1 << 30); // (the most that a context may have)
-        s.cu_q = offsets.data_ptr<int32_t>(); s.kv_len = lens.data_ptr<int32_t>(); s.page_table = table.data_ptr<int32_t>();
+        s.cu_q = ints(offsets, copies[0]); s.kv_len = ints(lens, copies[1]); s.page_table = ints(table, copies[2]);
         c.k_pages = kp.data_ptr(); c.v_pages = vp.data_ptr(); c.k_scale = fptr(ks); c.v_scale = fptr(vs);
     }
 };
@@ -225,7 +237,7 @@ PyObject *norm_rope_fwd(Args a) {
     const dn_rope r = rope_of(table, a[6], a[7]);
     weights(qw, kw, x.type, x.s.d);
     const at::Tensor qo = out(maybe(a[8], "q_out"), "q_out", q.sizes(), q, x.type), ko = out(maybe(a[9], "k_out"), "k_out", k.sizes(), q, x.type);
-    const int rc = lib.norm_rope_fwd(&x.s, &r, x.q.data_ptr(), x.k.data_ptr(), ptr(qw), ptr(kw), fptr(table), static_cast<int32_t *>(ptr(pos)), qo.data_ptr(),
+    const int rc = lib.norm_rope_fwd(&x.s, &r, x.q.data_ptr(), x.k.data_ptr(), ptr(qw), ptr(kw), fptr(table), x.positions, qo.data_ptr(),
                                      ko.data_ptr(), stream_of(q));
     return rc ? PyLong_FromLong(rc) : tuple_of({&qo, &ko});
 }
@@ -248,7 +260,7 @@ PyObject *norm_rope_bwd(Args a) {
     int rc = lib.norm_rope_bytes(&x.s, &need);
     if (rc) return PyLong_FromLong(rc);
     const Scratch ws(maybe(a[14], "workspace"), qw || kw ? need : 0, q);
-    rc = lib.norm_rope_bwd(&x.s, &r, x.q.data_ptr(), x.k.data_ptr(), dqo.data_ptr(), dko.data_ptr(), ptr(qw), ptr(kw), fptr(table), static_cast<int32_t *>(ptr(pos)),
+    rc = lib.norm_rope_bwd(&x.s, &r, x.q.data_ptr(), x.k.data_ptr(), dqo.data_ptr(), dko.data_ptr(), ptr(qw), ptr(kw), fptr(table), x.positions,
                            dq.data_ptr(), dk.data_ptr(), qw ? fptr(&dqw) : nullptr, kw ? fptr(&dkw) : nullptr, ws.p(), ws.bytes, stream_of(q));
     return rc ? PyLong_FromLong(rc) : tuple_of({&dq, &dk, qw ? &dqw : nullptr, kw ? &dkw : nullptr});
 }
