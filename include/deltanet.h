@@ -280,7 +280,7 @@ int deltanet_qk_norm_rope_bwd(const dn_qk_shape *shape, const dn_rope *rope, con
  * max |x| / 448 over the row, and the pages the e4m3 numbers nearest to x / factor, divided in fp32 (a row whose largest magnitude is under
  * 2^-100 is held as zeros, factor 0; one with an infinity reads back as NaN).  page_size is 16, 32, 64, 128 or 256.
  * Sequence n of the batch has kv_len[n] tokens in the cache, the new ones of this step included; its token p stands in page
- * page_table[n][p / page_size], slot p % page_size (entries past its last page are not read).  Its new tokens are rows
+ * page_table[n][p / page_size], slot p % page_size (entries past its last page may hold anything).  Its new tokens are rows
  * cu_q[n] .. cu_q[n + 1] - 1 of the packed tensors, the last of them at position kv_len[n] - 1.  Rows in front of cu_q[0] and from cu_q[num_seqs] on
  * lie in no sequence (the arrays may be a part of a larger batch's).
  * These arrays live on the device and are not validated: kernels work on the first max_kv tokens of longer contexts (whose rows keep their positions) and on the rows that
@@ -292,17 +292,18 @@ typedef struct {
     int32_t Hq, Hkv, d;
     int32_t dtype, cache_dtype;
     int32_t page_size, num_pages, max_pages; /* max_pages: columns of page_table */
-    int32_t max_q, max_kv;               /* no sequence has more new tokens or a longer context (bounds suffice); T, max_kv <= 2^30, T * Hq < 2^31 */
+    int32_t max_q, max_kv;               /* bounds: no sequence has more new tokens or a longer context; max_q <= T, max_kv <= max_pages * page_size,
+                                            T and max_kv <= 2^30, T * Hq < 2^31 */
     const int32_t *cu_q;                 /* DEVICE int32 [num_seqs + 1] */
     const int32_t *kv_len;               /* DEVICE int32 [num_seqs] */
     const int32_t *page_table;           /* DEVICE int32 [num_seqs, max_pages] */
     int64_t q_stride, k_stride, v_stride;
-} dn_paged_shape;
+} dn_paged_shape;                        /* every call checks Hq, T and the bounds, used or not, and the strides of the tensors that it has */
 
 typedef struct { void *k_pages, *v_pages; float *k_scale, *v_scale; } dn_paged_cache; /* scales: NULL unless DN_FP8 */
 
 /* Writes the new tokens' k and v to the cache.  Rows whose position is negative (a context shorter than the chunk) or for which there is no room (max_kv and
- * more), and rows in no sequence, are not written.  q_stride, max_q and Hq are not used. d as for the attention below. */
+ * more), and rows in no sequence, are not written.  q_stride is not used, max_q and Hq only checked. d as for the attention below. */
 int deltanet_paged_append(const dn_paged_shape *shape, const void *k, const void *v, const dn_paged_cache *cache,
                           void *hip_stream);
 

@@ -165,7 +165,7 @@ def deltanet_paged_attn_fwd(q, k_pages, v_pages, page_table, kv_len, cu_q, *, k_
                             stream=None) -> "torch.Tensor":
     """Attention of the new tokens q [T, Hq, d] over the paged cache, which holds their own keys and values already; returns o
     [T, Hq, d].  The row at position p sees keys max(0, p - window + 1) .. p (window 0: its whole past); scale is d ** -0.5 by
-    default.  max_q and max_kv: bounds on the longest chunk and the longest context (T and the page table's width by default; close bounds
-    make for better-sized launches)."""
+    default.  max_q and max_kv: bounds on the longest chunk and the longest context, at most T and the tokens that the page table has room for, which they
+    are by default (a constant bound of the caller's is passed as min(bound, T)); close bounds make for better-sized launches."""
     return _call("attn", stream, q, k_pages, v_pages, page_table, kv_len, cu_q, k_scale, v_scale, scale, window, max_q, max_kv, o,
                  workspace)

@@ -33,3 +33,13 @@ def test_fp32_chunks_of_more_tiles_than_a_launch_has_room_for(max_q, status):
     assert lib.deltanet_paged_attn_workspace_bytes(s, 0, out) == status
     s.dtype = s.cache_dtype = 1
     assert lib.deltanet_paged_attn_workspace_bytes(s, 0, out) == 0
+
+
+@pytest.mark.parametrize("field,value", [("Hq", 0), ("Hq", 1), ("Hq", 5), ("T", -1), ("max_q", 9), ("max_kv", 65)])
+def test_every_paged_call_checks_the_heads_and_bounds(field, value):
+    """also where it does not use them, as the header says"""
+    _, lib = _lib()
+    s = paged(**{field: value})
+    assert lib.deltanet_paged_append(s, FAKE, FAKE, cache(), None) == SHAPE
+    assert lib.deltanet_paged_read(s, cache(), FAKE, 8, FAKE, FAKE, None) == SHAPE
+    assert lib.deltanet_paged_attn_workspace_bytes(s, 0, ctypes.c_size_t(0)) == SHAPE
