@@ -71,11 +71,11 @@ template <typename T, int V> __device__ inline void load_weight(const void *w, i
     }
 }
 
-// Waves of the workgroup that has all of a tensor's gradient to itself, its steps (of a wave's rows) under way together, and the rounds of those and the bytes of the tensor up to
-// which it has.  It saves a launch, 3.6 us of the host's: forward and backward of 256 tokens of 2 heads of 64 in fp32 (4 rounds, 128 KB) take 14.7 us instead of 18.0, of 16 tokens of 16 heads of
-// 128 in bf16 15.5 instead of 18.9; of 2000 tokens of one head of 64 (8 rounds) they would take 27.9 instead of 18.5, of 60 of 16 heads of 128 (245 KB) 25.1 instead of 17.9.
-constexpr int kAloneWaves = 16, kAloneBatch = 2, kAloneRounds = 4;
-constexpr long kAloneBytes = 128 * 1024;
+// Waves of the workgroup that has all of a tensor's gradient to itself, its steps (of a wave's rows) under way together, and the elements per lane, in rounds of those, up to
+// which it has: it saves a launch, but has one CU.  Backward alone, by one workgroup per tensor and by two launches, in us: fp32, 2 + 2 heads of 64, three rounds (192 tokens) 8.2 and 10.6,
+// four 9.4 and 10.8, five 11.0 and 10.7, six 12.7 and 10.8; bf16, 16 + 16 heads of 128 (eight elements a lane), one round (8 tokens) 7.8 and 10.5, two 8.2 and 10.5, three 10.6 and 10.4, four 12.9
+// and 10.5; other numbers and sizes of heads within 0.3 of these.
+constexpr int kAloneWaves = 16, kAloneBatch = 2, kAloneElements = 16;
 
 // Loads of up to this many steps (64 / lanes of a row heads each) are requested before the first is worked on.
 constexpr int kRowBatch = 4;
@@ -539,7 +539,7 @@ struct BwdLaunch {
         int blocks = norm_rope_bwd_blocks(a.T), d = D;
         const int H = a.Hq > a.Hkv ? a.Hq : a.Hkv;
         const long rows = (long)a.T * H, round = kAloneWaves * kAloneBatch * L::RPW;
-        const bool alone = a.T > 0 && rows <= kAloneRounds * round && rows * D * (long)sizeof(T) <= kAloneBytes && (a.dqw || a.dkw);
+        const bool alone = a.T > 0 && rows <= kAloneElements / L::V * round && (a.dqw || a.dkw);
         if (a.T > 0) {
             void *args[] = {&a};
             const void *fn = a.interleaved ? of<T, D, true>(alone) : of<T, D, false>(alone);
