@@ -102,6 +102,7 @@ void *stream_of(const at::Tensor &t) {
     if (!h) throw Refusal{nullptr, ""};
     void *s = reinterpret_cast<void *>(PyLong_AsLongLong(h));
     Py_DECREF(h);
+    if (PyErr_Occurred()) throw Refusal{nullptr, ""};
     return s;
 }
 
@@ -129,7 +130,9 @@ struct Scratch {
 };
 
 dn_rope rope_of(const at::Tensor *table, PyObject *eps, PyObject *interleaved) {
-    dn_rope r = {0, PyObject_IsTrue(interleaved) > 0, 0, (float)number(eps, "eps")};
+    const int pairs = PyObject_IsTrue(interleaved);
+    if (pairs < 0) throw Refusal{nullptr, ""}; // (the object's own error)
+    dn_rope r = {0, pairs, 0, (float)number(eps, "eps")};
     if (table) {
         if (table->dim() != 2) throw Refusal{PyExc_ValueError, "rope must be [max_pos, rot], cosines then sines"};
         whole(*table, "rope", at::kFloat, table->sizes());
