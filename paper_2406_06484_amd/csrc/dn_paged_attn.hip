@@ -853,9 +853,11 @@ Plan plan_attn(int dtype, int d, const AttnArgs &a) {
     // all where those are not: the join would cost more than it brought.  (Most of these sequences are single tokens: one tile.)
     const long seen = range(kFewKeys), blocks = (N > 0 ? N : 1) * (p.slots ? 1 : p.tiles) * a.r.Hkv, uncut = kUncut / (dtype == 0 ? 2 * d : d);
     const long least = !p.slots ? (seen <= uncut ? seen : 256) : p.wide.splits == 1 ? seen : 2l * p.wide.keys;
-    // Workgroups of eight waves, one per CU: a CU has more loads under way and rounds end closer together (12 x 16 heads over 1000 keys, d = 128: 18.9 us instead of 23.8; 2 x 2 of 64
-    // in e4m3, 7.6 instead of 9.6; 32 x 16 over up to 2048, 72.8 instead of 75.2), except where two of four waves fit a CU and one round takes all of them (20 x 16 equal contexts of 1500 e4m3
-    // keys: 30.7 us instead of 35.2).
+    // Workgroups of eight waves, one per CU: a CU has more loads under way and rounds end closer together (equal contexts of 1000 keys, d = 128, 256 workgroups: 22.6 us instead of 26.2, e4m3 14.8
+    // instead of 18.1), except between one and two workgroups per CU, where two of four waves are all under way at once (320 of 1000 keys: 31.3 us instead of 33.9, e4m3 19.3 instead of 23.4; 496: 40.5
+    // instead of 40.8, 23.2 instead of 25.7).  At 512, where one round still holds all, equal contexts are 2 and 8 % faster by four waves, ragged ones (a quarter of the longest up, mean of eight
+    // batches) 2 % slower at d = 128 and 5 % faster in e4m3, 3 % faster at d = 64 and 10 % slower in e4m3; at 528 eight waves take 0.98, 1.03, 0.92 of the time of four (16 bits, e4m3, d = 64), at
+    // 640 0.98, 0.96, 0.97.  (Between 256 and 512 ragged batches go either way: at 320 0.89, 0.92, 1.07.)
     const bool twice = !p.slots && (dtype == 0 ? few_twice<float>(d) : few_twice<bf16>(d)) && (blocks <= 256 || blocks >= 512) && seen > kFewWaves * kFewKeys;
     p.waves = twice ? 2 * kFewWaves : kFewWaves;
     const long want = twice ? 256 : 512;
