@@ -241,7 +241,7 @@ int deltanet_gated_bwd_saved(const dn_shape *shape, const void *q, const void *k
  *
  * for the pairs (a, b) among the first `rot` elements; the others stay z.  Pairs are (i, i + rot / 2), or (2i, 2i + 1) if
  * `interleaved`; cos_sin (fp32 [max_pos, rot]) holds for each position the rot / 2 cosines, then the rot / 2 sines, of those
- * pairs' angles.  Arithmetic is fp32; y is rounded once.  Weights have the element type of q and k; a NULL weight is all ones.
+ * pairs' angles.  Arithmetic is fp32 (a row the sum of whose squares is past its range becomes zero); y is rounded once.  Weights have the element type of q and k; a NULL weight is all ones.
  * Positions outside [0, max_pos) read the table's nearest row.
  * Compiled: d = 32, 64, 128, 256 in fp32 and bf16; rot a multiple of 16 up to d, or 0 (no rotation; cos_sin may be NULL).
  */

@@ -367,7 +367,7 @@ __device__ inline int token_block() { return (blockIdx.z << kGridRowShift) + blo
 // normalises and rotates k).  Finding the token's place takes three loads in a row (its sequence, the context's length, the page),
 // and that latency, not the bytes, would be the time: all rows are requested before the search, and what the norm needs waits in the LDS, because a load
 // issued behind the first stores would wait for those.  8192 tokens of 16 + 4 + 4 heads of 128 into e4m3 pages (94 MB): 21 to 22 us, 4.3 TB/s, the vector ALU (norm,
-// rotation, maximum, quotients) busy for half of it; 32 single tokens of 16 + 16 + 16: 4.5 us.
+// rotation, maximum, quotients) busy for 0.37 of it; 32 single tokens of 16 + 16 + 16: 4.5 us.
 constexpr int kAppendSteps = 2;
 template <typename T, typename CT, int D, bool NORM, bool IL>
 __global__ __launch_bounds__(256) void k_paged_append(RowArgs a, PagedArgs c, int per) {

@@ -352,9 +352,9 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
 
 // --- Many rows: prompts and long chunks.
 //
-// Bound by the matrix cores and the vector ALU (softmax) one after the other: prompts of 4 x 2048 tokens, 16 heads of 128, 90 us (763 TFLOP/s of the 1195 of a large matrix
-// product); 512 tokens of 16 heads (4 of keys) behind 15872, 77 us and 10 for the join, the matrix pipes busy for 0.37 of it, the vector ALU for 0.47, the LDS for 0.2: the two waves of a SIMD
-// overlap little, and without the requests, the exponentials or half of the products it would still take 90 % (80 %).  A workgroup has 128
+// Products, softmax, products in turn: prompts of 4 x 2048 tokens, 16 heads of 128, 88 to 91 us (760 TFLOP/s of the 1195 of a large matrix product), the matrix pipes busy for 0.32 of the time, the
+// vector ALU for 0.33 or more (exponentials count as one instruction), the LDS for 0.16; the waves wait for 0.27 of theirs and are ready but not issued for 0.31.  512 tokens of 16 heads (4 of keys)
+// behind 15872, 86 us with the join (10), 0.37, 0.34, 0.19, 0.22, 0.32.  Without the requests, the exponentials or half of the products it would still take 90 % (80 %).  A workgroup has 128
 // rows, 32 per wave, and walks over its keys 64 at a time: K and V travel straight, 8-bit pages through registers (they become bf16 on the way, exactly), into one of two LDS buffers while the other
 // is worked on, so that a tile costs one barrier.  Rows of a tile are not padded: their 16-byte pieces are permuted by an XOR with the row, which spreads both the row
 // reads (K) and the transposing reads (V, four rows at a time) over the banks.
@@ -700,7 +700,8 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(
     attend_wide<CT, D>(a, cut, few_rows, true, blockIdx.x, lds);
 }
 // Chunks beside single tokens: both kinds of workgroup in one launch, the long ones first, so that the short ones, which wait for memory, run under them.  12 chunks of up to 256 tokens
-// and 12 single ones, 32 heads (8 of keys) of 64, e4m3, window 1024: 41 us, bound by the vector ALU (the softmax and the factors of K and V, 1600 clocks a tile against 512 of products).
+// and 12 single ones, 32 heads (8 of keys) of 64, e4m3, window 1024: 39.5 us, the matrix pipes busy for 0.13, the vector ALU for 0.34, the waves waiting for 0.44 of their time: with 8-bit pages at d = 64 and 128 the compiled
+// loop waits for the tile that it has just requested before it takes the first maximum, so that no request is under way under the softmax.
 template <typename CT, int D>
 __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_both(AttnArgs a, int tiles, Cut few, Cut wide, int few_rows, int wide_blocks) {
     extern __shared__ __align__(16) unsigned char lds[];
