@@ -336,6 +336,90 @@ int deltanet_paged_attn_fwd(const dn_paged_shape *shape, const void *q, const dn
                             int32_t window, void *o, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
+ * Around a mixer: the short convolution in front of it, the norm of its output with its gate, and what stands between two blocks.  The conventions at the top hold; rows
+ * may be strided where a stride is given (elements, a multiple of 16 bytes), so that inputs and gradients may be column blocks of a projection's; other tensors are contiguous.
+ * Sums are fp32 and in an order that the sizes alone decide.
+ *
+ * Short convolution.  Causal and per channel, with W taps (2, 3 or 4; the last one meets the present row): with X_t the sequence's rows, in front of its first row those of
+ * initial_state (zeros where there is none),
+ *
+ *     z_t = bias + sum_{j < W} weight_j X_{t-W+1+j} ,    y = z , or SiLU(z) = z sigmoid(z)
+ *
+ * x is dense [B, L, C] or packed [L, C] with cu_seqlens, as q above; weight [C, W], bias [C] or NULL, states [N, W - 1, C] (the last W - 1 rows of X, oldest first, which continue the
+ * sequence in another call), all of type dtype: a state is a copy of rows, not a sum.  The C channels are one to three parts (q, k and v side by side in a projection's output, say), each
+ * with an output of its own, [.., width] contiguous, and activated or not.  cu_seqlens_host is optional and validated if given; without it rows that lie in no sequence become zero, in y
+ * and in dx, and malformed offsets give meaningless results but no access outside the tensors.
+ * final_state may be initial_state itself (generation), otherwise no output may overlap an input.  C <= 2^20, B L <= 2^30.
+ */
+typedef struct {
+    int32_t B, L, C, W;
+    int32_t dtype;
+    int32_t num_seqs;                /* packed layout only: N */
+    const int32_t *cu_seqlens;       /* DEVICE int32 [N + 1], or NULL for the dense layout */
+    const int32_t *cu_seqlens_host;  /* optional HOST copy */
+    int32_t parts;                   /* 1 to 3 */
+    int32_t width[3], silu[3];       /* of each part: channels (a multiple of 16 bytes, C in all), whether SiLU is applied */
+    int64_t x_stride, dx_stride;     /* elements between rows; dx_stride: backward only */
+} dn_conv_shape;
+
+/* y: HOST array of `parts` device pointers.  final_state may be NULL (not written). */
+int deltanet_short_conv_fwd(const dn_conv_shape *shape, const void *x, const void *weight, const void *bias, const void *initial_state,
+                            void *const *y, void *final_state, void *hip_stream);
+
+/* Its gradient: from dy (HOST array of `parts` device pointers) and dfinal_state (NULL: zeros), dx and dinitial_state (element type; the latter NULL where not wanted), dweight (fp32
+ * [C, W]) and dbias (fp32 [C]; NULL where not wanted, also dweight). */
+int deltanet_short_conv_workspace_bytes(const dn_conv_shape *shape, size_t *out_bytes);
+int deltanet_short_conv_bwd(const dn_conv_shape *shape, const void *x, const void *weight, const void *const *dy, const void *bias,
+                            const void *initial_state, const void *dfinal_state, void *dx, float *dweight, float *dbias,
+                            void *dinitial_state, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Output norm.  Per token and head, with o a row of the mixer's output, g its gate's row and w a weight of d elements (NULL: ones),
+ *
+ *     y = o / sqrt(mean(o^2) + eps) * w * act(g) ,    act(g) = g sigmoid(g) or sigmoid(g)    (gate NULL: no such factor)
+ *
+ * o, gate and dgate are [T, H, d] with their strides between tokens, y, dy and d_o contiguous.  d = 32, 64, 128, 256 in fp32 and bf16; T <= 2^30, T * H < 2^31.
+ * Backward: d_o and dgate (element type; NULL where there is no gate), dweight (fp32 [d]; NULL where not wanted).  d_o may take the place of dy, and y that of a contiguous o.
+ */
+typedef enum { DN_ACT_SILU = 1, DN_ACT_SIGMOID = 2 } dn_act;
+typedef struct {
+    int32_t T, H, d;
+    int32_t dtype, act;              /* act: dn_act */
+    float eps;                       /* finite, >= 0 */
+    int64_t o_stride, gate_stride, dgate_stride; /* the latter two: where there is a gate; dgate_stride: backward only */
+} dn_out_norm_shape;
+int deltanet_out_norm_fwd(const dn_out_norm_shape *shape, const void *o, const void *gate, const void *weight, void *y, void *hip_stream);
+int deltanet_out_norm_workspace_bytes(const dn_out_norm_shape *shape, size_t *out_bytes);
+int deltanet_out_norm_bwd(const dn_out_norm_shape *shape, const void *o, const void *dy, const void *gate, const void *weight, void *d_o,
+                          void *dgate, float *dweight, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Block norm.  What stands between two blocks: the branch x that a block adds to the residual stream, its own norm (post_norm) and gate u per channel (NULL: ones), the sum, and the norm
+ * in front of the next block, with weight w (NULL: ones),
+ *
+ *     h = residual_scale * residual + scale * u * m ,  m = x , or x / sqrt(mean(x^2) + eps) ;    y = h / sqrt(mean(h^2) + eps) * w
+ *
+ * for T rows of D elements.  x, y, the vectors and their rows' gradients dy, dx are of type dtype; residual, h, dh and dresidual of stream_dtype (dtype, or DN_F32 for bf16 tensors).  y comes from
+ * the sum before it is rounded to h.  residual may be NULL (zeros), and h (not written).  D: a multiple of 8, at most 8192; T <= 2^30.
+ * Backward, from dy, dh (NULL: zeros), the h that the forward call left and (with post_norm or a gate) x: dx, dresidual, dweight and dgate (fp32 [D]), each NULL where not wanted.  A
+ * row's outputs may take the place of an input row of the same type and layout (y of x, h of residual, dx of dy, dresidual of dh).
+ */
+typedef struct {
+    int32_t T, D;
+    int32_t dtype, stream_dtype;
+    int32_t post_norm;
+    float scale, residual_scale;     /* finite */
+    float eps;                       /* finite, >= 0 */
+    int64_t x_stride, residual_stride;
+} dn_block_norm_shape;
+int deltanet_block_norm_fwd(const dn_block_norm_shape *shape, const void *x, const void *residual, const void *weight, const void *gate,
+                            void *y, void *h, void *hip_stream);
+int deltanet_block_norm_workspace_bytes(const dn_block_norm_shape *shape, size_t *out_bytes);
+int deltanet_block_norm_bwd(const dn_block_norm_shape *shape, const void *dy, const void *dh, const void *h, const void *x,
+                            const void *weight, const void *gate, void *dx, void *dresidual, float *dweight, float *dgate,
+                            void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * Measurement aid (not part of the method): per-kernel device time.  After
  * deltanet_profile_enable(1), every kernel launch of deltanet_fwd / deltanet_bwd is bracketed by a
  * pair of HIP events recorded on the launch stream.  deltanet_profile_collect waits for those

@@ -43,3 +43,11 @@ from .attention import (  # noqa: F401
     deltanet_qk_norm_rope_bwd,
     deltanet_qk_norm_rope_fwd,
 )
+from .layer import (  # noqa: F401
+    deltanet_block_norm_bwd,
+    deltanet_block_norm_fwd,
+    deltanet_out_norm_bwd,
+    deltanet_out_norm_fwd,
+    deltanet_short_conv_bwd,
+    deltanet_short_conv_fwd,
+)

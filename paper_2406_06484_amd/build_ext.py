@@ -1,5 +1,5 @@
 """Builds libdeltanet_hip.so in-tree with hipcc for gfx950 (one object per .hip file, in parallel), and the Python module that calls its
-attention operators with tensors (_attention.so, host code against torch's headers)."""
+attention and layer operators with tensors (_attention.so, host code against torch's headers)."""
 from __future__ import annotations
 
 import os
@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libdeltanet_hip.so")
 BINDING = os.path.join(HERE, "_attention.so")
 SOURCES = ["dn_api.hip", "dn_inst_f32.hip", "dn_inst_bf16.hip", "dn_inst_bf16_wide.hip", "dn_recurrent.hip", "dn_noalloc.hip", "dn_lds_probe.hip",
-           "dn_attn_api.hip", "dn_norm_rope.hip", "dn_paged_attn.hip"]
+           "dn_attn_api.hip", "dn_norm_rope.hip", "dn_paged_attn.hip", "dn_layer_api.hip", "dn_short_conv.hip", "dn_layer_norm.hip"]
+BINDING_SOURCES = ["dn_attention_binding.cpp", "dn_layer_binding.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
@@ -49,7 +50,7 @@ def _compile_binding() -> None:
     tmp = BINDING + ".tmp.%d" % os.getpid()
     cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
            "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
-           "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "dn_attention_binding.cpp"), "-o", tmp,
+           "-isystem", sysconfig.get_paths()["include"], *(os.path.join(CSRC, src) for src in BINDING_SOURCES), "-o", tmp,
            "-L" + os.path.join(root, "lib"), "-Wl,-rpath," + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-ldl"]
     try:
         r = subprocess.run(cmd, capture_output=True, text=True)
@@ -58,7 +59,7 @@ def _compile_binding() -> None:
     if r.returncode != 0:
         if os.path.exists(BINDING):
             os.remove(BINDING)
-        raise RuntimeError("g++ failed on dn_attention_binding.cpp:\n" + r.stderr)
+        raise RuntimeError("g++ failed on %s:\n%s" % (", ".join(BINDING_SOURCES), r.stderr))
     if r.stderr.strip():
         sys.stderr.write(r.stderr)
     os.replace(tmp, BINDING)

@@ -2,21 +2,19 @@
 // that the caller did not bring, the current stream: what attention.py would do, at a fraction of the interpreter's time (a call of
 // deltanet_paged_attn_fwd costs the host 10 us through ctypes; a decode step makes some tens of such calls, each of a few
 // microseconds on the device).  Every function returns its result, or the negative dn_status of the call as an integer.
-#include <Python.h>
-
-#include <ATen/ATen.h>
 #include <dlfcn.h>
-#include <torch/csrc/Exceptions.h>
-#include <torch/csrc/autograd/python_variable.h>
 
-#include <algorithm>
-#include <initializer_list>
-#include <sstream>
-#include <string>
+#include "dn_binding.hpp"
 
-#include "../../include/deltanet.h"
+// the functions of dn_layer_binding.cpp
+namespace dn_binding {
+extern const Symbol layer_symbols[];
+extern PyMethodDef layer_methods[];
+}
 
 namespace {
+
+using namespace dn_binding;
 
 // The library's entry points, found once in the file that the package names.
 struct Lib {
@@ -29,105 +27,6 @@ struct Lib {
     decltype(&deltanet_paged_attn_workspace_bytes) attn_bytes;
     decltype(&deltanet_paged_attn_fwd) attn;
 } lib;
-PyObject *g_raw_stream = nullptr; // device index -> handle of its current stream
-
-struct Refusal { PyObject *type; std::string text; };
-
-std::string text_of(at::IntArrayRef s) {
-    std::ostringstream o;
-    o << '(';
-    for (size_t i = 0; i < s.size(); ++i) o << (i ? ", " : "") << s[i];
-    o << ')';
-    return o.str();
-}
-
-const at::Tensor &tensor(PyObject *o, const char *name) {
-    if (!THPVariable_Check(o)) throw Refusal{PyExc_TypeError, std::string(name) + " must be a tensor"};
-    return THPVariable_Unpack(o);
-}
-const at::Tensor *maybe(PyObject *o, const char *name) { return o == Py_None ? nullptr : &tensor(o, name); }
-
-void on_device(const at::Tensor &t, const char *name, at::ScalarType type, at::IntArrayRef shape) {
-    if (!t.is_cuda()) throw Refusal{PyExc_ValueError, std::string(name) + " must be a device tensor"};
-    if (t.scalar_type() != type) throw Refusal{PyExc_TypeError, std::string(name) + " must be " + at::toString(type) + ", got " + at::toString(t.scalar_type())};
-    if (t.sizes() != shape) throw Refusal{PyExc_ValueError, std::string(name) + " must have shape " + text_of(shape) + ", got " + text_of(t.sizes())};
-}
-void whole(const at::Tensor &t, const char *name, at::ScalarType type, at::IntArrayRef shape) {
-    on_device(t, name, type, shape);
-    if (!t.is_contiguous()) throw Refusal{PyExc_ValueError, std::string(name) + " must be contiguous"};
-}
-// elements between the rows of t [T, heads, d], whose rows are contiguous
-int64_t rows(const at::Tensor &t, const char *name, at::ScalarType type, int64_t T, int64_t H, int64_t d) {
-    on_device(t, name, type, {T, H, d});
-    if ((t.stride(2) != 1 && d > 1) || (t.stride(1) != d && H > 1)) throw Refusal{PyExc_ValueError, std::string(name) + " must be contiguous within its rows of heads x d"};
-    return T > 1 ? t.stride(0) : H * d;
-}
-
-// The array of integers in t; one that begins inside a 16-byte word (a part of a larger batch's) as a copy that does not, made on the call's stream.
-const int32_t *ints(const at::Tensor &t, at::Tensor &copy) {
-    if (reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0) return t.data_ptr<int32_t>();
-    copy = t.clone();
-    return copy.data_ptr<int32_t>();
-}
-
-int32_t int32(int64_t v, const char *name) {
-    if (v < INT32_MIN || v > INT32_MAX) throw Refusal{PyExc_ValueError, std::string(name) + " does not fit 32 bits"};
-    return (int32_t)v;
-}
-int64_t integer(PyObject *o, const char *name) {
-    const long long v = PyLong_AsLongLong(o);
-    if (v == -1 && PyErr_Occurred()) { PyErr_Clear(); throw Refusal{PyExc_TypeError, std::string(name) + " must be an integer"}; }
-    return v;
-}
-double number(PyObject *o, const char *name) {
-    const double v = PyFloat_AsDouble(o);
-    if (v == -1.0 && PyErr_Occurred()) { PyErr_Clear(); throw Refusal{PyExc_TypeError, std::string(name) + " must be a number"}; }
-    return v;
-}
-
-int type_of(const at::Tensor &t, const char *name) {
-    if (t.scalar_type() == at::kFloat) return DN_F32;
-    if (t.scalar_type() == at::kBFloat16) return DN_BF16;
-    throw Refusal{PyExc_TypeError, std::string(name) + " must be float32 or bfloat16, got " + at::toString(t.scalar_type())};
-}
-
-void *ptr(const at::Tensor *t) { return t ? t->data_ptr() : nullptr; }
-float *fptr(const at::Tensor *t) { return static_cast<float *>(ptr(t)); }
-
-// handle of the current stream of t's device
-void *stream_of(const at::Tensor &t) {
-    PyObject *at = PyLong_FromLong(t.get_device());
-    PyObject *h = at ? PyObject_CallFunctionObjArgs(g_raw_stream, at, nullptr) : nullptr;
-    Py_XDECREF(at);
-    if (!h) throw Refusal{nullptr, ""};
-    void *s = reinterpret_cast<void *>(PyLong_AsLongLong(h));
-    Py_DECREF(h);
-    if (PyErr_Occurred()) throw Refusal{nullptr, ""};
-    return s;
-}
-
-at::Tensor out(const at::Tensor *given, const char *name, at::IntArrayRef shape, const at::Tensor &like, at::ScalarType type) {
-    if (!given) return at::empty(shape, like.options().dtype(type));
-    whole(*given, name, type, shape);
-    return *given;
-}
-
-// the caller's workspace, or one for this call (none if none is needed)
-struct Scratch {
-    at::Tensor held;
-    size_t bytes = 0;
-    Scratch(const at::Tensor *given, size_t need, const at::Tensor &like) {
-        if (given) {
-            if (!given->is_cuda() || !given->is_contiguous()) throw Refusal{PyExc_ValueError, "workspace must be a contiguous device tensor"};
-            held = *given;
-            bytes = given->nbytes();
-        } else if (need) {
-            held = at::empty({(int64_t)need}, like.options().dtype(at::kByte));
-            bytes = need;
-        }
-    }
-    void *p() const { return bytes ? held.data_ptr() : nullptr; }
-};
 
 dn_rope rope_of(const at::Tensor *table, PyObject *eps, PyObject *interleaved) {
     const int pairs = PyObject_IsTrue(interleaved);
@@ -144,13 +43,6 @@ dn_rope rope_of(const at::Tensor *table, PyObject *eps, PyObject *interleaved) {
 void weights(const at::Tensor *qw, const at::Tensor *kw, at::ScalarType type, int64_t d) {
     if (qw) whole(*qw, "q_weight", type, {d});
     if (kw) whole(*kw, "k_weight", type, {d});
-}
-
-// [B, L, H, d] with evenly spaced rows as [B L, H, d]
-at::Tensor flat(const at::Tensor &t, const char *name) {
-    const int64_t B = t.size(0), L = t.size(1);
-    if (B > 1 && L > 1 && t.stride(0) != L * t.stride(1)) throw Refusal{PyExc_ValueError, std::string(name) + " must have evenly spaced rows"};
-    return t.as_strided({B * L, t.size(2), t.size(3)}, {L > 1 || B <= 1 ? t.stride(1) : t.stride(0), t.stride(2), t.stride(3)});
 }
 
 struct QK {
@@ -217,21 +109,7 @@ int64_t first_size(const at::Tensor &t, const char *name) {
     return t.size(0);
 }
 
-PyObject *tuple_of(std::initializer_list<const at::Tensor *> ts) {
-    PyObject *r = PyTuple_New((Py_ssize_t)ts.size());
-    if (!r) return nullptr;
-    Py_ssize_t i = 0;
-    for (const at::Tensor *t : ts) {
-        PyObject *o = t ? THPVariable_Wrap(*t) : Py_NewRef(Py_None);
-        if (!o) { Py_DECREF(r); return nullptr; }
-        PyTuple_SET_ITEM(r, i++, o);
-    }
-    return r;
-}
-
 // --- the functions (arguments by position; None where the caller left one out)
-
-typedef PyObject *const *Args;
 
 PyObject *norm_rope_fwd(Args a) {
     const at::Tensor *qw = maybe(a[2], "q_weight"), *kw = maybe(a[3], "k_weight"), *table = maybe(a[4], "rope"), *pos = maybe(a[5], "positions");
@@ -329,19 +207,6 @@ PyObject *attn(Args a) {
     return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(o);
 }
 
-// nothing thrown leaves: refusals and torch's own errors (out of memory) become Python exceptions
-template <PyObject *(*F)(Args), int N> PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
-    HANDLE_TH_ERRORS
-    if (n != N) return PyErr_Format(PyExc_TypeError, "%d arguments wanted, got %zd", N, n);
-    try {
-        return F(args);
-    } catch (const Refusal &r) {
-        if (r.type) PyErr_SetString(r.type, r.text.c_str());
-        return nullptr;
-    }
-    END_HANDLE_TH_ERRORS
-}
-
 // open(path, raw_stream): finds the entry points in the library at `path`
 PyObject *open_library(PyObject *, PyObject *args) {
     const char *path;
@@ -349,18 +214,19 @@ PyObject *open_library(PyObject *, PyObject *args) {
     if (!PyArg_ParseTuple(args, "sO", &path, &raw)) return nullptr;
     void *h = dlopen(path, RTLD_NOW | RTLD_LOCAL);
     if (!h) return PyErr_Format(PyExc_OSError, "%s", dlerror());
-    struct { const char *name; void **to; } const want[] = {
+    const Symbol want[] = {
         {"deltanet_qk_norm_rope_fwd", (void **)&lib.norm_rope_fwd}, {"deltanet_qk_norm_rope_workspace_bytes", (void **)&lib.norm_rope_bytes},
         {"deltanet_qk_norm_rope_bwd", (void **)&lib.norm_rope_bwd}, {"deltanet_paged_append", (void **)&lib.append},
         {"deltanet_paged_norm_rope_append", (void **)&lib.norm_rope_append}, {"deltanet_paged_read", (void **)&lib.read},
         {"deltanet_paged_attn_workspace_bytes", (void **)&lib.attn_bytes}, {"deltanet_paged_attn_fwd", (void **)&lib.attn}};
-    for (const auto &w : want)
+    for (const Symbol &w : want)
         if (!(*w.to = dlsym(h, w.name))) return PyErr_Format(PyExc_OSError, "%s has no %s", path, w.name);
+    for (const Symbol *w = layer_symbols; w->name; ++w)
+        if (!(*w->to = dlsym(h, w->name))) return PyErr_Format(PyExc_OSError, "%s has no %s", path, w->name);
     Py_XSETREF(g_raw_stream, Py_NewRef(raw));
     Py_RETURN_NONE;
 }
 
-#define ENTRY(NAME, F, N) {NAME, (PyCFunction)(void (*)(void))(PyObject * (*)(PyObject *, PyObject *const *, Py_ssize_t))entry<F, N>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"open", open_library, METH_VARARGS, nullptr},
                          ENTRY("norm_rope_fwd", norm_rope_fwd, 10),
                          ENTRY("norm_rope_bwd", norm_rope_bwd, 15),
@@ -373,4 +239,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_attention", nullptr, -1, methods,
 
 } // namespace
 
-extern "C" PyObject *PyInit__attention() { return PyModule_Create(&module); }
+extern "C" PyObject *PyInit__attention() {
+    PyObject *m = PyModule_Create(&module);
+    if (m && PyModule_AddFunctions(m, layer_methods) < 0) { Py_DECREF(m); return nullptr; }
+    return m;
+}
