@@ -47,7 +47,7 @@
 extern "C" {
 #endif
 
-typedef enum { DN_F32 = 0, DN_BF16 = 1, DN_FP8 = 2 /* e4m3; pages of a cache only */ } dn_dtype;
+typedef enum { DN_F32 = 0, DN_BF16 = 1, DN_FP8 = 2 /* e4m3; pages of a cache only */, DN_FP4 = 4 /* e2m1, likewise */ } dn_dtype;
 
 typedef enum {
     DN_OK = 0,
@@ -276,9 +276,12 @@ int deltanet_qk_norm_rope_bwd(const dn_qk_shape *shape, const dn_rope *rope, con
 
 /*
  * The paged cache of a layer: k_pages, v_pages [num_pages, Hkv, page_size, d] of type cache_dtype, which is the tensors' type
- * or, for bf16 tensors, DN_FP8; then k_scale, v_scale (fp32 [num_pages, Hkv, page_size]) hold a factor per token and head,
+ * or, for bf16 tensors, DN_FP8 or DN_FP4.  With DN_FP8, k_scale, v_scale (fp32 [num_pages, Hkv, page_size]) hold a factor per token and head,
  * max |x| / 448 over the row, and the pages the e4m3 numbers nearest to x / factor, divided in fp32 (a row whose largest magnitude is under
- * 2^-100 is held as zeros, factor 0; one with an infinity reads back as NaN).  page_size is 16, 32, 64, 128 or 256.
+ * 2^-100 is held as zeros, factor 0; one with an infinity reads back as NaN); or DN_FP4: k_pages, v_pages [.., d / 2] hold two e2m1 numbers a byte (magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6; the sign in
+ * a number's highest bit), the first one in the low half, and k_scale, v_scale (bytes [num_pages, Hkv, page_size, d / 32]) a factor for each group of 32 along d, 2^(byte - 127), the least power of two of which
+ * six are no less than the group's largest magnitude; a number is the nearest to x / factor, ties to even (magnitudes over 1.5 * 2^127 are held as that; a group under 2^-100 is held as zeros, factor 1; one with an infinity or NaN, byte 255, reads back as
+ * NaN).  These values are bf16 numbers, so that attention over them rounds nothing that it would not round in bf16.  page_size is 16, 32, 64, 128 or 256.
  * Sequence n of the batch has kv_len[n] tokens in the cache, the new ones of this step included; its token p stands in page
  * page_table[n][p / page_size], slot p % page_size (entries past its last page may hold anything).  Its new tokens are rows
  * cu_q[n] .. cu_q[n + 1] - 1 of the packed tensors, the last of them at position kv_len[n] - 1.  Rows in front of cu_q[0] and from cu_q[num_seqs] on
@@ -300,7 +303,7 @@ typedef struct {
     int64_t q_stride, k_stride, v_stride;
 } dn_paged_shape;                        /* every call checks Hq, T and the bounds, used or not, and the strides of the tensors that it has */
 
-typedef struct { void *k_pages, *v_pages; float *k_scale, *v_scale; } dn_paged_cache; /* scales: NULL unless DN_FP8 */
+typedef struct { void *k_pages, *v_pages, *k_scale, *v_scale; } dn_paged_cache; /* scales: NULL unless DN_FP8 (fp32) or DN_FP4 (bytes) */
 
 /* Writes the new tokens' k and v to the cache.  Rows whose position is negative (a context shorter than the chunk) or for which there is no room (max_kv and
  * more), and rows in no sequence, are not written.  q_stride is not used, max_q and Hq only checked. d as for the attention below. */
@@ -328,7 +331,7 @@ int deltanet_paged_read(const dn_paged_shape *shape, const dn_paged_cache *cache
  * rounded, for few rows as two terms).  scale > 0.  Nothing at or past kv_len, nor before the windows of all of a sequence's new tokens, reaches a
  * result, whatever the pages hold there (values that one new token sees and another does not are given the weight zero in the other's row: an
  * infinity or NaN among THOSE may reach both).  Deterministic: the order of every sum depends on the sizes and lengths alone.
- * Compiled: d = 64, 128, 256 in bf16, with bf16 or DN_FP8 pages; d = 32, 64, 128 in fp32 (the precision mode; max_q * Hq < 2^26 there).
+ * Compiled: d = 64, 128, 256 in bf16, with bf16, DN_FP8 or DN_FP4 pages; d = 32, 64, 128 in fp32 (the precision mode; max_q * Hq < 2^26 there).
  * Workspace: deltanet_paged_attn_workspace_bytes (it depends on num_seqs, T, the heads, d, the types, max_q, max_kv and window).
  */
 int deltanet_paged_attn_workspace_bytes(const dn_paged_shape *shape, int32_t window, size_t *out_bytes);

@@ -12,7 +12,7 @@ from typing import Optional, Tuple
 from . import binding
 from .binding import DN_BF16, DN_F32, _check
 
-DN_FP8 = 2
+DN_FP8, DN_FP4 = 2, 4
 
 
 class dn_rope(ctypes.Structure):
@@ -112,11 +112,17 @@ def deltanet_qk_norm_rope_bwd(q, k, dq_out, dk_out, q_weight=None, k_weight=None
 
 def deltanet_paged_cache(num_pages: int, page_size: int, heads: int, d: int, dtype=None, device="cuda"):
     """The tensors of one layer's cache: (k_pages, v_pages, k_scale, v_scale), the scales None unless dtype (bfloat16 by default)
-    is float8_e4m3fn."""
+    is float8_e4m3fn (a factor per token and head) or float4_e2m1fn_x2 (two numbers an element of the pages [.., d / 2], float8_e8m0fnu factors [.., d / 32])."""
     import torch
     dtype = torch.bfloat16 if dtype is None else dtype
-    if dtype not in (torch.float32, torch.bfloat16, torch.float8_e4m3fn):
-        raise TypeError("a cache is float32, bfloat16 or float8_e4m3fn, got %s" % dtype)
+    if dtype not in (torch.float32, torch.bfloat16, torch.float8_e4m3fn, torch.float4_e2m1fn_x2):
+        raise TypeError("a cache is float32, bfloat16, float8_e4m3fn or float4_e2m1fn_x2, got %s" % dtype)
+    if dtype == torch.float4_e2m1fn_x2:
+        if d % 32:
+            raise ValueError("a 4-bit cache holds heads of a multiple of 32, got %d" % d)
+        k, v = (torch.empty(num_pages, heads, page_size, d // 2, dtype=dtype, device=device) for _ in range(2))
+        ks, vs = (torch.empty(num_pages, heads, page_size, d // 32, dtype=torch.float8_e8m0fnu, device=device) for _ in range(2))
+        return k, v, ks, vs
     k, v = (torch.empty(num_pages, heads, page_size, d, dtype=dtype, device=device) for _ in range(2))
     ks, vs = ((torch.empty(num_pages, heads, page_size, dtype=torch.float32, device=device) if dtype == torch.float8_e4m3fn else None)
               for _ in range(2))
@@ -124,7 +130,7 @@ def deltanet_paged_cache(num_pages: int, page_size: int, heads: int, d: int, dty
 
 
 def deltanet_paged_append(k, v, k_pages, v_pages, page_table, kv_len, cu_q, *, k_scale=None, v_scale=None, stream=None) -> None:
-    """Writes the new tokens' k and v [T, Hkv, d] to the paged cache (8-bit pages: quantised on the way).  Sequence n's new tokens are
+    """Writes the new tokens' k and v [T, Hkv, d] to the paged cache (8- and 4-bit pages: quantised on the way).  Sequence n's new tokens are
     rows cu_q[n] .. cu_q[n + 1] - 1, the last of them token kv_len[n] - 1 of its context; its token p stands in page
     page_table[n, p // page_size], slot p % page_size."""
     return _call("append", stream, k, v, k_pages, v_pages, page_table, kv_len, cu_q, k_scale, v_scale)
@@ -141,11 +147,11 @@ def deltanet_paged_norm_rope_append(q, k, v, k_pages, v_pages, page_table, kv_le
 
 def deltanet_paged_read(k_pages, v_pages, page_table, kv_len, cu_out, rows: int, *, dtype=None, k_scale=None, v_scale=None, k_out=None,
                         v_out=None, stream=None) -> Tuple["torch.Tensor", "torch.Tensor"]:
-    """Reads tokens back from the paged cache, as k, v [rows, Hkv, d] of `dtype` (the pages' type; bfloat16 for 8-bit pages): rows
+    """Reads tokens back from the paged cache, as k, v [rows, Hkv, d] of `dtype` (the pages' type; bfloat16 for 8- and 4-bit pages): rows
     cu_out[n] .. cu_out[n + 1] - 1 are the last tokens of sequence n's context, zeros in front of its start."""
     import torch
     held = k_pages.dtype if dtype is None else dtype
-    if held is torch.bfloat16 or (dtype is None and held is torch.float8_e4m3fn):
+    if held is torch.bfloat16 or (dtype is None and held in (torch.float8_e4m3fn, torch.float4_e2m1fn_x2)):
         code = DN_BF16
     elif held is torch.float32:
         code = DN_F32

@@ -82,9 +82,9 @@ struct Paged {
         const at::Tensor &lens = tensor(kv_len, "kv_len"), &offsets = tensor(cu, "cu_q"), *ks = maybe(k_scale, "k_scale"), *vs = maybe(v_scale, "v_scale");
         if (kp.dim() != 4 || table.dim() != 2) throw Refusal{PyExc_ValueError, "k_pages must be [num_pages, heads, page_size, d], page_table [sequences, max_pages]"};
         const at::ScalarType held = kp.scalar_type();
-        const bool quantised = held == at::kFloat8_e4m3fn;
-        if (!quantised && held != (dtype == DN_F32 ? at::kFloat : at::kBFloat16))
-            throw Refusal{PyExc_TypeError, std::string("pages must have the tensors' type or be float8_e4m3fn, got ") + at::toString(held)};
+        const bool fp4 = held == at::kFloat4_e2m1fn_x2, quantised = held == at::kFloat8_e4m3fn;
+        if (!quantised && !fp4 && held != (dtype == DN_F32 ? at::kFloat : at::kBFloat16))
+            throw Refusal{PyExc_TypeError, std::string("pages must have the tensors' type or be float8_e4m3fn or float4_e2m1fn_x2, got ") + at::toString(held)};
         const int64_t pages = kp.size(0), H = kp.size(1), ps = kp.size(2), N = table.size(0);
         whole(kp, "k_pages", held, kp.sizes());
         whole(vp, "v_pages", held, kp.sizes());
@@ -92,16 +92,20 @@ struct Paged {
             if (!ks || !vs) throw Refusal{PyExc_ValueError, "k_scale and v_scale are needed for an 8-bit cache"};
             whole(*ks, "k_scale", at::kFloat, {pages, H, ps});
             whole(*vs, "v_scale", at::kFloat, {pages, H, ps});
-        } else if (ks || vs) throw Refusal{PyExc_ValueError, "scales belong to an 8-bit cache"};
+        } else if (fp4) {
+            if (!ks || !vs) throw Refusal{PyExc_ValueError, "k_scale and v_scale are needed for a 4-bit cache"};
+            whole(*ks, "k_scale", at::kFloat8_e8m0fnu, {pages, H, ps, kp.size(3) / 16});
+            whole(*vs, "v_scale", at::kFloat8_e8m0fnu, {pages, H, ps, kp.size(3) / 16});
+        } else if (ks || vs) throw Refusal{PyExc_ValueError, "scales belong to an 8-bit or 4-bit cache"};
         whole(table, "page_table", at::kInt, table.sizes());
         whole(lens, "kv_len", at::kInt, {N});
         whole(offsets, "cu_q", at::kInt, {N + 1});
         s.num_seqs = int32(N, "sequences"); s.max_pages = int32(table.size(1), "max_pages");
-        s.num_pages = int32(pages, "num_pages"); s.Hkv = int32(H, "heads"); s.page_size = int32(ps, "page_size"); s.d = int32(kp.size(3), "d");
-        s.dtype = dtype; s.cache_dtype = quantised ? DN_FP8 : dtype;
+        s.num_pages = int32(pages, "num_pages"); s.Hkv = int32(H, "heads"); s.page_size = int32(ps, "page_size"); s.d = int32(kp.size(3) * (fp4 ? 2 : 1), "d");
+        s.dtype = dtype; s.cache_dtype = fp4 ? DN_FP4 : quantised ? DN_FP8 : dtype;
         s.max_kv = (int32_t)std::min<int64_t>(table.size(1) * ps, 1 << 30); // (the most that a context may have)
         s.cu_q = ints(offsets, copies[0]); s.kv_len = ints(lens, copies[1]); s.page_table = ints(table, copies[2]);
-        c.k_pages = kp.data_ptr(); c.v_pages = vp.data_ptr(); c.k_scale = fptr(ks); c.v_scale = fptr(vs);
+        c.k_pages = kp.data_ptr(); c.v_pages = vp.data_ptr(); c.k_scale = ptr(ks); c.v_scale = ptr(vs);
     }
 };
 int64_t first_size(const at::Tensor &t, const char *name) {

@@ -42,12 +42,15 @@ int check_qk(const dn_qk_shape *s) {
     return check_rows(s->k_stride, s->Hkv, s->d, elem_bytes(s->dtype));
 }
 
+// whether the pages' numbers are multiplied by factors beside them
+bool factored(const dn_paged_shape *s) { return s->cache_dtype == DN_FP8 || s->cache_dtype == DN_FP4; }
+
 int check_paged(const dn_paged_shape *s) {
     if (!s) return DN_ERR_NULL;
     if (int rc = check_heads(s->T, s->Hq, s->Hkv, s->dtype)) return rc;
     const bool d_ok = s->dtype == DN_F32 ? s->d == 32 || s->d == 64 || s->d == 128 : s->d == 64 || s->d == 128 || s->d == 256;
     if (!d_ok) return DN_ERR_UNSUPPORTED;
-    if (s->cache_dtype != s->dtype && !(s->cache_dtype == DN_FP8 && s->dtype == DN_BF16)) return DN_ERR_UNSUPPORTED;
+    if (s->cache_dtype != s->dtype && !(factored(s) && s->dtype == DN_BF16)) return DN_ERR_UNSUPPORTED;
     const int ps = s->page_size;
     if (ps != 16 && ps != 32 && ps != 64 && ps != 128 && ps != 256) return DN_ERR_UNSUPPORTED;
     if (s->num_seqs < 0 || s->num_seqs > 65535 || s->num_pages < 0 || s->max_pages < 0 || s->max_q < 0 || s->max_kv < 0) return DN_ERR_SHAPE;
@@ -63,7 +66,7 @@ int check_cache(const dn_paged_shape *s, const dn_paged_cache *c) {
     if (s->num_seqs && (!s->cu_q || !s->kv_len)) return DN_ERR_NULL;
     if (s->max_kv && s->num_seqs) {
         if (!s->page_table || !c->k_pages || !c->v_pages) return DN_ERR_NULL;
-        if (s->cache_dtype == DN_FP8 && (!c->k_scale || !c->v_scale)) return DN_ERR_NULL;
+        if (factored(s) && (!c->k_scale || !c->v_scale)) return DN_ERR_NULL;
     }
     const void *al[] = {c->k_pages, c->v_pages, c->k_scale, c->v_scale, s->cu_q, s->kv_len, s->page_table};
     for (const void *p : al) if (misaligned(p)) return DN_ERR_ALIGN;
@@ -72,7 +75,8 @@ int check_cache(const dn_paged_shape *s, const dn_paged_cache *c) {
 
 PagedArgs paged_args(const dn_paged_shape *s, const dn_paged_cache *c) {
     PagedArgs a;
-    a.kp = c->k_pages; a.vp = c->v_pages; a.ks = c->k_scale; a.vs = c->v_scale;
+    a.kp = c->k_pages; a.vp = c->v_pages; a.ks = static_cast<float *>(c->k_scale); a.vs = static_cast<float *>(c->v_scale);
+    a.fp4 = s->cache_dtype == DN_FP4;
     a.cu = s->cu_q; a.kv_len = s->kv_len; a.table = s->page_table;
     a.N = s->num_seqs;
     a.page_shift = __builtin_ctz((unsigned)s->page_size);

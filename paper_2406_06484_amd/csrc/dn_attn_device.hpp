@@ -7,6 +7,15 @@
 namespace dn {
 
 struct fp8 {}; // e4m3 pages
+struct fp4 {}; // e2m1 pages, two numbers a byte, a factor (a power of two) for each group of 32
+constexpr int kGroup = 32;
+
+// How a cache holds a row of D elements: its bytes, and those of its factors.
+template <typename CT, int D> struct Held {
+    static constexpr int BYTES = D * (int)sizeof(CT), FACTORS = 0;
+};
+template <int D> struct Held<fp8, D> { static constexpr int BYTES = D, FACTORS = 4; };
+template <int D> struct Held<fp4, D> { static constexpr int BYTES = D / 2, FACTORS = D / kGroup; };
 
 template <typename T> __device__ inline void unpack16(const uint4 &w, float (&f)[16 / sizeof(T)]) {
     const unsigned d[4] = {w.x, w.y, w.z, w.w};
@@ -37,6 +46,36 @@ __device__ inline void from_fp8x8(const uint2 &w, float (&f)[8]) {
         const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)(i ? w.y : w.x), false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)(i ? w.y : w.x), true);
         f[4 * i] = a[0]; f[4 * i + 1] = a[1]; f[4 * i + 2] = b[0]; f[4 * i + 3] = b[1];
     }
+}
+
+// Eight e2m1 numbers, the first in the lowest bits, and their factor, as bf16 (exact: two significant bits and a power of two).
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+template <int PAIR> __device__ inline unsigned fp4_pair(unsigned w, float factor) {
+    typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, factor, PAIR);
+    return __builtin_bit_cast(unsigned, v);
+}
+__device__ inline u32x4 from_fp4x8(unsigned w, float factor) { return u32x4{fp4_pair<0>(w, factor), fp4_pair<1>(w, factor), fp4_pair<2>(w, factor), fp4_pair<3>(w, factor)}; }
+// The factor that a byte stands for, 2^(byte - 127); 255 is NaN, as all the group's numbers are then.  (The conversion takes the exponent alone, and a zero for
+// another number than 2^-127.)
+__device__ inline float fp4_factor(unsigned byte) { return __uint_as_float(max(byte << 23, 0x00400000u)); }
+// The byte of the least power of two of which six, the largest e2m1 number, are enough for a group whose largest magnitude is `top`.  A group under 2^-100 is held as zeros,
+// one with an infinity or NaN as NaN.
+__device__ inline unsigned fp4_factor_byte(float top) {
+    const unsigned u = __float_as_uint(top), e = u >> 23; // 6 = 1.5 2^2
+    const unsigned b = e - ((u & 0x7fffffu) > 0x400000u ? 1u : 2u);
+    return e == 255u ? 255u : top < 0x1p-100f ? 127u : b;
+}
+// eight numbers over their factor, each rounded to the nearest e2m1 number, ties to even (the largest ones to three of the largest factor: four would be past bf16's range)
+__device__ inline unsigned to_fp4x8(const float (&y)[8], float factor) {
+    unsigned w = 0;
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = __builtin_amdgcn_fmed3f(y[i], -0x1.8p127f, 0x1.8p127f);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[0], f[1], factor, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[2], f[3], factor, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[4], f[5], factor, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[6], f[7], factor, 3);
 }
 
 // x combined over the lanes of an aligned group of N, in all of them: lane swaps on the vector ALU, no LDS traffic.  Every

@@ -23,9 +23,10 @@ struct RowArgs {
 // The cache and the batch's place in it.
 struct PagedArgs {
     void *kp, *vp;
-    float *ks, *vs;
+    float *ks, *vs;                      // 4-bit pages: the groups' factors, a byte each
     const int32_t *cu, *kv_len, *table;  // cu: of the rows that are written, read back or attend
     int N, page_shift, num_pages, max_pages, max_kv;
+    bool fp4;                            // pages of e2m1 numbers
 };
 
 struct AttnArgs {
@@ -38,7 +39,7 @@ struct AttnArgs {
     void *workspace;
 };
 
-// All return 0 or the hipError_t of the failing launch.  dtype: 0 = fp32, 1 = bf16; fp8: whether the pages are 8-bit.
+// All return 0 or the hipError_t of the failing launch.  dtype: 0 = fp32, 1 = bf16; fp8: whether the pages are 8-bit (4-bit: fp4 in the arguments; else they have the tensors' type).
 int run_norm_rope_fwd(int dtype, int d, const RowArgs &a, hipStream_t stream);
 int run_norm_rope_bwd(int dtype, int d, const RowArgs &a, hipStream_t stream);
 int run_paged_append(int dtype, int d, bool fp8, bool norm, const RowArgs &a, const PagedArgs &c, hipStream_t stream);

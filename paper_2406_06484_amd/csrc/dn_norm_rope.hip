@@ -355,6 +355,19 @@ __device__ inline void cache_row(const Rows &to, const Rows &scale, int step, in
         typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
         __builtin_amdgcn_raw_buffer_store_b64(u32x2{w.x, w.y}, to.rs, to.off + step * to.step, 0, 0);
         if (e0 == 0) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(s), scale.rs, scale.off + step * scale.step, 0, 0);
+    } else if constexpr (__is_same(CT, fp4)) {
+        // A group's factor is a power of two: quotients are exact but for the one rounding to e2m1, which the conversion does.
+        float amax = 0.f;
+#pragma unroll
+        for (int i = 0; i < L::V; ++i) amax = fmaxf(amax, fabsf(y[i]));
+        bool whole = amax < INFINITY;
+#pragma unroll
+        for (int i = 0; i < L::V; ++i) whole = whole && y[i] == y[i];
+        amax = lanes_max<kGroup / L::V>(whole ? amax : INFINITY); // (a maximum passes over NaN)
+        const unsigned byte = fp4_factor_byte(amax);
+        const unsigned w = amax < 0x1p-100f ? 0u : to_fp4x8(y, fp4_factor(byte));
+        __builtin_amdgcn_raw_buffer_store_b32(w, to.rs, to.off + step * to.step, 0, 0);
+        if (e0 % kGroup == 0) __builtin_amdgcn_raw_buffer_store_b8((unsigned char)byte, scale.rs, scale.off + step * scale.step, 0, 0);
     } else store16(to, step, pack16<T>(y));
 }
 
@@ -372,7 +385,7 @@ constexpr int kAppendSteps = 2;
 template <typename T, typename CT, int D, bool NORM, bool IL>
 __global__ __launch_bounds__(256) void k_paged_append(RowArgs a, PagedArgs c, int per) {
     using L = RowLayout<T, D>;
-    constexpr int ES = (int)sizeof(T), CB = __is_same(CT, fp8) ? 1 : ES; // bytes of an element, and in the cache
+    constexpr int ES = (int)sizeof(T), CB = Held<CT, D>::BYTES, FB = Held<CT, D>::FACTORS; // bytes of an element; of a row and of its factors in the cache
     __shared__ __align__(16) float turns[NORM ? 4 : 1][NORM ? D : 4];
     __shared__ __align__(16) T weight[NORM ? 2 : 1][NORM ? D : 8];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), e0 = (lane % L::LPR) * L::V, sub = lane / L::LPR;
@@ -434,8 +447,8 @@ __global__ __launch_bounds__(256) void k_paged_append(RowArgs a, PagedArgs c, in
                 store16(to, step, pack16<T>(y));
             } else { // head h of the token is row s.base + h s.stride
                 const int rows = live ? (a.Hkv - 1) * s.stride + 1 : 0;
-                const Rows to{make_rsrc(static_cast<char *>(what == 1 ? c.kp : c.vp) + s.base * (D * CB), rows * (D * CB)), (sub * s.stride * D + e0) * CB, L::RPW * s.stride * D * CB};
-                const Rows scale{make_rsrc((what == 1 ? c.ks : c.vs) + s.base, rows * 4), sub * s.stride * 4, L::RPW * s.stride * 4};
+                const Rows to{make_rsrc(static_cast<char *>(what == 1 ? c.kp : c.vp) + s.base * CB, rows * CB), sub * s.stride * CB + e0 * CB / D, L::RPW * s.stride * CB};
+                const Rows scale{make_rsrc(reinterpret_cast<char *>(what == 1 ? c.ks : c.vs) + s.base * FB, rows * FB), sub * s.stride * FB + (__is_same(CT, fp4) ? e0 / kGroup : 0), L::RPW * s.stride * FB};
                 cache_row<T, CT, D>(to, scale, step, e0, y);
             }
         }
@@ -472,6 +485,9 @@ __global__ __launch_bounds__(256) void k_paged_read(RowArgs a, PagedArgs c, int 
                 const uint2 w = *reinterpret_cast<const uint2 *>(static_cast<const unsigned char *>(pages) + row * D + e0);
                 x[b].x = w.x; x[b].y = w.y;
                 f[b] = (is_k ? c.ks : c.vs)[row];
+            } else if constexpr (__is_same(CT, fp4)) {
+                x[b].x = *reinterpret_cast<const unsigned *>(static_cast<const unsigned char *>(pages) + row * (D / 2) + e0 / 2);
+                f[b] = fp4_factor(reinterpret_cast<const unsigned char *>(is_k ? c.ks : c.vs)[row * (D / kGroup) + e0 / kGroup]);
             } else x[b] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(pages) + row * D + e0);
         }
     }
@@ -488,6 +504,7 @@ __global__ __launch_bounds__(256) void k_paged_read(RowArgs a, PagedArgs c, int 
             for (int i = 0; i < 8; ++i) y[i] *= f[b];
             x[b] = pack16<T>(y);
         }
+        if constexpr (__is_same(CT, fp4)) x[b] = __builtin_bit_cast(uint4, from_fp4x8(x[b].x, live ? f[b] : 1.f)); // (rows without a place: zeros)
         if (h < a.Hkv) *reinterpret_cast<uint4 *>(static_cast<T *>(is_k ? a.k_out : a.v_out) + ((long)t * a.Hkv + h) * D + e0) = x[b];
     }
 }
@@ -577,8 +594,10 @@ struct AppendLaunch {
         int waves, per = steps_per_wave<T, D>(a.T, norm ? a.Hq : 0, a.Hkv, kAppendSteps, &waves);
         void *args[] = {&a, &c, &per};
         const void *fn = of<T, D, T>();
-        if constexpr (sizeof(T) == 2)
-            if (fp8_pages) fn = of<T, D, fp8>();
+        if constexpr (sizeof(T) == 2) {
+            if (c.fp4) fn = of<T, D, fp4>();
+            else if (fp8_pages) fn = of<T, D, fp8>();
+        }
         return launch("k_paged_append", fn, token_grid(a.T, waves), args, stream);
     }
 };
@@ -594,8 +613,10 @@ struct ReadLaunch {
         int waves, per = steps_per_wave<T, D>(a.T, 0, a.Hkv, skv < 2 ? 2 : skv < kReadSteps ? skv : kReadSteps, &waves);
         void *args[] = {&a, &c, &per};
         const void *fn = reinterpret_cast<const void *>(k_paged_read<T, T, D>);
-        if constexpr (sizeof(T) == 2)
-            if (fp8_pages) fn = reinterpret_cast<const void *>(k_paged_read<T, fp8, D>);
+        if constexpr (sizeof(T) == 2) {
+            if (c.fp4) fn = reinterpret_cast<const void *>(k_paged_read<T, fp4, D>);
+            else if (fp8_pages) fn = reinterpret_cast<const void *>(k_paged_read<T, fp8, D>);
+        }
         return launch("k_paged_read", fn, token_grid(a.T, waves), args, stream);
     }
 };

@@ -84,13 +84,9 @@ constexpr int kFewTile = 16, kFewKeys = 32, kFewWaves = 4;
 // Twice as many waves per workgroup where there are few workgroups, if their registers allow it.
 template <typename T> constexpr bool few_twice(int d) { return d * sizeof(T) <= 256; }
 
-template <typename T, typename CT> struct PageElem { typedef CT type; static constexpr int bytes = (int)sizeof(CT); };
-template <typename T> struct PageElem<T, fp8> { typedef unsigned char type; static constexpr int bytes = 1; };
-
 // W words, from `off` bytes behind a descriptor's base on, in pieces of 16 bytes that are `step` bytes apart.  (Buffer loads: the base, the same for the whole wave, stays in scalar registers, where a global load
 // would have a 64-bit address per lane and load.)
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 template <int W> __device__ inline void load_words(unsigned (&w)[W], __amdgpu_buffer_rsrc_t rs, int off, int step = 16) {
     if constexpr (W == 1) w[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0);
     else if constexpr (W == 2) { const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0); w[0] = x[0]; w[1] = x[1]; }
@@ -114,12 +110,14 @@ __device__ inline u32x4 widen(unsigned lo, unsigned hi) { return u32x4{bf16_pair
 template <typename T, typename CT, int D, int WAVES>
 __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut, int max_rows, int block, float *smem) {
     const int splits = cut.splits, split_keys = cut.keys;
-    constexpr int EB = PageElem<T, CT>::bytes;
+    constexpr bool FP8 = __is_same(CT, fp8), FP4 = __is_same(CT, fp4);
+    constexpr int RB = Held<CT, D>::BYTES;              // bytes of a row
     constexpr int KE = D / 4, VE = D / 16;              // elements of a key, of a value, that a lane holds
-    constexpr int KW = KE * EB / 4, VW = VE * EB / 4;   // in words
-    constexpr int KV = 16 / EB;                         // elements of a piece of a key: (4 piece + g) KV ..
-    constexpr int VV = VE * EB > 16 ? 16 / EB : VE;     // ... and of a value: (16 piece + col) VV ..
-    constexpr bool FP8 = __is_same(CT, fp8);
+    constexpr int KB = RB / 4, VB = RB / 16;            // in bytes
+    constexpr int KW = KB / 4, VW = VB < 4 ? 1 : VB / 4; // in words
+    constexpr int KP = KB < 16 ? KB : 16, KV = KP * D / RB; // bytes, elements of a piece of a key: (4 piece + g) KV ..
+    constexpr int VV = VB > 16 ? 16 * D / RB : VE;      // ... and of a value: (16 piece + col) VV ..
+    constexpr int FB = FP4 ? D / kGroup : 1, FW = FP4 ? FB : 1; // factors of a row; words with those of four rows
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int Hkv = a.r.Hkv, G = a.r.Hq / Hkv;
     int b = block;
@@ -161,11 +159,18 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
     const char *kp = static_cast<const char *>(a.c.kp), *vp = static_cast<const char *>(a.c.vp);
     unsigned kw[2][KW], vw[8][VW];
     float4 ks[2], vs[2];
+    // 4-bit pages: the factors' bytes, of key col's groups, and of all groups of the values 4 g .. 4 g + 3
+    unsigned kf[2][FP4 && D > 128 ? 2 : 1], vf[2][FW];
     auto load_k = [&](int k0, const int (&page)[2]) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const long row = row_of(a.c, page[h], k0 + 16 * h, kvh, Hkv);
-            load_words(kw[h], make_rsrc(kp + row * (D * EB)), col * D * EB + 16 * g, 64);
+            load_words(kw[h], make_rsrc(kp + row * RB), col * RB + KP * g, 64);
+            if constexpr (FP4) {
+                const __amdgpu_buffer_rsrc_t fa = make_rsrc(reinterpret_cast<const char *>(a.c.ks) + row * FB);
+                if constexpr (FB == 2) kf[h][0] = __builtin_amdgcn_raw_buffer_load_b16(fa, col * FB, 0, 0);
+                else load_words(kf[h], fa, col * FB);
+            }
             if constexpr (FP8) ks[h] = *reinterpret_cast<const float4 *>(a.c.ks + row + 4 * g);
         }
     };
@@ -173,9 +178,13 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const long row = row_of(a.c, page[h], k0 + 16 * h, kvh, Hkv);
-            const __amdgpu_buffer_rsrc_t va = make_rsrc(vp + row * (D * EB));
+            const __amdgpu_buffer_rsrc_t va = make_rsrc(vp + row * RB);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) load_words(vw[4 * h + i], va, ((4 * g + i) * D + col * VV) * EB, 256);
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (VB == 2) vw[4 * h + i][0] = __builtin_amdgcn_raw_buffer_load_b16(va, (4 * g + i) * RB + col * VB, 0, 0);
+                else load_words(vw[4 * h + i], va, (4 * g + i) * RB + col * (VV * RB / D), 256);
+            }
+            if constexpr (FP4) load_words(vf[h], make_rsrc(reinterpret_cast<const char *>(a.c.vs) + row * FB), 4 * g * FB);
             if constexpr (FP8) vs[h] = *reinterpret_cast<const float4 *>(a.c.vs + row + 4 * g);
         }
     };
@@ -197,6 +206,13 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
     for (; k0 < k_end; k0 += STEP) {
         const bool more = k0 + STEP < k_end;
         f32x4 st[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+        // (the lane's group of a key: element (4 piece + g) KV / 32)
+        float kfac[2][FP4 ? KE / KV : 1];
+        if constexpr (FP4)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < KE / KV; ++i) kfac[h][i] = fp4_factor(kf[h][i] >> 8 * (g * KV / kGroup) & 255u);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             if constexpr (sizeof(T) == 4) {
@@ -208,6 +224,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
                 for (int e = 0; e < KE / 8; ++e) {
                     u32x4 kk;
                     if constexpr (FP8) kk = widen(kw[h][2 * e], kw[h][2 * e + 1]);
+                    else if constexpr (FP4) kk = from_fp4x8(kw[h][e], kfac[h][8 * e / KV]);
                     else kk = u32x4{kw[h][4 * e], kw[h][4 * e + 1], kw[h][4 * e + 2], kw[h][4 * e + 3]};
                     const u32x4 qq = u32x4{qw[4 * e], qw[4 * e + 1], qw[4 * e + 2], qw[4 * e + 3]};
                     st[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kk), __builtin_bit_cast(bf16x8, qq), st[h], 0, 0, 0);
@@ -247,6 +264,16 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
 #pragma unroll
             for (int i = 0; i < 4; ++i) { st[h][i] = __builtin_amdgcn_exp2f((st[h][i] - m) * c); sum += st[h][i]; }
         l += sum;
+        float vfac[FP4 ? 8 : 1];
+        if constexpr (FP4)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int at = (i & 3) * FB; // byte of row i's first factor
+                unsigned w = vf[i >> 2][at / 4] >> 8 * (at % 4);
+                const int group = col * VV / kGroup;
+                if constexpr (FB > 4) w ^= (w ^ vf[i >> 2][at / 4 + 1]) & (group < 4 ? 0u : ~0u);
+                vfac[i] = fp4_factor(w >> 8 * (group & 3) & 255u);
+            }
         if (k0 + kFewKeys > hi || k0 < from) { // what no row sees enters no result
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -257,6 +284,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
 #pragma unroll
                     for (int w = 0; w < VW; ++w) vw[4 * h + i][w] = dead ? 0u : vw[4 * h + i][w];
                     if constexpr (FP8) if (dead) reinterpret_cast<float *>(&vs[h])[i] = 0.f;
+                    if constexpr (FP4) vfac[4 * h + i] = dead ? 1.f : vfac[4 * h + i];
                 }
         }
         if constexpr (FP8)
@@ -284,6 +312,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     if constexpr (FP8) x[i] = bf16_pair(vw[i][w / 2], w & 1);
+                    else if constexpr (FP4) x[i] = w % 4 == 0 ? fp4_pair<0>(vw[i][w / 4], vfac[i]) : w % 4 == 1 ? fp4_pair<1>(vw[i][w / 4], vfac[i]) : w % 4 == 2 ? fp4_pair<2>(vw[i][w / 4], vfac[i]) : fp4_pair<3>(vw[i][w / 4], vfac[i]);
                     else x[i] = vw[i][w];
                 }
                 u32x4 even, odd;
@@ -377,10 +406,10 @@ __device__ inline unsigned lds_place(const unsigned char *p) {
 __device__ __forceinline__ void wait_moved() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 template <typename CT, int D> struct WideTile {
-    static constexpr bool FP8 = __is_same(CT, fp8);
+    static constexpr bool FP8 = __is_same(CT, fp8), FP4 = __is_same(CT, fp4);
     static constexpr int KEYS = wide_keys(D);
     static constexpr int CH = D / 8, ROWB = 2 * D;                 // 16-byte pieces, bytes of a row in the LDS
-    static constexpr int PER = FP8 ? 2 : 1, LPR = CH / PER;        // pieces per load, lanes per row
+    static constexpr int PER = FP4 ? (D > 64 ? 4 : 2) : FP8 ? 2 : 1, LPR = CH / PER; // pieces per load, lanes per row
     static constexpr int NL = KEYS * LPR / (64 * kWideWaves); // loads per thread and tensor
     static constexpr int BYTES = KEYS * ROWB;
     static constexpr int oV = BYTES, oKS = 2 * BYTES, oVS = oKS + (FP8 ? 4 * KEYS : 0), SIZE = oVS + (FP8 ? 4 * KEYS : 0);
@@ -425,8 +454,8 @@ template <typename CT, int D>
 __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few, bool zero, int block, unsigned char *wsmem) {
     const int splits = cut.splits, split_keys = cut.keys;
     using W = WideTile<CT, D>;
-    constexpr bool FP8 = W::FP8;
-    constexpr int EB = FP8 ? 1 : 2, NB = D / 32, KEYS = W::KEYS, NX = KEYS / 32;
+    constexpr bool FP8 = W::FP8, FP4 = W::FP4, WIDEN = FP8 || FP4;
+    constexpr int RB = Held<CT, D>::BYTES, NB = D / 32, KEYS = W::KEYS, NX = KEYS / 32;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), col = lane & 31, h = lane >> 5;
     const int Hkv = a.r.Hkv, G = a.r.Hq / Hkv;
     int b = block;
@@ -471,13 +500,14 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
     auto set_off = [&]() __attribute__((always_inline)) { off = fmaxf(m * c, kNoScore); far = __any(m > kNoScore && fabsf(off) > kFarScore); };
     set_off();
 
-    // this thread's pieces of a tile on their way (8-bit pages; 16-bit ones go straight to the LDS)
+    // this thread's pieces of a tile on their way (8- and 4-bit pages; 16-bit ones go straight to the LDS)
     u32x4 rk[W::NL], rv[W::NL];
     float rs = 0.f;
+    unsigned fk[W::NL], fv[W::NL]; // 4-bit pages: their groups' factors
     const char *kp = static_cast<const char *>(a.c.kp), *vp = static_cast<const char *>(a.c.vp);
     const int piece = t % W::LPR;
     int page[W::NL], spage = 0; // of the next tile to fetch, looked up a tile ahead
-    const unsigned page_bytes = (unsigned)(Hkv << a.c.page_shift) * (D * EB);
+    const unsigned page_bytes = (unsigned)(Hkv << a.c.page_shift) * RB;
     auto look_up = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < W::NL; ++i) page[i] = page_entry(a.c, n, k0 + ((i * 256 + wave * 64) / W::LPR & ~15));
@@ -487,17 +517,32 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
     auto fetch = [&](unsigned char *buf, int k0, int i) __attribute__((always_inline)) {
         const int r0 = (i * 256 + wave * 64) / W::LPR, kk = k0 + (r0 & ~15); // the wave's rows lie in one group of 16 keys
         const unsigned id = __builtin_amdgcn_readfirstlane(page_id(a.c, page[i]));
-        const long at = (long)((unsigned long)id * page_bytes) + ((kvh << a.c.page_shift) + (kk & ((1 << a.c.page_shift) - 1))) * (D * EB);
+        const long at = (long)((unsigned long)id * page_bytes) + ((kvh << a.c.page_shift) + (kk & ((1 << a.c.page_shift) - 1))) * RB;
         const int r = r0 + lane / W::LPR;
-        if constexpr (FP8) {
-            const int off = (r & 15) * (D * EB) + piece * 16;
+        if constexpr (FP4) {
+            constexpr int LB = 4 * W::PER, FB = D / kGroup; // bytes of a load; factors of a row
+            const int off = (r & 15) * RB + piece * LB;
+            if constexpr (LB == 8) {
+                const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(make_rsrc(kp + at), off, 0, 0), y = __builtin_amdgcn_raw_buffer_load_b64(make_rsrc(vp + at), off, 0, 0);
+                rk[i] = u32x4{x[0], x[1], 0, 0};
+                rv[i] = u32x4{y[0], y[1], 0, 0};
+            } else {
+                rk[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(kp + at), off, 0, 0);
+                rv[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(vp + at), off, 0, 0);
+            }
+            const long fat = at / RB * FB; // (a page is under 2^30 bytes and starts at a multiple of RB)
+            const int foff = (r & 15) * FB + piece * 2 * LB / kGroup;
+            fk[i] = __builtin_amdgcn_raw_buffer_load_b8(make_rsrc(reinterpret_cast<const char *>(a.c.ks) + fat), foff, 0, 0);
+            fv[i] = __builtin_amdgcn_raw_buffer_load_b8(make_rsrc(reinterpret_cast<const char *>(a.c.vs) + fat), foff, 0, 0);
+        } else if constexpr (FP8) {
+            const int off = (r & 15) * RB + piece * 16;
             rk[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(kp + at), off, 0, 0);
             rv[i] = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(vp + at), off, 0, 0);
             if (i == 0 && wave < 2 && lane < KEYS)
                 rs = (wave ? a.c.vs : a.c.ks)[row_of(a.c, page_id(a.c, spage), k0 + (lane & 48), kvh, Hkv) + (lane & 15)];
         } else {
             // values that no row sees arrive as zeros
-            const int off = (r & 15) * (D * EB) + ((piece ^ W::swizzle(r)) << 4);
+            const int off = (r & 15) * RB + ((piece ^ W::swizzle(r)) << 4);
             const unsigned to = lds_place(buf) + (i * 256 + wave * 64) * 16;
             move16(make_rsrc(kp + at), off, to);
             move16(make_rsrc(vp + at), (unsigned)(k0 + r - from) < (unsigned)(hi - from) ? off : kBufRange, to + W::oV);
@@ -516,6 +561,16 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
             const int r = (i * 256 + t) / W::LPR;
             u32x4 v = rv[i];
             if (ends && dead(k0 + r)) v = u32x4{0, 0, 0, 0};
+            if constexpr (FP4) {
+                const float ck = fp4_factor(fk[i]), cv = fp4_factor(ends && dead(k0 + r) ? 127u : fv[i]);
+#pragma unroll
+                for (int u = 0; u < W::PER; ++u) {
+                    unsigned char *at = buf + r * W::ROWB + (((W::PER * piece + u) ^ W::swizzle(r)) << 4);
+                    *reinterpret_cast<u32x4 *>(at) = from_fp4x8(rk[i][u], ck);
+                    *reinterpret_cast<u32x4 *>(at + W::oV) = from_fp4x8(v[u], cv);
+                }
+                continue;
+            }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 unsigned char *at = buf + r * W::ROWB + (((2 * piece + u) ^ W::swizzle(r)) << 4);
@@ -523,7 +578,8 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
                 *reinterpret_cast<u32x4 *>(at + W::oV) = widen(v[2 * u], v[2 * u + 1]);
             }
         }
-        if (wave < 2 && lane < KEYS) reinterpret_cast<float *>(buf + (wave ? W::oVS : W::oKS))[lane] = ends && dead(k0 + lane) ? 0.f : rs;
+        if constexpr (FP8)
+            if (wave < 2 && lane < KEYS) reinterpret_cast<float *>(buf + (wave ? W::oVS : W::oKS))[lane] = ends && dead(k0 + lane) ? 0.f : rs;
     };
     // a tile's work, and between its first products the requests for tile `next` (16 bits: into `to`), if `more`
     auto work = [&](const unsigned char *buf, int k0, unsigned char *to, int next, bool more) __attribute__((always_inline)) {
@@ -544,10 +600,10 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
                 for (int x = 0; x < NX; ++x) st[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x][i], q[i], i ? st[x] : f32x16{}, 0, 0, 0);
                 if (i % EVERY == EVERY - 1) {
                     __builtin_amdgcn_sched_barrier(0);
-                    if (more) fetch(to, next, i / EVERY);
+                    if (FP4 || more) fetch(to, next, i / EVERY); // (4 bits: always; a request under a condition is waited for where its paths meet)
                 }
             }
-            if (more) look_up(next + KEYS);
+            if (FP4 || more) look_up(next + KEYS);
             __builtin_amdgcn_s_setprio(0);
         }
         if constexpr (FP8)
@@ -638,7 +694,7 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
     auto seen = [&](int k0) { return k0 <= some_to && k0 + KEYS > some_from; };
     if (k_begin < k_end) {
         look_up(k_begin);
-        if constexpr (FP8) {
+        if constexpr (WIDEN) {
             fetch_all(wsmem, k_begin);
             park(wsmem, k_begin);
             if (k_begin + KEYS < k_end) fetch_all(wsmem, k_begin + KEYS);
@@ -942,6 +998,10 @@ int run_paged_attn(int dtype, int d, bool fp8_pages, const AttnArgs &a, hipStrea
         if (d == 32) return launch_attn<float, float, 32>(dtype, a, stream);
         if (d == 64) return launch_attn<float, float, 64>(dtype, a, stream);
         if (d == 128) return launch_attn<float, float, 128>(dtype, a, stream);
+    } else if (a.c.fp4) {
+        if (d == 64) return launch_attn<bf16, fp4, 64>(dtype, a, stream);
+        if (d == 128) return launch_attn<bf16, fp4, 128>(dtype, a, stream);
+        if (d == 256) return launch_attn<bf16, fp4, 256>(dtype, a, stream);
     } else if (fp8_pages) {
         if (d == 64) return launch_attn<bf16, fp8, 64>(dtype, a, stream);
         if (d == 128) return launch_attn<bf16, fp8, 128>(dtype, a, stream);

@@ -1,0 +1,211 @@
+"""The paged cache of 4-bit numbers on the GPU: written, read back and attended to, against the 64-bit statements."""
+import pytest
+import torch
+
+import paper_2406_06484_amd as dn
+from tests import attention_reference as ref
+from tests import fp4_reference as f4
+from tests.attention_util import near, replays
+from tests.fp4_reference import Batch4
+
+pytestmark = pytest.mark.gpu
+
+
+def place(b, n, pos):
+    return int(b.table_host[n, pos // b.page]), pos % b.page
+
+
+def special_rows(b):
+    """k and v rows with every kind of group among ordinary ones, bf16"""
+    x, _ = b.rows(b.Hkv)
+    y, _ = b.rows(b.Hkv)
+    levels = torch.tensor([0.0, 0.25, 0.5, 0.75, 1.0, 1.25, 1.5, 1.75, 2.0, 2.5, 3.0, 3.5, 4.0, 5.0, 6.0, -0.25, -0.75, -1.25, -1.75, -2.5, -3.5, -5.0, -6.0, -0.0])
+    ties = torch.cat([levels, levels[:8]])[:32]
+    for t, s in enumerate((1.0, 2.0 ** 40, 2.0 ** -90, 2.0 ** 124)):
+        x[t, 0, :32] = (ties * s).bfloat16().cuda()
+    x[1, 0, 32:64] = 0.0
+    x[2, 0, 32:64] = 2.0 ** -101
+    x[3, 0, 33] = float("nan")
+    y[0, 0, :32] = 3.3895e38
+    y[1, 0, 5] = float("-inf")
+    y[2, 0, 32:64] = 1e-40          # under the least normal number
+    y[3, 0, :32] = -0.0
+    return x, y
+
+
+@pytest.mark.parametrize("d,Hkv,page", [(64, 1, 16), (64, 5, 32), (128, 4, 16), (128, 2, 256), (256, 3, 64)])
+def test_append_and_read(d, Hkv, page):
+    qs, kvs = [5, 1, 0, 40, 3], [5, 300, 17, 61, 40]
+    b = Batch4(qs, kvs, Hkv, d, page=page, seed=d + Hkv)
+    k, v = special_rows(b)
+    before = {w: b.raw(w) for w in "kv"}
+    dn.deltanet_paged_append(k, v, *b.tensors(), b.cu, **b.scales())
+    back, cu_back = [9, 1, 17, 70, 3], [0, 9, 10, 27, 97, 100]
+    kr, vr = dn.deltanet_paged_read(*b.tensors(), torch.tensor(cu_back, dtype=torch.int32).cuda(), 102, **b.scales())
+    assert kr.dtype == torch.bfloat16
+    for w, x, got in (("k", k, kr), ("v", v, vr)):
+        codes, factors = f4.quantise(x.double().cpu())
+        want = [t.clone() for t in before[w]]
+        at = 0
+        for n, (m, kv) in enumerate(zip(qs, kvs)):
+            for i in range(m):
+                p, slot = place(b, n, kv - m + i)
+                want[0][p, :, slot], want[1][p, :, slot] = codes[at], factors[at]
+                at += 1
+        now = b.raw(w)
+        assert torch.equal(now[1], want[1])
+        sound = (want[1] != 255).repeat_interleave(32, -1)
+        assert torch.equal(now[0][sound], want[0][sound])
+        held = f4.values(*now)
+        got = got.double().cpu()
+        for n, (m, kv) in enumerate(zip(back, kvs)):
+            for i in range(m):
+                pos, row = kv - m + i, got[cu_back[n] + i]
+                if pos < 0:
+                    assert not row.any()
+                else:
+                    p, slot = place(b, n, pos)
+                    assert torch.equal(torch.nan_to_num(row, 7.5e37), torch.nan_to_num(held[p, :, slot], 7.5e37)) and torch.equal(row.isnan(), held[p, :, slot].isnan())
+        assert not got[100:].any()
+
+
+def test_factors_at_the_ends_of_their_range_are_read_exactly():
+    b = Batch4([1], [64], 1, 64)
+    codes = torch.randint(0, 16, (64, 64), generator=torch.Generator().manual_seed(1), dtype=torch.int32)
+    factors = torch.tensor([0, 1, 2, 24, 126, 127, 128, 250, 251, 252, 253] + [100] * 53, dtype=torch.int32)[:, None].expand(64, 2)
+    for pos in range(64):
+        p, slot = place(b, 0, pos)
+        for w in "kv":
+            getattr(b, w + "_pages").view(torch.uint8)[p, 0, slot] = f4.packed(codes[pos]).cuda()
+            getattr(b, w + "_scale").view(torch.uint8)[p, 0, slot] = factors[pos].to(torch.uint8).cuda()
+    kr, vr = dn.deltanet_paged_read(*b.tensors(), torch.tensor([0, 64], dtype=torch.int32).cuda(), 64, **b.scales())
+    want = f4.values(codes, factors).bfloat16().double()   # (exact but for 4 and 6 times 2^126, infinities in bf16, which an append does not write)
+    assert torch.equal(kr[:, 0].double().cpu(), want) and torch.equal(vr[:, 0].double().cpu(), want)
+
+
+def test_tokens_without_a_place_are_not_written():
+    b = Batch4([4, 3, 2], [2, 40, 16], 2, 64)
+    k, v = (b.rows(2)[0] for _ in range(2))
+    table = b.table.clone()
+    table[1, 2] = 10 ** 6                   # the page of positions 32 to 47 of sequence 1
+    before = [t.view(torch.uint8).clone() for t in (b.k_pages, b.v_pages, b.k_scale, b.v_scale)]
+    cu = torch.tensor([1, 4, 7, 8], dtype=torch.int32).cuda()   # the first and the last row lie in no sequence; sequence 0 has three rows over a context of two
+    dn.deltanet_paged_append(k, v, b.k_pages, b.v_pages, table, b.kv_len, cu, **b.scales())
+    codes, factors = f4.quantise(k.double().cpu())
+    for pos, row in ((0, 2), (1, 3)):
+        p, slot = place(b, 0, pos)
+        assert torch.equal(b.raw("k")[0][p, :, slot], codes[row])
+    for t, old in zip((b.k_pages, b.v_pages, b.k_scale, b.v_scale), before):
+        t = t.view(torch.uint8)
+        changed = (t != old).flatten(3).any(-1).any(1).nonzero().tolist()
+        allowed = [list(place(b, 0, 0)), list(place(b, 0, 1)), list(place(b, 2, 15))]
+        assert all(c in allowed for c in changed), changed
+
+
+@pytest.mark.parametrize("d,interleaved", [(64, False), (128, True), (256, False)])
+def test_norm_and_rotation_on_the_way(d, interleaved):
+    b = Batch4([30, 1, 7], [100, 64, 7], 2, d, seed=d)
+    (q, q64), (k, k64), (v, v64) = b.rows(4), b.rows(2), b.rows(2)
+    g = torch.Generator().manual_seed(9)
+    w = (1 + 0.1 * torch.randn(d, generator=g, dtype=torch.float64)).bfloat16()
+    table = ref.rope_table(128, d)
+    qo = dn.deltanet_paged_norm_rope_append(q, k, v, *b.tensors(), b.cu, w.cuda(), w.cuda(), table.cuda(), interleaved=interleaved, **b.scales())
+    pos = torch.cat([torch.arange(kv - m, kv) for m, kv in zip(b.qs, b.kvs)])
+    args = (w.double(), table, pos, 1e-6, interleaved)
+    near(qo, ref.norm_rope(q64, *args), ref.norm_rope_bound(q64, *args, "bf16"), "q")
+    y = ref.norm_rope(k64, *args)
+    err = ref.norm_rope_bound(k64, *args, "f32")    # (unrounded, but for fp32's roundings, until it takes the pages' type)
+    where = [place(b, n, kv - m + i) for n, (m, kv) in enumerate(zip(b.qs, b.kvs)) for i in range(m)]
+    take = lambda t: torch.stack([t[p, :, s] for p, s in where])  # noqa: E731
+    codes, factors = (take(t) for t in b.raw("k"))
+    # a factor and a number are those of some value within the bound of y: one factor of the two on either side, and a number no further from y than the nearest by twice the bound
+    low, high = f4.quantise(y.abs() - err)[1], f4.quantise(y.abs() + err)[1]
+    assert ((factors >= low) & (factors <= high)).all()
+    s = torch.exp2(factors.double() - 127).repeat_interleave(32, -1)
+    off = (f4.values(codes, factors) - y).abs()
+    best = ((y.abs() / s)[..., None] - f4.LEVELS).abs().amin(-1) * s
+    assert (off <= best + 2 * err).all()
+    vc, vf = (take(t) for t in b.raw("v"))
+    wc, wf = f4.quantise(v64)
+    assert torch.equal(vc, wc) and torch.equal(vf, wf)
+
+
+FEW = [([1], [1]), ([1, 1, 1], [77, 1, 200]), ([2, 0, 1, 3], [33, 64, 5, 3]), ([1] * 5, [2048, 1, 17, 500, 1030]), ([8, 7], [40, 1000])]
+WIDE = [([130], [130]), ([200, 1, 33, 0, 70], [200, 400, 97, 50, 600]), ([64, 64], [1024, 640]), ([300, 1, 1], [310, 700, 20])]
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("G", [1, 4])
+@pytest.mark.parametrize("batch", range(len(FEW) + len(WIDE)))
+def test_attention(d, G, batch):
+    qs, kvs = (FEW + WIDE)[batch]
+    page, window = [16, 64, 128][batch % 3], [0, 100, 0, 33][batch % 4]
+    b = Batch4(qs, kvs, 2, d, page=page, seed=100 * d + batch)
+    q, q64 = b.rows(2 * G)
+    o = b.attend(q, window=window, max_q=max(qs), max_kv=max(kvs))
+    b.check(o, q64, d ** -0.5, window, "d %d G %d batch %d" % (d, G, batch))
+
+
+@pytest.mark.parametrize("d,kv", [(64, 20000), (128, 9000), (256, 5000)])
+def test_long_contexts_in_pieces(d, kv):
+    b = Batch4([1, 2], [kv, kv // 3], 1, d, page=64, seed=kv)
+    q, q64 = b.rows(4)
+    b.check(b.attend(q), q64, d ** -0.5, 0, "long %d" % d)
+    b.check(b.attend(q, window=1000), q64, d ** -0.5, 1000, "long windowed %d" % d)
+
+
+def test_what_masks_hide_reaches_nothing():
+    """Pages behind a context's end and in front of all windows hold NaN factors: results are finite, and the same whatever stands there."""
+    for qs, kvs, window in (([1, 1], [50, 333], 20), ([150, 3], [700, 40], 64)):
+        b = Batch4(qs, kvs, 2, 128, page=16, seed=5)
+        q, _ = b.rows(4)
+        kw = dict(window=window)
+        for n, (m, kv) in enumerate(zip(qs, kvs)):
+            for pos in range(max(kv - m - window + 1, 0)):
+                p, slot = place(b, n, pos)
+                for w in "kv":
+                    getattr(b, w + "_scale").view(torch.uint8)[p, :, slot] = 255
+        o = b.attend(q, **kw)
+        assert torch.isfinite(o).all()
+        for w in "kv":
+            t = getattr(b, w + "_scale").view(torch.uint8)
+            t[t == 255] = 127
+        assert torch.equal(o, b.attend(q, **kw))
+
+
+def test_rows_without_a_position_or_a_sequence_become_zero():
+    b = Batch4([5, 1], [3, 30], 1, 64)
+    q, q64 = b.rows(2)
+    o = b.attend(q)
+    assert not o[:2].any() and torch.isfinite(o).all() and o[2:].any()
+    o = dn.deltanet_paged_attn_fwd(q, *b.tensors(), torch.tensor([1, 1, 2], dtype=torch.int32).cuda(), **b.scales())
+    assert not o[:1].any() and not o[2:].any() and o[1].any()
+
+
+def test_captured_steps():
+    b = Batch4([1, 20, 1], [300, 60, 1], 2, 128)
+    (q, _), (k, _), (v, _) = b.rows(4), b.rows(2), b.rows(2)
+    o = torch.empty_like(q)
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    kr, vr = torch.empty(22, 2, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(22, 2, 128, dtype=torch.bfloat16, device="cuda")
+
+    def step():
+        dn.deltanet_paged_append(k, v, *b.tensors(), b.cu, **b.scales())
+        b.attend(q, o=o, workspace=ws)
+        dn.deltanet_paged_read(*b.tensors(), b.cu, 22, k_out=kr, v_out=vr, **b.scales())
+    replays(step, [o, kr, vr], lambda: ws.fill_(0x7f))
+
+
+def test_refusals():
+    b = Batch4([1], [20], 2, 64)
+    q, _ = b.rows(2)
+    with pytest.raises(ValueError, match="4-bit"):
+        dn.deltanet_paged_attn_fwd(q, *b.tensors(), b.cu)
+    with pytest.raises(TypeError):
+        dn.deltanet_paged_attn_fwd(q, *b.tensors(), b.cu, k_scale=b.k_scale.view(torch.uint8), v_scale=b.v_scale)
+    with pytest.raises(ValueError):
+        dn.deltanet_paged_attn_fwd(q, *b.tensors(), b.cu, k_scale=b.k_scale[..., :1].contiguous(), v_scale=b.v_scale)
+    with pytest.raises(dn.DeltaNetError):
+        dn.deltanet_paged_attn_fwd(q.float(), *b.tensors(), b.cu, **b.scales())
+    with pytest.raises(TypeError):
+        dn.deltanet_paged_read(*b.tensors(), b.cu, 1, dtype=torch.float16, **b.scales())
