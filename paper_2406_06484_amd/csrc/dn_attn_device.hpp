@@ -56,9 +56,9 @@ template <int PAIR> __device__ inline unsigned fp4_pair(unsigned w, float factor
     return __builtin_bit_cast(unsigned, v);
 }
 __device__ inline u32x4 from_fp4x8(unsigned w, float factor) { return u32x4{fp4_pair<0>(w, factor), fp4_pair<1>(w, factor), fp4_pair<2>(w, factor), fp4_pair<3>(w, factor)}; }
-// The factor that a byte stands for, 2^(byte - 127); 255 is NaN, as all the group's numbers are then.  (The conversion takes the exponent alone, and a zero for
-// another number than 2^-127.)
-__device__ inline float fp4_factor(unsigned byte) { return __uint_as_float(max(byte << 23, 0x00400000u)); }
+// The factor that a byte stands for, 2^(byte - 127); 255 is NaN, as all the group's numbers are then.  (The conversions take a factor's exponent alone; without the bit below it
+// a zero would be another number than 2^-127.)
+__device__ inline float fp4_factor(unsigned byte) { return __uint_as_float(byte << 23 | 0x00400000u); }
 // The byte of the least power of two of which six, the largest e2m1 number, are enough for a group whose largest magnitude is `top`.  A group under 2^-100 is held as zeros,
 // one with an infinity or NaN as NaN.
 __device__ inline unsigned fp4_factor_byte(float top) {

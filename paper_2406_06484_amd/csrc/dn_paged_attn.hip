@@ -10,6 +10,8 @@
 // that lane, so that P never leaves its registers.
 #include "dn_attn_device.hpp"
 
+#include <type_traits>
+
 namespace dn {
 
 // How the key axis is cut: `splits` pieces of `keys` keys from the first that a row tile sees.
@@ -117,6 +119,10 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
     constexpr int KW = KB / 4, VW = VB < 4 ? 1 : VB / 4; // in words
     constexpr int KP = KB < 16 ? KB : 16, KV = KP * D / RB; // bytes, elements of a piece of a key: (4 piece + g) KV ..
     constexpr int VV = VB > 16 ? 16 * D / RB : VE;      // ... and of a value: (16 piece + col) VV ..
+    // 4-bit pages bring so many keys per byte that the vector ALU's work shows beside the reading: sums are rescaled only when a row's maximum has grown by 2^8, and
+    // probabilities enter the second product as one bf16 term.
+    constexpr bool LAZY = FP4, TWO_TERMS = !FP4;
+    constexpr int AHEAD = 1;
     constexpr int FB = FP4 ? D / kGroup : 1, FW = FP4 ? FB : 1; // factors of a row; words with those of four rows
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int Hkv = a.r.Hkv, G = a.r.Hq / Hkv;
@@ -157,34 +163,37 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
     const float c = a.scale * kLog2e;
 
     const char *kp = static_cast<const char *>(a.c.kp), *vp = static_cast<const char *>(a.c.vp);
-    unsigned kw[2][KW], vw[8][VW];
-    float4 ks[2], vs[2];
+    // `AHEAD` steps are on their way while one is worked on: step i stands in buffer i % AHEAD
+    unsigned kw_[AHEAD][2][KW], vw_[AHEAD][8][VW];
+    float4 ks_[AHEAD][2], vs_[AHEAD][2];
     // 4-bit pages: the factors' bytes, of key col's groups, and of all groups of the values 4 g .. 4 g + 3
-    unsigned kf[2][FP4 && D > 128 ? 2 : 1], vf[2][FW];
-    auto load_k = [&](int k0, const int (&page)[2]) __attribute__((always_inline)) {
+    unsigned kf_[AHEAD][2][FP4 && D > 128 ? 2 : 1], vf_[AHEAD][2][FW];
+    auto load_k = [&](int at, int k0, const int (&page)[2], int range) __attribute__((always_inline)) {
+        auto &kw = kw_[at]; auto &ks = ks_[at]; auto &kf = kf_[at];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const long row = row_of(a.c, page[h], k0 + 16 * h, kvh, Hkv);
-            load_words(kw[h], make_rsrc(kp + row * RB), col * RB + KP * g, 64);
+            load_words(kw[h], make_rsrc(kp + row * RB, range), col * RB + KP * g, 64);
             if constexpr (FP4) {
-                const __amdgpu_buffer_rsrc_t fa = make_rsrc(reinterpret_cast<const char *>(a.c.ks) + row * FB);
+                const __amdgpu_buffer_rsrc_t fa = make_rsrc(reinterpret_cast<const char *>(a.c.ks) + row * FB, range);
                 if constexpr (FB == 2) kf[h][0] = __builtin_amdgcn_raw_buffer_load_b16(fa, col * FB, 0, 0);
                 else load_words(kf[h], fa, col * FB);
             }
             if constexpr (FP8) ks[h] = *reinterpret_cast<const float4 *>(a.c.ks + row + 4 * g);
         }
     };
-    auto load_v = [&](int k0, const int (&page)[2]) __attribute__((always_inline)) {
+    auto load_v = [&](int at, int k0, const int (&page)[2], int range) __attribute__((always_inline)) {
+        auto &vw = vw_[at]; auto &vs = vs_[at]; auto &vf = vf_[at];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const long row = row_of(a.c, page[h], k0 + 16 * h, kvh, Hkv);
-            const __amdgpu_buffer_rsrc_t va = make_rsrc(vp + row * RB);
+            const __amdgpu_buffer_rsrc_t va = make_rsrc(vp + row * RB, range);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if constexpr (VB == 2) vw[4 * h + i][0] = __builtin_amdgcn_raw_buffer_load_b16(va, (4 * g + i) * RB + col * VB, 0, 0);
                 else load_words(vw[4 * h + i], va, (4 * g + i) * RB + col * (VV * RB / D), 256);
             }
-            if constexpr (FP4) load_words(vf[h], make_rsrc(reinterpret_cast<const char *>(a.c.vs) + row * FB), 4 * g * FB);
+            if constexpr (FP4) load_words(vf[h], make_rsrc(reinterpret_cast<const char *>(a.c.vs) + row * FB, range), 4 * g * FB);
             if constexpr (FP8) vs[h] = *reinterpret_cast<const float4 *>(a.c.vs + row + 4 * g);
         }
     };
@@ -194,17 +203,41 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
     for (int j = 0; j < VE; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = kNoScore, l = 0.f;
 
+    // Requests are made whether or not there is a further step, past the end of their descriptors (which costs no access) where there is none: one under a condition would be waited for where its
+    // paths meet, and with it all that was requested before.  Page entries are fetched a step before their pages.
     constexpr int STEP = WAVES * kFewKeys;
     int k0 = k_begin + wave * kFewKeys;
-    int page[2], next[2];
+    int page[AHEAD][2], entry[2];
+    auto look_up = [&](int kk) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) entry[h] = page_entry(a.c, n, kk + 16 * h);
+    };
     if (k0 < k_end) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) { page[h] = page_of(a.c, n, k0 + 16 * h); next[h] = page_of(a.c, n, k0 + STEP + 16 * h); }
-        load_k(k0, page);
-        load_v(k0, page);
+        for (int i = 0; i < AHEAD; ++i) {
+            const int kk = k0 + i * STEP < k_end ? k0 + i * STEP : k0;
+            look_up(kk);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) page[i][h] = __builtin_amdgcn_readfirstlane(page_id(a.c, entry[h]));
+            load_k(i, kk, page[i], kBufRange);
+            load_v(i, kk, page[i], kBufRange);
+        }
+        look_up(k0 + AHEAD * STEP);
+        // the query is there before the loop, which would else wait for it, and for the loads behind it, in every step
+#pragma unroll
+        for (int i = 0; i < (int)(KE * sizeof(T) / 4); ++i) asm volatile("" : "+v"(qw[i]));
     }
-    for (; k0 < k_end; k0 += STEP) {
-        const bool more = k0 + STEP < k_end;
+    auto step = [&](auto buffer) __attribute__((always_inline)) {
+        constexpr int B = decltype(buffer)::value;
+        auto &kw = kw_[B]; auto &vw = vw_[B]; auto &ks = ks_[B]; auto &vs = vs_[B]; auto &kf = kf_[B]; auto &vf = vf_[B];
+        const bool more = k0 + AHEAD * STEP < k_end;
+        const int kn = more ? k0 + AHEAD * STEP : k0, range = more ? kBufRange : 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int id = __builtin_amdgcn_readfirstlane(page_id(a.c, entry[h]));
+            page[B][h] = more ? id : page[B][h];
+        }
+        look_up(k0 + (AHEAD + 1) * STEP);
         f32x4 st[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
         // (the lane's group of a key: element (4 piece + g) KV / 32)
         float kfac[2][FP4 ? KE / KV : 1];
@@ -232,7 +265,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
             }
             if constexpr (FP8) { st[h][0] *= ks[h].x; st[h][1] *= ks[h].y; st[h][2] *= ks[h].z; st[h][3] *= ks[h].w; }
         }
-        if (more) load_k(k0 + STEP, next);
+        load_k(B, kn, page[B], range);
         if (k0 < all_from || k0 + kFewKeys - 1 > all_to) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -251,7 +284,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
             mt = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
         }
         const float mn = fmaxf(m, mt);
-        if (__any(mn > m)) {
+        if (LAZY ? __any((mt - m) * c > 8.f) : __any(mn > m)) {
             const float f = __builtin_amdgcn_exp2f((m - mn) * c);
             l *= f;
 #pragma unroll
@@ -304,7 +337,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
             for (int i = 0; i < 8; ++i) {
                 const float x = st[i >> 2][i & 3];
                 pt[i] = (bf16)x;
-                pl[i] = (bf16)(x - (float)pt[i]);
+                if constexpr (TWO_TERMS) pl[i] = (bf16)(x - (float)pt[i]);
             }
 #pragma unroll
             for (int w = 0; w < VE / 2; ++w) { // a pair of elements of eight keys -> eight keys of each element
@@ -323,15 +356,15 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
                 }
                 o[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), pt, o[2 * w], 0, 0, 0);
                 o[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), pt, o[2 * w + 1], 0, 0, 0);
+                if constexpr (!TWO_TERMS) continue;
                 o[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), pl, o[2 * w], 0, 0, 0);
                 o[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), pl, o[2 * w + 1], 0, 0, 0);
             }
         }
-        if (more) {
-            load_v(k0 + STEP, next);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) next[h] = page_of(a.c, n, k0 + 2 * STEP + 16 * h);
-        }
+        load_v(B, kn, page[B], range);
+    };
+    for (; k0 < k_end; k0 += STEP) {
+        step(std::integral_constant<int, 0>());
     }
 
     // the waves' sums: o of element (16 piece + 4 g + r) VV + j and query col stands at o[piece VV + j][r]
@@ -600,10 +633,10 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
                 for (int x = 0; x < NX; ++x) st[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x][i], q[i], i ? st[x] : f32x16{}, 0, 0, 0);
                 if (i % EVERY == EVERY - 1) {
                     __builtin_amdgcn_sched_barrier(0);
-                    if (FP4 || more) fetch(to, next, i / EVERY); // (4 bits: always; a request under a condition is waited for where its paths meet)
+                    if (more) fetch(to, next, i / EVERY);
                 }
             }
-            if (FP4 || more) look_up(next + KEYS);
+            if (more) look_up(next + KEYS);
             __builtin_amdgcn_s_setprio(0);
         }
         if constexpr (FP8)
@@ -701,9 +734,9 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
             lds_barrier();
             for (int k0 = k_begin, j = 0; k0 < k_end; k0 += KEYS, j ^= 1) {
                 if (k0 + KEYS < k_end) park(wsmem + (j ^ 1) * W::SIZE, k0 + KEYS);
-                const bool more = k0 + 2 * KEYS < k_end;
-                if (seen(k0)) work(wsmem + j * W::SIZE, k0, wsmem, k0 + 2 * KEYS, more);
-                else if (more) fetch_all(wsmem, k0 + 2 * KEYS);
+                // (requested here, on one path: between the products, as with 16 bits, the loop would wait for the requests where it joins the path without them)
+                if (k0 + 2 * KEYS < k_end) fetch_all(wsmem, k0 + 2 * KEYS);
+                if (seen(k0)) work(wsmem + j * W::SIZE, k0, wsmem, 0, false);
                 lds_barrier();
             }
         } else {
@@ -746,7 +779,7 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
 }
 
 template <typename T, typename CT, int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void k_attn_few(AttnArgs a, int tiles, Cut cut, int max_rows) {
+__global__ __launch_bounds__(64 * WAVES, __is_same(CT, fp4) && D > 128 ? 2 : 1) void k_attn_few(AttnArgs a, int tiles, Cut cut, int max_rows) {
     extern __shared__ __align__(16) unsigned char lds[];
     attend_few<T, CT, D, WAVES>(a, tiles, cut, max_rows, blockIdx.x, reinterpret_cast<float *>(lds));
 }
@@ -917,7 +950,7 @@ Plan plan_attn(int dtype, int d, const AttnArgs &a) {
     // 640 0.98, 0.96, 0.97.  (Between 256 and 512 ragged batches go either way: at 320 0.89, 0.92, 1.07.)
     const bool twice = !p.slots && (dtype == 0 ? few_twice<float>(d) : few_twice<bf16>(d)) && (blocks <= 256 || blocks >= 512) && seen > kFewWaves * kFewKeys;
     p.waves = twice ? 2 * kFewWaves : kFewWaves;
-    const long want = twice ? 256 : 512;
+    const long want = twice && !a.c.fp4 ? 256 : 512;
     p.few = p.per_seq && N ? cut_keys(seen, blocks, 64 * blocks < want ? 64 * blocks : want, least > 256 ? least : 256, kFewKeys * p.waves) : Cut{1, 128};
     return p;
 }
