@@ -1,5 +1,6 @@
 // The operators around a mixer (short convolution, output norm, block norm) in the Python module `_attention`: their C ABI called with tensors.  Work and memory belong to the tensors' device, whichever
 // is the current one.
+#include <ATen/core/DimVector.h>
 #include <c10/core/DeviceGuard.h>
 
 #include <vector>
@@ -60,7 +61,7 @@ struct Conv {
     at::Tensor copy;
     std::vector<int32_t> host;
     at::ScalarType type;
-    std::vector<int64_t> lead; // leading sizes of x
+    at::DimVector lead; // leading sizes of x
     int64_t sequences = 0;
     bool split;
     Conv(const at::Tensor &x, const at::Tensor &w, PyObject *splits, PyObject *silu, PyObject *cu_, PyObject *cu_host) : split(splits != Py_None) {
@@ -69,7 +70,7 @@ struct Conv {
         type = x.scalar_type();
         if (x.dim() != (cu ? 2 : 3)) throw Refusal{PyExc_ValueError, "x must be [B, L, C], or [T, C] with cu_seqlens"};
         const int64_t n = x.dim(), C = x.size(n - 1);
-        lead.assign(x.sizes().begin(), x.sizes().end() - 1);
+        lead.append(x.sizes().begin(), x.sizes().end() - 1);
         s.x_stride = row_step(x, "x", type, x.sizes());
         s.B = cu ? 1 : int32(x.size(0), "B"); s.L = int32(x.size(n - 2), "L"); s.C = int32(C, "C");
         if (w.dim() != 2) throw Refusal{PyExc_ValueError, "weight must be [C, W]"};
@@ -112,12 +113,12 @@ struct Conv {
             for (int i = 0; i < s.parts; ++i) s.silu[i] = truth(at[i]);
         }
     }
-    std::vector<int64_t> shape(int64_t C) const {
-        std::vector<int64_t> v(lead);
+    at::DimVector shape(int64_t C) const {
+        at::DimVector v(lead);
         v.push_back(C);
         return v;
     }
-    std::vector<int64_t> states() const { return {sequences, s.W - 1, s.C}; }
+    at::DimVector states() const { return {sequences, s.W - 1, s.C}; }
     // the tensors of the parts (given as one tensor where there is one part without splits)
     void parts(PyObject *given, const char *name, const at::Tensor &x, bool make, at::Tensor (&t)[3], void *(&p)[3]) const {
         for (int i = 0; i < s.parts; ++i) if (s.width[i] < 0) throw Refusal{PyExc_ValueError, "splits must be widths"};

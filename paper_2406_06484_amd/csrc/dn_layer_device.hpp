@@ -27,6 +27,21 @@ template <typename T, int V> struct Word {
             for (int i = 0; i < N / 4; ++i) reinterpret_cast<uint4 *>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
         }
     }
+    // past the caches
+    __device__ inline void store_once(T *p) const {
+        typedef unsigned raw __attribute__((ext_vector_type(N < 4 ? N : 4)));
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            raw r;
+#pragma unroll
+            for (int j = 0; j < (N < 4 ? N : 4); ++j) r[j] = w[i + j];
+            __builtin_nontemporal_store(r, reinterpret_cast<raw *>(p) + i / 4);
+        }
+    }
+    __device__ inline void store(T *p, bool once) const {
+        if (once) store_once(p);
+        else store(p);
+    }
     __device__ inline float get(int i) const {
         if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
         else return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);

@@ -30,6 +30,7 @@ struct OutNormArgs {
     unsigned magic;                      // row / H = mulhi(row, magic) >> shift
     int shift;
     float eps;
+    bool once;                           // whether gradients are stored past the caches (set by the launch)
 };
 
 struct BlockNormArgs {
@@ -39,6 +40,7 @@ struct BlockNormArgs {
     long x_stride, res_stride;           // elements
     int T, D;
     float scale, res_scale, eps;
+    bool once;                           // whether the stream and gradients are stored past the caches (set by the launch)
 };
 
 // All return 0 or the hipError_t of the failing launch.  dtype: 0 = fp32, 1 = bf16.

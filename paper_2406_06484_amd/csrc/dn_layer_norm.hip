@@ -15,6 +15,11 @@
 
 namespace dn {
 
+// Outputs that the caches would not hold until they are read are stored past them: gradients, and the stream, which the next block's end reads, of over kPastCaches bytes.  (Both passes in a row 10 % faster at 16384 rows of
+// 2048; a pass and the product that reads its result: 175 us instead of 178 to 184 at 16384 rows, output norm backward, and at 2048 rows 39 instead of 36, block norm backward.  y, which the next product reads, stays: 141 us
+// instead of 143.)
+constexpr long kPastCaches = 32l << 20;
+
 // --- output norm: a wave has 64 16 / (D sizeof(T)) rows (token and head) at a time
 
 template <typename T, int D> struct HeadRow {
@@ -140,10 +145,10 @@ __global__ __launch_bounds__(256) void k_out_norm_bwd(OutNormArgs a) {
             }
             Word<T, V> out;
             out.pack(f);
-            if (live) out.store(d_o + (long)row * D);
+            if (live) out.store(d_o + (long)row * D, a.once);
             if (a.gate) {
                 out.pack(dg);
-                if (live) out.store(dgate + head_row(a, D, row, a.dgate_stride));
+                if (live) out.store(dgate + head_row(a, D, row, a.dgate_stride), a.once);
             }
         }
     }
@@ -166,7 +171,7 @@ template <int WAVES> __device__ inline float row_sum(float x, float *part) {
     x = lanes_sum<64>(x);
     if constexpr (WAVES > 1) {
         if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
-        __syncthreads();
+        lds_barrier();
         x = part[0];
 #pragma unroll
         for (int i = 1; i < WAVES; ++i) x += part[i];
@@ -178,7 +183,7 @@ template <int WAVES> __device__ inline float2 row_sums(float x, float y, float *
     y = lanes_sum<64>(y);
     if constexpr (WAVES > 1) {
         if ((threadIdx.x & 63) == 0) { part[threadIdx.x >> 6] = x; part[WAVES + (threadIdx.x >> 6)] = y; }
-        __syncthreads();
+        lds_barrier();
         x = part[0];
         y = part[WAVES];
 #pragma unroll
@@ -238,7 +243,7 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_fwd(BlockNo
                 if (a.h_out) {
                     Word<RT, V> out;
                     out.pack(h[i]);
-                    out.store(static_cast<RT *>(a.h_out) + (long)row * a.D + e);
+                    out.store(static_cast<RT *>(a.h_out) + (long)row * a.D + e, a.once);
                 }
             }
         }
@@ -255,13 +260,14 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_fwd(BlockNo
                 w.store(static_cast<T *>(a.y) + (long)row * a.D + e);
             }
         }
-        if constexpr (WAVES > 1 && !POST) __syncthreads(); // (the next row's sum takes the same place)
+        if constexpr (WAVES > 1 && !POST) lds_barrier(); // (the next row's sum takes the same place)
     }
 }
 
 template <typename T, typename RT, int WAVES, int NW, bool POST>
 __global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_bwd(BlockNormArgs a) {
     constexpr int V = 16 / (int)sizeof(T), LANES = 64 * WAVES, ROWS = kBlockRows<WAVES>;
+    constexpr bool AHEAD = NW <= 2; // (a next row's words as well would not fit beside four and their sums)
     __shared__ float part[2][2 * WAVES];
     const int lane = WAVES > 1 ? threadIdx.x : threadIdx.x & 63, mine = WAVES > 1 ? 0 : threadIdx.x >> 6;
     const int words = a.D / V;
@@ -282,21 +288,29 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_bwd(BlockNo
         for (int v = 0; v < V; ++v) dw[i][v] = du[i][v] = 0.f;
     }
     const int step = gridDim.x * ROWS;
-    for (int row = blockIdx.x * ROWS + mine; row < a.T; row += step) {
+    int row = blockIdx.x * ROWS + mine;
+    struct Row {
         Word<T, V> dy[NW], x[NW];
         Word<RT, V> h[NW], dh[NW];
+    } buffer[AHEAD ? 2 : 1];
+    auto load = [&](Row &r, int at_row) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
             const int e = (lane + i * LANES) * V;
-            const long at = (long)row * a.D + e;
-            dy[i].zero(); x[i].zero(); h[i].zero(); dh[i].zero();
+            const long at = (long)at_row * a.D + e;
+            r.dy[i].zero(); r.x[i].zero(); r.h[i].zero(); r.dh[i].zero();
             if (lane + i * LANES < words) {
-                dy[i].load(static_cast<const T *>(a.dy) + at);
-                h[i].load(static_cast<const RT *>(a.h) + at);
-                if (a.dh) dh[i].load(static_cast<const RT *>(a.dh) + at);
-                if (branch) x[i].load(static_cast<const T *>(a.x) + row * a.x_stride + e);
+                r.dy[i].load(static_cast<const T *>(a.dy) + at);
+                r.h[i].load(static_cast<const RT *>(a.h) + at);
+                if (a.dh) r.dh[i].load(static_cast<const RT *>(a.dh) + at);
+                if (branch) r.x[i].load(static_cast<const T *>(a.x) + at_row * a.x_stride + e);
             }
         }
+    };
+    auto work = [&](Row &now, Row &next) __attribute__((always_inline)) {
+        auto &dy = now.dy; auto &x = now.x; auto &h = now.h; auto &dh = now.dh;
+        if constexpr (AHEAD) load(next, min(row + step, a.T - 1));
+        else load(now, row);
         // mean(h^2), mean(dz h), and of the branch mean(x^2)
         float ss = 0.f, dot = 0.f, xx = 0.f;
 #pragma unroll
@@ -346,20 +360,30 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_bwd(BlockNo
                 if (a.dx) {
                     Word<T, V> out;
                     out.pack(d);
-                    out.store(static_cast<T *>(a.dx) + at);
+                    out.store(static_cast<T *>(a.dx) + at, a.once);
                 }
                 if (a.dres) {
                     Word<RT, V> out;
                     out.pack(H[i]);
-                    out.store(static_cast<RT *>(a.dres) + at);
+                    out.store(static_cast<RT *>(a.dres) + at, a.once);
                 }
             }
         }
-        if constexpr (WAVES > 1 && !POST) __syncthreads(); // (the next row's sums take the same place)
-    }
+        if constexpr (WAVES > 1 && !POST) lds_barrier(); // (the next row's sums take the same place)
+        row += step;
+    };
+    if constexpr (AHEAD) {
+        if (row < a.T) load(buffer[0], row);
+        while (row < a.T) {
+            work(buffer[0], buffer[1]);
+            if (row >= a.T) break;
+            work(buffer[1], buffer[0]);
+        }
+    } else
+        while (row < a.T) work(buffer[0], buffer[0]);
     if (!a.dw && !a.dgate) return;
     const bool alone = gridDim.x == 1;
-    float *tw = alone ? a.dw : a.partial + (long)blockIdx.x * 2 * a.D, *tu = alone ? a.dgate : tw + a.D;
+    float *at = a.partial + (long)blockIdx.x * 2 * a.D, *tw = alone || !a.dw ? a.dw : at, *tu = alone || !a.dgate ? a.dgate : at + a.D;
     if constexpr (WAVES > 1) {
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
@@ -490,17 +514,31 @@ int out_norm_bwd_blocks(int dtype, int d, int T, int H) {
     return rows ? fewer((rows + per - 1) / per, 1024) : 1;
 }
 int block_norm_bwd_blocks(int dtype, int T, int D) {
-    const int rows = rows_of_workgroup(dtype, D);
-    return T ? fewer(((long)T + rows - 1) / rows, 1024) : 1;
+    // Eight waves to a CU, so that their sums are few: with twice as many workgroups 4101 rows of 4104 (fp32 stream, normed and gated branch) take 110 us instead of 105, with half as many 16384 rows of 2048 in
+    // bf16 118 instead of 101 (both passes).
+    const int rows = rows_of_workgroup(dtype, D), words = D / (dtype == 0 ? 4 : 8);
+    return T ? fewer(((long)T + rows - 1) / rows, words > 512 ? 256 : 512) : 1;
 }
 
+namespace {
+bool past_caches(long elements, bool wide) { return elements * (wide ? 4 : 2) > kPastCaches; }
+} // namespace
+
 int run_out_norm_fwd(int dtype, int d, const OutNormArgs &a, hipStream_t stream) { return a.T == 0 ? 0 : by_head(dtype, d, OutFwd{a, stream}); }
-int run_out_norm_bwd(int dtype, int d, const OutNormArgs &a, hipStream_t stream) { return a.T == 0 && !a.dw ? 0 : by_head(dtype, d, OutBwd{a, stream}); }
+int run_out_norm_bwd(int dtype, int d, const OutNormArgs &a, hipStream_t stream) {
+    OutNormArgs b = a;
+    b.once = past_caches((long)a.T * a.H * d, dtype == 0);
+    return a.T == 0 && !a.dw ? 0 : by_head(dtype, d, OutBwd{b, stream});
+}
 int run_block_norm_fwd(int dtype, bool wide_stream, bool post, const BlockNormArgs &a, hipStream_t stream) {
-    return a.T == 0 ? 0 : block_norm<BlockFwd>(dtype, wide_stream, post, a, stream);
+    BlockNormArgs b = a;
+    b.once = past_caches((long)a.T * a.D, dtype == 0 || wide_stream);
+    return a.T == 0 ? 0 : block_norm<BlockFwd>(dtype, wide_stream, post, b, stream);
 }
 int run_block_norm_bwd(int dtype, bool wide_stream, bool post, const BlockNormArgs &a, hipStream_t stream) {
-    return a.T == 0 && !a.dw && !a.dgate ? 0 : block_norm<BlockBwd>(dtype, wide_stream, post, a, stream);
+    BlockNormArgs b = a;
+    b.once = past_caches((long)a.T * a.D, dtype == 0 || wide_stream);
+    return a.T == 0 && !a.dw && !a.dgate ? 0 : block_norm<BlockBwd>(dtype, wide_stream, post, b, stream);
 }
 
 } // namespace dn

@@ -6,7 +6,9 @@
 // A sequence's W - 1 last rows are its final_state; rows in front of it take their gradient to dinitial_state, and a gradient with respect to final_state is
 // added to those rows' own.  z is formed again in the backward pass (W products an element, where keeping it would be another tensor of traffic).
 //
-// Bound by HBM.  A wave has V channels per lane and walks down a strip of a sequence's rows with the W - 1 rows behind it in registers, so that a row is fetched once, and W - 1
+// Bound by HBM: 16384 rows of 6144 channels in bf16 take 71 us forward (403 MB, 5.7 TB/s) and 117 backward (604 MB, 5.2 TB/s) and 4 for the weights' sums.  Workgroups that follow each other have neighbouring columns of the same
+// rows, so that what is under way at a time is whole rows (the other way round, with a kilobyte of a row each, 237 us for both passes instead of 218), and outputs are stored past the caches (193).
+// A wave has V channels per lane and walks down a strip of a sequence's rows with the W - 1 rows behind it in registers, so that a row is fetched once, and W - 1
 // more at the ends of a strip.  Strips are cut from each sequence's start: strip i of sequence n is at slot cu[n] / S + n + i, slots that are left over have
 // nothing to do, and the place of a slot is found by a search of the offsets alone.  Only a sequence's first strip touches its states, which may so be updated in place.
 #include "dn_layer_device.hpp"
@@ -62,7 +64,7 @@ struct Lane {
     int c, part, width, off;
     bool live, silu;
     template <int V> __device__ inline void find(const ConvArgs &a) {
-        c = (blockIdx.y * 64 + (threadIdx.x & 63)) * V;
+        c = (blockIdx.x * 64 + (threadIdx.x & 63)) * V;
         live = c < a.C;
         c = live ? c : a.C - V; // (loads what another lane has, stores nothing)
         part = (c >= a.at[1]) + (c >= a.at[2]);
@@ -85,7 +87,8 @@ template <typename T, int W, int V> struct Taps {
     __device__ inline float get(int v, int j) const { return w[(v * W + j) / V].get((v * W + j) % V); }
 };
 
-// R: rows of a strip.
+// Rows of a strip of the forward pass (R), and where sequences have few rows.
+constexpr int kFwdRows = 8, kFewRows = 4;
 template <typename T, int W, int V, int R>
 __global__ __launch_bounds__(256) void k_short_conv_fwd(ConvArgs a, int slots) {
     Lane ln;
@@ -95,7 +98,7 @@ __global__ __launch_bounds__(256) void k_short_conv_fwd(ConvArgs a, int slots) {
     const bool act = __any(ln.silu);
     const T *x = static_cast<const T *>(a.x) + ln.c;
     T *y = static_cast<T *>(ln.of(a.y)) + ln.off;
-    for (int slot = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); slot < slots; slot += gridDim.x * 4) {
+    for (int slot = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); slot < slots; slot += gridDim.y * 4) {
         Strip s;
         if (!strip_at(a, R, slot, &s)) continue;
         T *to = y + (long)(s.row0 + s.first) * ln.width;
@@ -155,7 +158,10 @@ __global__ __launch_bounds__(256) void k_short_conv_fwd(ConvArgs a, int slots) {
                 for (int v = 0; v < V; ++v) z[v] = ln.silu ? z[v] * sigmoid_fast_f32(z[v]) : z[v];
             Word<T, V> out;
             out.pack(z);
-            if (ln.live && r < s.rows) out.store(to + (long)r * ln.width);
+            if (ln.live && r < s.rows) {
+                if constexpr (R > kFewRows) out.store_once(to + (long)r * ln.width);
+                else out.store(to + (long)r * ln.width);
+            }
         }
     }
 }
@@ -183,7 +189,7 @@ __global__ __launch_bounds__(256) void k_short_conv_bwd(ConvArgs a, int slots, i
 #pragma unroll
         for (int j = 0; j < W; ++j) dw[j][v] = 0.f;
     }
-    for (int slot = blockIdx.x * 4 + wave; slot < slots; slot += gridDim.x * 4) {
+    for (int slot = blockIdx.y * 4 + wave; slot < slots; slot += gridDim.y * 4) {
         Strip s;
         if (!strip_at(a, S, slot, &s)) continue;
         T *to = dx + s.row0 * a.dx_stride;
@@ -263,7 +269,7 @@ __global__ __launch_bounds__(256) void k_short_conv_bwd(ConvArgs a, int slots, i
                     Word<T, V> out;
                     out.pack(d);
                     if (ln.live) {
-                        if (e >= 0) out.store(to + e * a.dx_stride);
+                        if (e >= 0) out.store_once(to + e * a.dx_stride);
                         else out.store(static_cast<T *>(a.ds0) + state + (long)(W - 1 + e) * a.C);
                     }
                 }
@@ -281,8 +287,8 @@ __global__ __launch_bounds__(256) void k_short_conv_bwd(ConvArgs a, int slots, i
         }
     __syncthreads();
     if (wave || !ln.live) return;
-    const bool alone = gridDim.x == 1; // (then these are the gradients)
-    float *tw = alone ? a.dw : a.partial + (long)blockIdx.x * ((long)a.C * (W + 1)), *tb = alone ? a.db : tw + (long)a.C * W;
+    const bool alone = gridDim.y == 1; // (then these are the gradients)
+    float *tw = alone ? a.dw : a.partial + (long)blockIdx.y * ((long)a.C * (W + 1)), *tb = alone ? a.db : tw + (long)a.C * W;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         if (tw)
@@ -328,8 +334,7 @@ long slots_of(const ConvArgs &a, int S) {
 }
 int column_blocks(const ConvArgs &a, int V) { return (a.C / V + 63) / 64; }
 
-constexpr int kFwdRows = 16, kFewRows = 4;
-constexpr int kMostBlocks = 1 << 16; // in x; waves go on to further slots
+constexpr int kMostBlocks = 1 << 15; // along the rows; waves go on to further slots
 constexpr int kBwdBlocks = 64;
 
 template <typename T, int W> int launch_fwd(ConvArgs a, hipStream_t stream) {
@@ -340,7 +345,7 @@ template <typename T, int W> int launch_fwd(ConvArgs a, hipStream_t stream) {
     const int blocks = (slots + 3) / 4;
     void *args[] = {&a, &slots};
     const void *fn = few ? reinterpret_cast<const void *>(k_short_conv_fwd<T, W, V, kFewRows>) : reinterpret_cast<const void *>(k_short_conv_fwd<T, W, V, kFwdRows>);
-    return launch("k_short_conv_fwd", fn, dim3(blocks < kMostBlocks ? blocks : kMostBlocks, column_blocks(a, V)), 256, args, stream);
+    return launch("k_short_conv_fwd", fn, dim3(column_blocks(a, V), blocks < kMostBlocks ? blocks : kMostBlocks), 256, args, stream);
 }
 
 // Rows of a strip of the backward pass.
@@ -359,7 +364,7 @@ template <typename T, int W> int launch_bwd(ConvArgs a, hipStream_t stream) {
     int S = bwd_strip(a), slots = (int)slots_of(a, S);
     const int blocks = slots ? bwd_blocks(a) : 1; // (with no sequence the gradients of weight and bias are zero)
     void *args[] = {&a, &slots, &S};
-    const int e = launch("k_short_conv_bwd", reinterpret_cast<const void *>(k_short_conv_bwd<T, W, V>), dim3(blocks, column_blocks(a, V)), 256, args, stream);
+    const int e = launch("k_short_conv_bwd", reinterpret_cast<const void *>(k_short_conv_bwd<T, W, V>), dim3(column_blocks(a, V), blocks), 256, args, stream);
     if (e || blocks == 1 || (!a.dw && !a.db)) return e;
     return run_sum_partials(a.partial, blocks, (long)a.C * (W + 1), (long)a.C * W, a.dw, a.db, stream);
 }
