@@ -38,16 +38,25 @@ __device__ inline bool strip_at(const ConvArgs &a, int S, int slot, Strip *s) {
         // rows in front of the first sequence and behind the last one count as sequences, too: offsets 0, cu[0], .. cu[N], T
         auto offset = [&](int k) { return k == 0 ? 0 : k == a.N + 2 ? a.T : min(max(a.cu[k - 1], 0), a.T); };
         const int lane = threadIdx.x & 63;
-        int lo = 0, hi = a.N + 1; // the answer, the last k with offset(k) / S + k <= slot, lies in [lo, hi]
-        while (lo < hi) {
-            const int step = (hi - lo + 63) >> 6, at = lo + (lane + 1) * step;
-            const bool over = at <= hi && offset(min(at, hi)) / S + at <= slot;
-            lo += __builtin_popcountll(__ballot(over)) * step;
-            hi = min(hi, lo + step - 1);
+        int k; // the answer, the last one with offset(k) / S + k <= slot
+        if (a.N + 3 <= 64) { // (one fetch)
+            const int own = offset(min(lane, a.N + 2));
+            k = __builtin_popcountll(__ballot(lane <= a.N + 1 && own / S + lane <= slot)) - 1;
+            k = max(k, 0);
+            s->row0 = __builtin_amdgcn_readlane(own, k);
+            s->len = max(__builtin_amdgcn_readlane(own, k + 1) - s->row0, 0);
+        } else {
+            int lo = 0, hi = a.N + 1; // it lies in [lo, hi]
+            while (lo < hi) {
+                const int step = (hi - lo + 63) >> 6, at = lo + (lane + 1) * step;
+                const bool over = at <= hi && offset(min(at, hi)) / S + at <= slot;
+                lo += __builtin_popcountll(__ballot(over)) * step;
+                hi = min(hi, lo + step - 1);
+            }
+            k = __builtin_amdgcn_readfirstlane(lo);
+            s->row0 = offset(k);
+            s->len = max(offset(k + 1) - s->row0, 0);
         }
-        const int k = __builtin_amdgcn_readfirstlane(lo);
-        s->row0 = offset(k);
-        s->len = max(offset(k + 1) - s->row0, 0);
         s->n = k - 1;
         s->none = k == 0 || k == a.N + 1;
         i = slot - (s->row0 / S + k);
