@@ -164,24 +164,25 @@ __global__ __launch_bounds__(256) void k_out_norm_bwd(OutNormArgs a) {
     for (int e = threadIdx.x; e < D; e += 256) to[e] = (part[0][e] + part[1][e]) + (part[2][e] + part[3][e]);
 }
 
-// --- block norm: WAVES waves to a row, NW words of 16 bytes (of T) a lane
+// --- block norm: LANES lanes to a row (a part of a wave, one, or some waves), NW words of 16 bytes (of T) a lane
 
-// Sums over a row's waves; `part` has a place for each of them, and is free for the next sum when a later barrier has passed.
-template <int WAVES> __device__ inline float row_sum(float x, float *part) {
-    x = lanes_sum<64>(x);
-    if constexpr (WAVES > 1) {
+// Sums over a row's lanes; `part` has a place for each of its waves, and is free for the next sum when a later barrier has passed.
+template <int LANES> __device__ inline float row_sum(float x, float *part) {
+    x = lanes_sum<LANES < 64 ? LANES : 64>(x);
+    if constexpr (LANES > 64) {
         if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
         lds_barrier();
         x = part[0];
 #pragma unroll
-        for (int i = 1; i < WAVES; ++i) x += part[i];
+        for (int i = 1; i < LANES / 64; ++i) x += part[i];
     }
     return x;
 }
-template <int WAVES> __device__ inline float2 row_sums(float x, float y, float *part) {
-    x = lanes_sum<64>(x);
-    y = lanes_sum<64>(y);
-    if constexpr (WAVES > 1) {
+template <int LANES> __device__ inline float2 row_sums(float x, float y, float *part) {
+    constexpr int WAVES = LANES / 64;
+    x = lanes_sum<LANES < 64 ? LANES : 64>(x);
+    y = lanes_sum<LANES < 64 ? LANES : 64>(y);
+    if constexpr (LANES > 64) {
         if ((threadIdx.x & 63) == 0) { part[threadIdx.x >> 6] = x; part[WAVES + (threadIdx.x >> 6)] = y; }
         lds_barrier();
         x = part[0];
@@ -192,18 +193,20 @@ template <int WAVES> __device__ inline float2 row_sums(float x, float y, float *
     return make_float2(x, y);
 }
 
-template <int WAVES> constexpr int kBlockRows = WAVES > 1 ? 1 : 4; // rows of a workgroup
-template <int WAVES> constexpr int kBlockThreads = WAVES > 1 ? 64 * WAVES : 256;
+template <int LANES> constexpr int kBlockRows = LANES > 64 ? 1 : 256 / LANES; // rows of a workgroup
+template <int LANES> constexpr int kBlockThreads = LANES > 64 ? LANES : 256;
 
-template <typename T, typename RT, int WAVES, int NW, bool POST>
-__global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_fwd(BlockNormArgs a) {
-    constexpr int V = 16 / (int)sizeof(T), LANES = 64 * WAVES;
-    __shared__ float part[2][WAVES];
-    const int lane = WAVES > 1 ? threadIdx.x : threadIdx.x & 63;
+template <typename T, typename RT, int LANES, int NW, bool POST>
+__global__ __launch_bounds__(kBlockThreads<LANES>) void k_block_norm_fwd(BlockNormArgs a) {
+    constexpr int V = 16 / (int)sizeof(T);
+    __shared__ float part[2][LANES > 64 ? LANES / 64 : 1];
+    const int lane = threadIdx.x % LANES, sub = LANES < 64 ? (threadIdx.x & 63) / LANES : 0; // (sub: the row among those of the wave, which goes on to the last of them)
     const int words = a.D / V;
     const float inv = 1.f / (float)a.D;
-    const int step = gridDim.x * kBlockRows<WAVES>;
-    for (int row = blockIdx.x * kBlockRows<WAVES> + (WAVES > 1 ? 0 : threadIdx.x >> 6); row < a.T; row += step) {
+    const int step = gridDim.x * kBlockRows<LANES>;
+    for (int first = blockIdx.x * kBlockRows<LANES> + (LANES > 64 ? 0 : (threadIdx.x >> 6) * (LANES < 64 ? 64 / LANES : 1)); first < a.T; first += step) {
+        const int row = min(first + sub, a.T - 1);
+        const bool live = LANES >= 64 || first + sub < a.T;
         Word<T, V> x[NW];
         Word<RT, V> r[NW];
         float h[NW][V];
@@ -223,7 +226,7 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_fwd(BlockNo
             for (int i = 0; i < NW; ++i)
 #pragma unroll
                 for (int v = 0; v < V; ++v) ss = fmaf(x[i].get(v), x[i].get(v), ss);
-            rx = rsqrtf(row_sum<WAVES>(ss, part[0]) * inv + a.eps);
+            rx = rsqrtf(row_sum<LANES>(ss, part[0]) * inv + a.eps);
         }
         float ss = 0.f;
 #pragma unroll
@@ -240,18 +243,18 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_fwd(BlockNo
             if (lane + i * LANES < words) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) ss = fmaf(h[i][v], h[i][v], ss);
-                if (a.h_out) {
+                if (a.h_out && live) {
                     Word<RT, V> out;
                     out.pack(h[i]);
                     out.store(static_cast<RT *>(a.h_out) + (long)row * a.D + e, a.once);
                 }
             }
         }
-        const float rh = rsqrtf(row_sum<WAVES>(ss, part[1]) * inv + a.eps);
+        const float rh = rsqrtf(row_sum<LANES>(ss, part[1]) * inv + a.eps);
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
             const int e = (lane + i * LANES) * V;
-            if (lane + i * LANES < words) {
+            if (lane + i * LANES < words && live) {
                 Word<T, V> w;
                 if (a.w) w.load(static_cast<const T *>(a.w) + e);
 #pragma unroll
@@ -260,16 +263,16 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_fwd(BlockNo
                 w.store(static_cast<T *>(a.y) + (long)row * a.D + e);
             }
         }
-        if constexpr (WAVES > 1 && !POST) lds_barrier(); // (the next row's sum takes the same place)
+        if constexpr (LANES > 64 && !POST) lds_barrier(); // (the next row's sum takes the same place)
     }
 }
 
-template <typename T, typename RT, int WAVES, int NW, bool POST>
-__global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_bwd(BlockNormArgs a) {
-    constexpr int V = 16 / (int)sizeof(T), LANES = 64 * WAVES, ROWS = kBlockRows<WAVES>;
+template <typename T, typename RT, int LANES, int NW, bool POST>
+__global__ __launch_bounds__(kBlockThreads<LANES>) void k_block_norm_bwd(BlockNormArgs a) {
+    constexpr int V = 16 / (int)sizeof(T), ROWS = kBlockRows<LANES>;
     constexpr bool AHEAD = NW <= 2; // (a next row's words as well would not fit beside four and their sums)
-    __shared__ float part[2][2 * WAVES];
-    const int lane = WAVES > 1 ? threadIdx.x : threadIdx.x & 63, mine = WAVES > 1 ? 0 : threadIdx.x >> 6;
+    __shared__ float part[2][LANES > 64 ? LANES / 32 : 1];
+    const int lane = threadIdx.x % LANES, mine = LANES > 64 ? 0 : threadIdx.x >> 6, sub = LANES < 64 ? (threadIdx.x & 63) / LANES : 0; // (the wave; the row among its rows)
     const int words = a.D / V;
     const float inv = 1.f / (float)a.D;
     const bool branch = POST || a.gate;
@@ -288,12 +291,13 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_bwd(BlockNo
         for (int v = 0; v < V; ++v) dw[i][v] = du[i][v] = 0.f;
     }
     const int step = gridDim.x * ROWS;
-    int row = blockIdx.x * ROWS + mine;
+    int first = blockIdx.x * ROWS + mine * (LANES < 64 ? 64 / LANES : 1);
     struct Row {
         Word<T, V> dy[NW], x[NW];
         Word<RT, V> h[NW], dh[NW];
     } buffer[AHEAD ? 2 : 1];
-    auto load = [&](Row &r, int at_row) __attribute__((always_inline)) {
+    auto load = [&](Row &r, int of) __attribute__((always_inline)) {
+        const int at_row = min(of + sub, a.T - 1);
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
             const int e = (lane + i * LANES) * V;
@@ -309,8 +313,10 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_bwd(BlockNo
     };
     auto work = [&](Row &now, Row &next) __attribute__((always_inline)) {
         auto &dy = now.dy; auto &x = now.x; auto &h = now.h; auto &dh = now.dh;
-        if constexpr (AHEAD) load(next, min(row + step, a.T - 1));
-        else load(now, row);
+        const int row = first + sub;
+        const bool live = LANES >= 64 || row < a.T;
+        if constexpr (AHEAD) load(next, min(first + step, a.T - 1));
+        else load(now, first);
         // mean(h^2), mean(dz h), and of the branch mean(x^2)
         float ss = 0.f, dot = 0.f, xx = 0.f;
 #pragma unroll
@@ -322,7 +328,7 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_bwd(BlockNo
                 dot = fmaf(g, f, dot);
                 if constexpr (POST) xx = fmaf(x[i].get(v), x[i].get(v), xx);
             }
-        const float2 s = row_sums<WAVES>(ss, dot, part[0]);
+        const float2 s = row_sums<LANES>(ss, dot, part[0]);
         const float r = rsqrtf(s.x * inv + a.eps), m = s.y * r * inv;
         float H[NW][V];
 #pragma unroll
@@ -331,7 +337,7 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_bwd(BlockNo
             for (int v = 0; v < V; ++v) {
                 const float q = h[i].get(v) * r, g = dy[i].get(v);
                 H[i][v] = fmaf(r, fmaf(-q, m, a.w ? g * w[i].get(v) : g), dh[i].get(v));
-                dw[i][v] = fmaf(g, q, dw[i][v]);
+                if (live) dw[i][v] = fmaf(g, q, dw[i][v]);
             }
         float rx = 1.f, mx = 0.f;
         if constexpr (POST) {
@@ -340,7 +346,7 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_bwd(BlockNo
             for (int i = 0; i < NW; ++i)
 #pragma unroll
                 for (int v = 0; v < V; ++v) bx = fmaf(a.gate ? H[i][v] * u[i].get(v) : H[i][v], x[i].get(v), bx);
-            const float2 sx = row_sums<WAVES>(xx, bx * a.scale, part[1]);
+            const float2 sx = row_sums<LANES>(xx, bx * a.scale, part[1]);
             rx = rsqrtf(sx.x * inv + a.eps);
             mx = sx.y * rx * inv;
         }
@@ -352,11 +358,11 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_bwd(BlockNo
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const float n = x[i].get(v) * rx, b = a.scale * (a.gate ? u[i].get(v) * H[i][v] : H[i][v]);
-                du[i][v] = fmaf(H[i][v], n, du[i][v]);
+                if (live) du[i][v] = fmaf(H[i][v], n, du[i][v]);
                 d[v] = POST ? rx * fmaf(-n, mx, b) : b;
                 H[i][v] *= a.res_scale;
             }
-            if (lane + i * LANES < words) {
+            if (lane + i * LANES < words && live) {
                 if (a.dx) {
                     Word<T, V> out;
                     out.pack(d);
@@ -369,22 +375,22 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_bwd(BlockNo
                 }
             }
         }
-        if constexpr (WAVES > 1 && !POST) lds_barrier(); // (the next row's sums take the same place)
-        row += step;
+        if constexpr (LANES > 64 && !POST) lds_barrier(); // (the next row's sums take the same place)
+        first += step;
     };
     if constexpr (AHEAD) {
-        if (row < a.T) load(buffer[0], row);
-        while (row < a.T) {
+        if (first < a.T) load(buffer[0], first);
+        while (first < a.T) {
             work(buffer[0], buffer[1]);
-            if (row >= a.T) break;
+            if (first >= a.T) break;
             work(buffer[1], buffer[0]);
         }
     } else
-        while (row < a.T) work(buffer[0], buffer[0]);
+        while (first < a.T) work(buffer[0], buffer[0]);
     if (!a.dw && !a.dgate) return;
     const bool alone = gridDim.x == 1;
     float *at = a.partial + (long)blockIdx.x * 2 * a.D, *tw = alone || !a.dw ? a.dw : at, *tu = alone || !a.dgate ? a.dgate : at + a.D;
-    if constexpr (WAVES > 1) {
+    if constexpr (LANES > 64) {
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
             const int e = (lane + i * LANES) * V;
@@ -397,15 +403,21 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void k_block_norm_bwd(BlockNo
             }
         }
     } else {
-        // the four waves' rows, in their order
-        __shared__ float sums[3][2 * NW * V][64];
-        if (mine)
+        // the rows of a wave, then the four waves, in their order
+        __shared__ float sums[3][2 * NW * V][LANES];
+#pragma unroll
+        for (int i = 0; i < NW; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int m = LANES; m < 64; m <<= 1) { dw[i][v] += __shfl_xor(dw[i][v], m); du[i][v] += __shfl_xor(du[i][v], m); }
+        if (mine && sub == 0)
 #pragma unroll
             for (int i = 0; i < NW; ++i)
 #pragma unroll
                 for (int v = 0; v < V; ++v) { sums[mine - 1][i * V + v][lane] = dw[i][v]; sums[mine - 1][NW * V + i * V + v][lane] = du[i][v]; }
         __syncthreads();
-        if (mine) return;
+        if (mine || sub) return;
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
             const int e = (lane + i * LANES) * V;
@@ -468,36 +480,39 @@ struct OutBwd {
     }
 };
 
-// f<T, WAVES, NW>() for rows of D elements
+// f<T, LANES, NW>() for rows of D elements
 template <typename T, typename F> int by_width(int D, F f) {
     const int words = D / (16 / (int)sizeof(T));
-    if (words <= 64) return f.template operator()<T, 1, 1>();
-    if (words <= 128) return f.template operator()<T, 1, 2>();
-    if (words <= 256) return f.template operator()<T, 4, 1>();
-    if (words <= 512) return f.template operator()<T, 4, 2>();
-    if (words <= 1024) return f.template operator()<T, 8, 2>();
+    if (words <= 8) return f.template operator()<T, 8, 1>();
+    if (words <= 16) return f.template operator()<T, 16, 1>();
+    if (words <= 32) return f.template operator()<T, 32, 1>();
+    if (words <= 64) return f.template operator()<T, 64, 1>();
+    if (words <= 128) return f.template operator()<T, 64, 2>();
+    if (words <= 256) return f.template operator()<T, 256, 1>();
+    if (words <= 512) return f.template operator()<T, 256, 2>();
+    if (words <= 1024) return f.template operator()<T, 512, 2>();
     if constexpr (sizeof(T) == 4) // (bf16 rows of that many words would not fit a wave's registers)
-        if (words <= 2048) return f.template operator()<T, 8, 4>();
+        if (words <= 2048) return f.template operator()<T, 512, 4>();
     return (int)hipErrorInvalidValue;
 }
-int rows_of_workgroup(int dtype, int D) { return D / (dtype == 0 ? 4 : 8) <= 128 ? 4 : 1; }
+int rows_of_workgroup(int words) { return words <= 8 ? 32 : words <= 16 ? 16 : words <= 32 ? 8 : words <= 128 ? 4 : 1; }
 
 template <typename RT, bool POST> struct BlockFwd {
     BlockNormArgs a;
     hipStream_t stream;
-    template <typename T, int WAVES, int NW> int operator()() {
+    template <typename T, int LANES, int NW> int operator()() {
         void *args[] = {&a};
-        return launch("k_block_norm_fwd", reinterpret_cast<const void *>(k_block_norm_fwd<T, RT, WAVES, NW, POST>), fewer(((long)a.T + kBlockRows<WAVES> - 1) / kBlockRows<WAVES>, 1 << 16),
-                      kBlockThreads<WAVES>, args, stream);
+        return launch("k_block_norm_fwd", reinterpret_cast<const void *>(k_block_norm_fwd<T, RT, LANES, NW, POST>), fewer(((long)a.T + kBlockRows<LANES> - 1) / kBlockRows<LANES>, 1 << 16),
+                      kBlockThreads<LANES>, args, stream);
     }
 };
 template <typename RT, bool POST> struct BlockBwd {
     BlockNormArgs a;
     hipStream_t stream;
-    template <typename T, int WAVES, int NW> int operator()() {
+    template <typename T, int LANES, int NW> int operator()() {
         const int blocks = block_norm_bwd_blocks(sizeof(T) == 4 ? 0 : 1, a.T, a.D);
         void *args[] = {&a};
-        const int e = launch("k_block_norm_bwd", reinterpret_cast<const void *>(k_block_norm_bwd<T, RT, WAVES, NW, POST>), blocks, kBlockThreads<WAVES>, args, stream);
+        const int e = launch("k_block_norm_bwd", reinterpret_cast<const void *>(k_block_norm_bwd<T, RT, LANES, NW, POST>), blocks, kBlockThreads<LANES>, args, stream);
         return e || blocks == 1 || (!a.dw && !a.dgate) ? e : run_sum_partials(a.partial, blocks, 2 * (long)a.D, a.D, a.dw, a.dgate, stream);
     }
 };
@@ -516,7 +531,7 @@ int out_norm_bwd_blocks(int dtype, int d, int T, int H) {
 int block_norm_bwd_blocks(int dtype, int T, int D) {
     // Eight waves to a CU, so that their sums are few: with twice as many workgroups 4101 rows of 4104 (fp32 stream, normed and gated branch) take 110 us instead of 105, with half as many 16384 rows of 2048 in
     // bf16 118 instead of 101 (both passes).
-    const int rows = rows_of_workgroup(dtype, D), words = D / (dtype == 0 ? 4 : 8);
+    const int words = D / (dtype == 0 ? 4 : 8), rows = rows_of_workgroup(words);
     return T ? fewer(((long)T + rows - 1) / rows, words > 512 ? 256 : 512) : 1;
 }
 

@@ -344,7 +344,6 @@ long slots_of(const ConvArgs &a, int S) {
 int column_blocks(const ConvArgs &a, int V) { return (a.C / V + 63) / 64; }
 
 constexpr int kMostBlocks = 1 << 15; // along the rows; waves go on to further slots
-constexpr int kBwdBlocks = 64;
 
 template <typename T, int W> int launch_fwd(ConvArgs a, hipStream_t stream) {
     constexpr int V = 16 / (int)sizeof(T);
@@ -357,21 +356,24 @@ template <typename T, int W> int launch_fwd(ConvArgs a, hipStream_t stream) {
     return launch("k_short_conv_fwd", fn, dim3(column_blocks(a, V), blocks < kMostBlocks ? blocks : kMostBlocks), 256, args, stream);
 }
 
-// Rows of a strip of the backward pass.
-int bwd_strip(const ConvArgs &a) {
+// Rows of a strip of the backward pass, as long as there are strips for 4096 waves; workgroups along the rows, up to 1024 in all, or 64 where there are many columns (their sums are traffic,
+// too).  16000 rows of 64 channels, both passes: by 64 workgroups 42 us, by 500 16.
+int bwd_columns(int dtype, const ConvArgs &a) { return column_blocks(a, dtype == 0 ? kBwdV<float> : kBwdV<bf16>); }
+int bwd_strip(int dtype, const ConvArgs &a) {
     int S = 64;
-    while (S > kBwdBatch && (long)a.T / S * column_blocks(a, 8) < 2048) S /= 2;
+    while (S > kBwdBatch && (long)a.T / S * bwd_columns(dtype, a) < 4096) S /= 2;
     return S;
 }
-int bwd_blocks(const ConvArgs &a) {
-    const long blocks = (slots_of(a, bwd_strip(a)) + 3) / 4;
-    return (int)(blocks < kBwdBlocks ? blocks : kBwdBlocks);
+int bwd_blocks(int dtype, const ConvArgs &a) {
+    const long blocks = (slots_of(a, bwd_strip(dtype, a)) + 3) / 4, wide = 1024 / bwd_columns(dtype, a), most = wide > 64 ? wide : 64;
+    return (int)(blocks < most ? blocks : most);
 }
 
 template <typename T, int W> int launch_bwd(ConvArgs a, hipStream_t stream) {
     constexpr int V = kBwdV<T>;
-    int S = bwd_strip(a), slots = (int)slots_of(a, S);
-    const int blocks = slots ? bwd_blocks(a) : 1; // (with no sequence the gradients of weight and bias are zero)
+    const int dtype = sizeof(T) == 4 ? 0 : 1;
+    int S = bwd_strip(dtype, a), slots = (int)slots_of(a, S);
+    const int blocks = slots ? bwd_blocks(dtype, a) : 1; // (with no sequence the gradients of weight and bias are zero)
     void *args[] = {&a, &slots, &S};
     const int e = launch("k_short_conv_bwd", reinterpret_cast<const void *>(k_short_conv_bwd<T, W, V>), dim3(column_blocks(a, V), blocks), 256, args, stream);
     if (e || blocks == 1 || (!a.dw && !a.db)) return e;
@@ -380,7 +382,7 @@ template <typename T, int W> int launch_bwd(ConvArgs a, hipStream_t stream) {
 
 } // namespace
 
-int short_conv_bwd_blocks(int, const ConvArgs &a) { return bwd_blocks(a); }
+int short_conv_bwd_blocks(int dtype, const ConvArgs &a) { return bwd_blocks(dtype, a); }
 
 int run_short_conv_fwd(int dtype, const ConvArgs &a, hipStream_t stream) {
     if (dtype == 0) return a.W == 2 ? launch_fwd<float, 2>(a, stream) : a.W == 3 ? launch_fwd<float, 3>(a, stream) : launch_fwd<float, 4>(a, stream);

@@ -75,7 +75,7 @@ def test_output_norm_dense_rows_and_gates_of_every_size():
     near(dg.flatten(0, 1), *gg, "dgate")
 
 
-WIDTHS = [(1, 8), (3, 64), (9, 504), (130, 512), (6, 520), (5, 1024), (17, 1032), (33, 2048), (4, 2056), (3, 4096), (7, 4104), (5, 8192), (0, 64)]
+WIDTHS = [(1, 8), (3, 64), (9, 504), (130, 512), (6, 520), (5, 1024), (17, 1032), (33, 2048), (4, 2056), (3, 4096), (7, 4104), (5, 8192), (0, 64), (70, 24), (77, 128), (1030, 136), (35, 256), (1, 200), (4099, 32)]
 
 
 @pytest.mark.parametrize("dtype,stream", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
