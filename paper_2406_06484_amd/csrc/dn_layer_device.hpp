@@ -5,7 +5,7 @@
 
 namespace dn {
 
-// V elements of type T as they are loaded and stored: V sizeof(T) is 8 or 16 bytes.
+// V elements of type T as they are loaded and stored: V sizeof(T) is 4, 8 or a multiple of 16 bytes.
 template <typename T, int V> struct Word {
     static constexpr int N = V * (int)sizeof(T) / 4;
     unsigned w[N];
@@ -14,14 +14,16 @@ template <typename T, int V> struct Word {
         for (int i = 0; i < N; ++i) w[i] = 0;
     }
     __device__ inline void load(const T *p) {
-        if constexpr (N == 2) { const uint2 x = *reinterpret_cast<const uint2 *>(p); w[0] = x.x; w[1] = x.y; }
+        if constexpr (N == 1) w[0] = *reinterpret_cast<const unsigned *>(p);
+        else if constexpr (N == 2) { const uint2 x = *reinterpret_cast<const uint2 *>(p); w[0] = x.x; w[1] = x.y; }
         else {
 #pragma unroll
             for (int i = 0; i < N / 4; ++i) { const uint4 x = reinterpret_cast<const uint4 *>(p)[i]; w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w; }
         }
     }
     __device__ inline void store(T *p) const {
-        if constexpr (N == 2) *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+        if constexpr (N == 1) *reinterpret_cast<unsigned *>(p) = w[0];
+        else if constexpr (N == 2) *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
         else {
 #pragma unroll
             for (int i = 0; i < N / 4; ++i) reinterpret_cast<uint4 *>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
@@ -51,6 +53,10 @@ template <typename T, int V> struct Word {
         for (int i = 0; i < V; ++i) f[i] = get(i);
     }
     __device__ inline void pack(const float (&f)[V]) {
+        if constexpr (V == 1) {
+            w[0] = __float_as_uint(f[0]);
+            return;
+        }
         typedef T vec __attribute__((ext_vector_type(V)));
         typedef unsigned raw __attribute__((ext_vector_type(N)));
         vec v;

@@ -524,15 +524,18 @@ template <template <typename, bool> class L> int block_norm(int dtype, bool wide
 
 } // namespace
 
+// Rounds of a workgroup's rows up to which one workgroup has all of a backward pass and so its vectors' sums: it saves a launch and the partial sums' memory.
+constexpr int kAloneRounds = 4;
+
 int out_norm_bwd_blocks(int dtype, int d, int T, int H) {
     const long rows = (long)T * H, per = out_rows(dtype, d, kOutBwdBatch);
-    return rows ? fewer((rows + per - 1) / per, 1024) : 1;
+    return rows > kAloneRounds * per ? fewer((rows + per - 1) / per, 1024) : 1;
 }
 int block_norm_bwd_blocks(int dtype, int T, int D) {
     // Eight waves to a CU, so that their sums are few: with twice as many workgroups 4101 rows of 4104 (fp32 stream, normed and gated branch) take 110 us instead of 105, with half as many 16384 rows of 2048 in
     // bf16 118 instead of 101 (both passes).
     const int words = D / (dtype == 0 ? 4 : 8), rows = rows_of_workgroup(words);
-    return T ? fewer(((long)T + rows - 1) / rows, words > 512 ? 256 : 512) : 1;
+    return T > kAloneRounds * rows ? fewer(((long)T + rows - 1) / rows, words > 512 ? 256 : 512) : 1;
 }
 
 namespace {

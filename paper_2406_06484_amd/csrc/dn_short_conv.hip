@@ -154,30 +154,31 @@ __global__ __launch_bounds__(256) void k_short_conv_fwd(ConvArgs a, int slots) {
             }
         }
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float z[V];
+        for (int r = 0; r < R; ++r)
+            if (R > kFewRows || r < s.rows) { // (in a long strip the branch costs more than the last strip's missing rows)
+                float z[V];
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                z[v] = taps.b.get(v);
+                for (int v = 0; v < V; ++v) {
+                    z[v] = taps.b.get(v);
 #pragma unroll
-                for (int j = 0; j < W; ++j) z[v] = fmaf(taps.get(v, j), in[r + j].get(v), z[v]);
+                    for (int j = 0; j < W; ++j) z[v] = fmaf(taps.get(v, j), in[r + j].get(v), z[v]);
+                }
+                if (act)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) z[v] = ln.silu ? z[v] * sigmoid_fast_f32(z[v]) : z[v];
+                Word<T, V> out;
+                out.pack(z);
+                if (ln.live && r < s.rows) {
+                    if constexpr (R > kFewRows) out.store_once(to + (long)r * ln.width);
+                    else out.store(to + (long)r * ln.width);
+                }
             }
-            if (act)
-#pragma unroll
-                for (int v = 0; v < V; ++v) z[v] = ln.silu ? z[v] * sigmoid_fast_f32(z[v]) : z[v];
-            Word<T, V> out;
-            out.pack(z);
-            if (ln.live && r < s.rows) {
-                if constexpr (R > kFewRows) out.store_once(to + (long)r * ln.width);
-                else out.store(to + (long)r * ln.width);
-            }
-        }
     }
 }
 
 // Rows that are requested together in the backward pass; strips are S rows, a multiple of it.
 constexpr int kBwdBatch = 8;
-template <typename T> constexpr int kBwdV = 8 / (int)sizeof(T);
+
 
 template <typename T, int W, int V>
 __global__ __launch_bounds__(256) void k_short_conv_bwd(ConvArgs a, int slots, int S) {
@@ -345,44 +346,50 @@ int column_blocks(const ConvArgs &a, int V) { return (a.C / V + 63) / 64; }
 
 constexpr int kMostBlocks = 1 << 15; // along the rows; waves go on to further slots
 
+// Bytes of a row that a lane has: 16 forward and 8 backward (more registers), half of that where there are no two waves for each SIMD, which a strip's instructions then keep busy longer than the memory does.
+constexpr long kFewWaves = 2048;
+
+template <typename T, int W, int R> const void *fwd_of(bool thin) {
+    return thin ? reinterpret_cast<const void *>(k_short_conv_fwd<T, W, 8 / (int)sizeof(T), R>) : reinterpret_cast<const void *>(k_short_conv_fwd<T, W, 16 / (int)sizeof(T), R>);
+}
 template <typename T, int W> int launch_fwd(ConvArgs a, hipStream_t stream) {
-    constexpr int V = 16 / (int)sizeof(T);
     const bool few = (long)a.T <= (long)kFewRows * a.N;
     int slots = (int)slots_of(a, few ? kFewRows : kFwdRows);
     if (!slots) return 0;
-    const int blocks = (slots + 3) / 4;
+    const bool thin = (long)slots * column_blocks(a, 16 / (int)sizeof(T)) < kFewWaves;
+    const int blocks = (slots + 3) / 4, columns = column_blocks(a, (thin ? 8 : 16) / (int)sizeof(T));
     void *args[] = {&a, &slots};
-    const void *fn = few ? reinterpret_cast<const void *>(k_short_conv_fwd<T, W, V, kFewRows>) : reinterpret_cast<const void *>(k_short_conv_fwd<T, W, V, kFwdRows>);
-    return launch("k_short_conv_fwd", fn, dim3(column_blocks(a, V), blocks < kMostBlocks ? blocks : kMostBlocks), 256, args, stream);
+    return launch("k_short_conv_fwd", few ? fwd_of<T, W, kFewRows>(thin) : fwd_of<T, W, kFwdRows>(thin), dim3(columns, blocks < kMostBlocks ? blocks : kMostBlocks), 256, args, stream);
 }
 
-// Rows of a strip of the backward pass, as long as there are strips for 4096 waves; workgroups along the rows, up to 1024 in all, or 64 where there are many columns (their sums are traffic,
-// too).  16000 rows of 64 channels, both passes: by 64 workgroups 42 us, by 500 16.
-int bwd_columns(int dtype, const ConvArgs &a) { return column_blocks(a, dtype == 0 ? kBwdV<float> : kBwdV<bf16>); }
-int bwd_strip(int dtype, const ConvArgs &a) {
-    int S = 64;
-    while (S > kBwdBatch && (long)a.T / S * bwd_columns(dtype, a) < 4096) S /= 2;
-    return S;
-}
-int bwd_blocks(int dtype, const ConvArgs &a) {
-    const long blocks = (slots_of(a, bwd_strip(dtype, a)) + 3) / 4, wide = 1024 / bwd_columns(dtype, a), most = wide > 64 ? wide : 64;
-    return (int)(blocks < most ? blocks : most);
+// The backward pass's split.  Strips are as long as there are 4096 of them and columns.  Workgroups along the rows: up to 1024 in all, or 64 where there are many columns (their sums are traffic, too):
+// 16000 rows of 64 channels, both passes, by 64 workgroups 42 us, by 500 16.
+struct BwdPlan { int strip, slots, blocks, columns; bool thin; };
+BwdPlan bwd_plan(int dtype, const ConvArgs &a) {
+    const int V = dtype == 0 ? 2 : 4, wide = column_blocks(a, V);
+    BwdPlan p;
+    p.strip = 64;
+    while (p.strip > kBwdBatch && (long)a.T / p.strip * wide < 4096) p.strip /= 2;
+    p.slots = (int)slots_of(a, p.strip);
+    p.thin = (long)p.slots * wide < kFewWaves;
+    p.columns = p.thin ? column_blocks(a, V / 2) : wide;
+    const int blocks = (p.slots + 3) / 4, most = 1024 / p.columns > 64 ? 1024 / p.columns : 64;
+    p.blocks = blocks < 1 ? 1 : blocks < most ? blocks : most; // (with no sequence the gradients of weight and bias are zero)
+    return p;
 }
 
 template <typename T, int W> int launch_bwd(ConvArgs a, hipStream_t stream) {
-    constexpr int V = kBwdV<T>;
-    const int dtype = sizeof(T) == 4 ? 0 : 1;
-    int S = bwd_strip(dtype, a), slots = (int)slots_of(a, S);
-    const int blocks = slots ? bwd_blocks(dtype, a) : 1; // (with no sequence the gradients of weight and bias are zero)
-    void *args[] = {&a, &slots, &S};
-    const int e = launch("k_short_conv_bwd", reinterpret_cast<const void *>(k_short_conv_bwd<T, W, V>), dim3(column_blocks(a, V), blocks), 256, args, stream);
-    if (e || blocks == 1 || (!a.dw && !a.db)) return e;
-    return run_sum_partials(a.partial, blocks, (long)a.C * (W + 1), (long)a.C * W, a.dw, a.db, stream);
+    BwdPlan p = bwd_plan(sizeof(T) == 4 ? 0 : 1, a);
+    void *args[] = {&a, &p.slots, &p.strip};
+    const void *fn = p.thin ? reinterpret_cast<const void *>(k_short_conv_bwd<T, W, 4 / (int)sizeof(T)>) : reinterpret_cast<const void *>(k_short_conv_bwd<T, W, 8 / (int)sizeof(T)>);
+    const int e = launch("k_short_conv_bwd", fn, dim3(p.columns, p.blocks), 256, args, stream);
+    if (e || p.blocks == 1 || (!a.dw && !a.db)) return e;
+    return run_sum_partials(a.partial, p.blocks, (long)a.C * (W + 1), (long)a.C * W, a.dw, a.db, stream);
 }
 
 } // namespace
 
-int short_conv_bwd_blocks(int dtype, const ConvArgs &a) { return bwd_blocks(dtype, a); }
+int short_conv_bwd_blocks(int dtype, const ConvArgs &a) { return bwd_plan(dtype, a).blocks; }
 
 int run_short_conv_fwd(int dtype, const ConvArgs &a, hipStream_t stream) {
     if (dtype == 0) return a.W == 2 ? launch_fwd<float, 2>(a, stream) : a.W == 3 ? launch_fwd<float, 3>(a, stream) : launch_fwd<float, 4>(a, stream);
