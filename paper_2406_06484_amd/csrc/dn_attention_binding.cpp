@@ -119,6 +119,7 @@ PyObject *norm_rope_fwd(Args a) {
     const at::Tensor *qw = maybe(a[2], "q_weight"), *kw = maybe(a[3], "k_weight"), *table = maybe(a[4], "rope"), *pos = maybe(a[5], "positions");
     const at::Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k");
     const QK x(q, k, pos);
+    const c10::DeviceGuard on(q.device());
     const dn_rope r = rope_of(table, a[6], a[7]);
     weights(qw, kw, x.type, x.s.d);
     const at::Tensor qo = out(maybe(a[8], "q_out"), "q_out", q.sizes(), q, x.type), ko = out(maybe(a[9], "k_out"), "k_out", k.sizes(), q, x.type);
@@ -131,6 +132,7 @@ PyObject *norm_rope_bwd(Args a) {
     const at::Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k"), &dqo = tensor(a[2], "dq_out"), &dko = tensor(a[3], "dk_out");
     const at::Tensor *qw = maybe(a[4], "q_weight"), *kw = maybe(a[5], "k_weight"), *table = maybe(a[6], "rope"), *pos = maybe(a[7], "positions");
     const QK x(q, k, pos);
+    const c10::DeviceGuard on(q.device());
     const dn_rope r = rope_of(table, a[8], a[9]);
     weights(qw, kw, x.type, x.s.d);
     whole(dqo, "dq_out", x.type, q.sizes());
@@ -153,6 +155,7 @@ PyObject *norm_rope_bwd(Args a) {
 PyObject *append(Args a) {
     const at::Tensor &k = tensor(a[0], "k"), &v = tensor(a[1], "v");
     Paged p(a[2], a[3], a[4], a[5], a[6], a[7], a[8], type_of(k, "k"));
+    const c10::DeviceGuard on(k.device());
     const int64_t T = first_size(k, "k");
     p.s.T = int32(T, "T"); p.s.Hq = p.s.Hkv;
     p.s.k_stride = rows(k, "k", k.scalar_type(), T, p.s.Hkv, p.s.d);
@@ -166,6 +169,7 @@ PyObject *norm_rope_append(Args a) {
     const at::Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k"), &v = tensor(a[2], "v");
     const at::Tensor *qw = maybe(a[8], "q_weight"), *kw = maybe(a[9], "k_weight"), *table = maybe(a[10], "rope");
     Paged p(a[3], a[4], a[5], a[6], a[7], a[11], a[12], type_of(q, "q"));
+    const c10::DeviceGuard on(q.device());
     const at::ScalarType type = q.scalar_type();
     const int64_t T = first_size(q, "q"), Hq = q.size(1);
     p.s.T = int32(T, "T"); p.s.Hq = int32(Hq, "heads");
@@ -183,6 +187,7 @@ PyObject *read(Args a) { // dtype as a dn_dtype
     const at::Tensor &kp = tensor(a[0], "k_pages");
     const int dtype = (int)integer(a[6], "dtype");
     Paged p(a[0], a[1], a[2], a[3], a[4], a[7], a[8], dtype);
+    const c10::DeviceGuard on(kp.device());
     const int32_t T = int32(integer(a[5], "rows"), "rows");
     if (T < 0) return PyLong_FromLong(DN_ERR_SHAPE);
     p.s.Hq = p.s.Hkv;
@@ -195,6 +200,7 @@ PyObject *read(Args a) { // dtype as a dn_dtype
 PyObject *attn(Args a) {
     const at::Tensor &q = tensor(a[0], "q");
     Paged p(a[1], a[2], a[3], a[4], a[5], a[6], a[7], type_of(q, "q"));
+    const c10::DeviceGuard on(q.device());
     const int64_t T = first_size(q, "q"), Hq = q.size(1);
     p.s.T = int32(T, "T"); p.s.Hq = int32(Hq, "heads");
     p.s.q_stride = rows(q, "q", q.scalar_type(), T, Hq, p.s.d);

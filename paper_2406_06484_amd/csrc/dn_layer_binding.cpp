@@ -1,8 +1,6 @@
 // The operators around a mixer (short convolution, output norm, block norm) in the Python module `_attention`: their C ABI called with tensors.  Work and memory belong to the tensors' device, whichever
 // is the current one.
-#include <ATen/EmptyTensor.h>
 #include <ATen/core/DimVector.h>
-#include <c10/core/DeviceGuard.h>
 
 #include <vector>
 
@@ -28,35 +26,6 @@ void together(const at::Tensor &with, std::initializer_list<const at::Tensor *> 
     for (const at::Tensor *t : ts)
         if (t && t->device() != with.device()) throw Refusal{PyExc_ValueError, "all tensors must be on one device"};
 }
-
-// A new tensor on the current device, which is that of `like` (a DeviceGuard of the function's), from like's own allocator: past torch's dispatcher, which takes as long as the allocation (a
-// small call makes two to six of them, at half a microsecond each instead of one).
-at::Tensor fresh(at::IntArrayRef shape, const at::Tensor &like, at::ScalarType type) {
-    at::Allocator *from = like.has_storage() ? like.storage().allocator() : nullptr; // (none where the memory came from elsewhere)
-    if (!from) return at::empty(shape, like.options().dtype(type));
-    return at::detail::empty_generic(shape, from, c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt);
-}
-at::Tensor result(const at::Tensor *given, const char *name, at::IntArrayRef shape, const at::Tensor &like, at::ScalarType type) {
-    if (!given) return fresh(shape, like, type);
-    whole(*given, name, type, shape);
-    return *given;
-}
-// the caller's workspace, or one for this call (none if none is needed)
-struct Work {
-    at::Tensor held;
-    size_t bytes = 0;
-    Work(const at::Tensor *given, size_t need, const at::Tensor &like) {
-        if (given || !need) {
-            const Scratch s(given, 0, like);
-            held = s.held;
-            bytes = s.bytes;
-        } else {
-            held = fresh({(int64_t)need}, like, at::kByte);
-            bytes = need;
-        }
-    }
-    void *p() const { return bytes ? held.data_ptr() : nullptr; }
-};
 
 // elements between the rows of t [T, C] or [B, L, C], whose elements are contiguous
 int64_t row_step(const at::Tensor &t, const char *name, at::ScalarType type, at::IntArrayRef shape) {
@@ -184,7 +153,7 @@ PyObject *conv_fwd(Args a) {
     void *p[3] = {};
     c.parts(a[9], "y", x, true, y, p);
     const bool want = given || truth(a[8]);
-    if (want) last = result(given, "final_state", c.states(), x, c.type);
+    if (want) last = out(given, "final_state", c.states(), x, c.type);
     const int rc = lib.conv_fwd(&c.s, x.data_ptr(), w.data_ptr(), ptr(b), ptr(s0), p, want ? last.data_ptr() : nullptr, stream_of(x));
     if (rc) return PyLong_FromLong(rc);
     PyObject *ys = !c.split ? THPVariable_Wrap(y[0]) : c.s.parts == 1 ? tuple_of({&y[0]}) : c.s.parts == 2 ? tuple_of({&y[0], &y[1]}) : tuple_of({&y[0], &y[1], &y[2]});
@@ -209,14 +178,14 @@ PyObject *conv_bwd(Args a) {
     c.parts(a[2], "dy", x, false, dy, p);
     dx = gx ? *gx : fresh(x.sizes(), x, c.type);
     c.s.dx_stride = row_step(dx, "dx", c.type, x.sizes());
-    dw = result(gw, "dweight", w.sizes(), x, at::kFloat);
-    if (b) db = result(gb, "dbias", {c.s.C}, x, at::kFloat);
+    dw = out(gw, "dweight", w.sizes(), x, at::kFloat);
+    if (b) db = out(gb, "dbias", {c.s.C}, x, at::kFloat);
     const bool states = s0 || gs;
-    if (states) ds0 = result(gs, "dinitial_state", c.states(), x, c.type);
+    if (states) ds0 = out(gs, "dinitial_state", c.states(), x, c.type);
     size_t need = 0;
     int rc = lib.conv_bytes(&c.s, &need);
     if (rc) return PyLong_FromLong(rc);
-    const Work scratch(ws, need, x);
+    const Scratch scratch(ws, need, x);
     rc = lib.conv_bwd(&c.s, x.data_ptr(), w.data_ptr(), p, ptr(b), ptr(s0), ptr(dsT), dx.data_ptr(), fptr(&dw), b ? fptr(&db) : nullptr,
                       states ? ds0.data_ptr() : nullptr, scratch.p(), scratch.bytes, stream_of(x));
     return rc ? PyLong_FromLong(rc) : tuple_of({&dx, &dw, b ? &db : nullptr, states ? &ds0 : nullptr});
@@ -255,7 +224,7 @@ PyObject *out_fwd(Args a) {
     const Out x(o, gate, w, a[3], a[4]);
     const c10::DeviceGuard on(o.device());
     together(o, {gate, w, gy});
-    const at::Tensor y = result(gy, "y", o.sizes(), o, x.type);
+    const at::Tensor y = out(gy, "y", o.sizes(), o, x.type);
     const int rc = lib.out_fwd(&x.s, o.data_ptr(), ptr(gate), ptr(w), y.data_ptr(), stream_of(o));
     return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(y);
 }
@@ -269,18 +238,18 @@ PyObject *out_bwd(Args a) {
     whole(dy, "dy", x.type, o.sizes());
     if (gg && !gate) throw Refusal{PyExc_ValueError, "no gradient of a gate that is not there"};
     if (gw && !w) throw Refusal{PyExc_ValueError, "no gradient of a weight that is not there"};
-    const at::Tensor d_o = result(go, "d_o", o.sizes(), o, x.type);
+    const at::Tensor d_o = out(go, "d_o", o.sizes(), o, x.type);
     at::Tensor dg, dw;
     if (gate) {
         dg = gg ? *gg : fresh(o.sizes(), o, x.type);
         on_device(dg, "dgate", x.type, o.sizes());
         x.s.dgate_stride = rows(heads(dg, "dgate"), "dgate", x.type, x.s.T, x.s.H, x.s.d);
     }
-    if (w) dw = result(gw, "dweight", {x.s.d}, o, at::kFloat);
+    if (w) dw = out(gw, "dweight", {x.s.d}, o, at::kFloat);
     size_t need = 0;
     int rc = lib.out_bytes(&x.s, &need);
     if (rc) return PyLong_FromLong(rc);
-    const Work scratch(ws, w ? need : 0, o);
+    const Scratch scratch(ws, w ? need : 0, o);
     rc = lib.out_bwd(&x.s, o.data_ptr(), dy.data_ptr(), ptr(gate), ptr(w), d_o.data_ptr(), gate ? dg.data_ptr() : nullptr, w ? fptr(&dw) : nullptr, scratch.p(), scratch.bytes, stream_of(o));
     return rc ? PyLong_FromLong(rc) : tuple_of({&d_o, gate ? &dg : nullptr, w ? &dw : nullptr});
 }
@@ -317,10 +286,10 @@ PyObject *block_fwd(Args a) {
     together(x, {res, w, gate, gy, gh});
     k.s.x_stride = row_step(x, "x", k.type, x.sizes());
     if (res) k.s.residual_stride = row_step(*res, "residual", k.stream, x.sizes());
-    const at::Tensor y = result(gy, "y", x.sizes(), x, k.type);
+    const at::Tensor y = out(gy, "y", x.sizes(), x, k.type);
     // without a residual, norm, gate or scale the stream is the branch itself
     const bool same = !res && !gh && !gate && !k.s.post_norm && k.s.scale == 1.f;
-    const at::Tensor h = same ? x : result(gh, "h", x.sizes(), x, k.stream);
+    const at::Tensor h = same ? x : out(gh, "h", x.sizes(), x, k.stream);
     const int rc = lib.block_fwd(&k.s, x.data_ptr(), ptr(res), ptr(w), ptr(gate), y.data_ptr(), same ? nullptr : h.data_ptr(), stream_of(x));
     return rc ? PyLong_FromLong(rc) : tuple_of({&y, &h});
 }
@@ -344,15 +313,15 @@ PyObject *block_bwd(Args a) {
     const bool want = gr || truth(a[10]);
     // one tensor where both gradients are the same numbers
     const bool same = want && !gx && !gr && !branch && k.s.scale == k.s.residual_scale && k.type == k.stream;
-    const at::Tensor dx = result(gx, "dx", dy.sizes(), dy, k.type);
+    const at::Tensor dx = out(gx, "dx", dy.sizes(), dy, k.type);
     at::Tensor dr, dw, dg;
-    if (want) dr = same ? dx : result(gr, "dresidual", dy.sizes(), dy, k.stream);
-    if (w) dw = result(gw, "dweight", {k.s.D}, dy, at::kFloat);
-    if (gate) dg = result(gg, "dgate", {k.s.D}, dy, at::kFloat);
+    if (want) dr = same ? dx : out(gr, "dresidual", dy.sizes(), dy, k.stream);
+    if (w) dw = out(gw, "dweight", {k.s.D}, dy, at::kFloat);
+    if (gate) dg = out(gg, "dgate", {k.s.D}, dy, at::kFloat);
     size_t need = 0;
     int rc = lib.block_bytes(&k.s, &need);
     if (rc) return PyLong_FromLong(rc);
-    const Work scratch(ws, w || gate ? need : 0, dy);
+    const Scratch scratch(ws, w || gate ? need : 0, dy);
     rc = lib.block_bwd(&k.s, dy.data_ptr(), ptr(dh), h.data_ptr(), branch ? ptr(x) : nullptr, ptr(w), ptr(gate), dx.data_ptr(), want && !same ? dr.data_ptr() : nullptr,
                        w ? fptr(&dw) : nullptr, gate ? fptr(&dg) : nullptr, scratch.p(), scratch.bytes, stream_of(dy));
     return rc ? PyLong_FromLong(rc) : tuple_of({&dx, want ? &dr : nullptr, w ? &dw : nullptr, gate ? &dg : nullptr});
