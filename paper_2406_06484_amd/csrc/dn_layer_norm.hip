@@ -9,7 +9,8 @@
 //     h = keep residual + scale u m ,  y = r h w ,  r = 1 / sqrt(mean(h^2) + eps) ;  with  q = r h ,  dz = dy w :
 //     H = dh + r (dz - q mean(dz q)) ,  dresidual = keep H ,  B = scale u H ,  dx = B, or r_x (B - m mean(B m)) ,  dw = sum dy q ,  du = scale sum H m
 //
-// Bound by HBM: about ten operations an element forward and thirty backward.  Each element is fetched once and written once; sums over a row stay in registers and lane swaps (a row wider than
+// Bound by HBM: about ten operations an element forward and thirty backward.  In bf16, 16384 tokens of 16 heads of 128: output norm 37 us forward (201 MB), 59 backward (336 MB, 5.7 TB/s) and 5 for the weight's sums; 16384 rows of 2048: block norm
+// 45 (268 MB, 6.0 TB/s), 56 (273 MB) and 5; 4101 rows of 4104 with an fp32 stream and a normed, gated branch 43 (202 MB), 64 (303 MB) and 5.  Each element is fetched once and written once; sums over a row stay in registers and lane swaps (a row wider than
 // two words a lane: and the LDS).  y comes from the sum before it is rounded to the stream's type, and the backward pass, which forms r and q again, from the stream as it was stored.
 #include "dn_layer_device.hpp"
 
@@ -524,7 +525,8 @@ template <template <typename, bool> class L> int block_norm(int dtype, bool wide
 
 } // namespace
 
-// Rounds of a workgroup's rows up to which one workgroup has all of a backward pass and so its vectors' sums: it saves a launch and the partial sums' memory.
+// Rounds of a workgroup's rows up to which one workgroup has all of a backward pass and so its vectors' sums: it saves a launch and the partial sums' memory
+// (block norm, 16 rows of 256: 4.3 us by one workgroup, 8.6 by two launches; output norm, 16 tokens of 4 heads: 5.6 and 10.0).
 constexpr int kAloneRounds = 4;
 
 int out_norm_bwd_blocks(int dtype, int d, int T, int H) {

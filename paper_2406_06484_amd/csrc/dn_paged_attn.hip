@@ -10,8 +10,6 @@
 // that lane, so that P never leaves its registers.
 #include "dn_attn_device.hpp"
 
-#include <type_traits>
-
 namespace dn {
 
 // How the key axis is cut: `splits` pieces of `keys` keys from the first that a row tile sees.
@@ -46,7 +44,6 @@ __device__ inline void key_range(const AttnArgs &a, const SeqRows &s, int G, int
 // cache row of d elements.
 __device__ inline int page_entry(const PagedArgs &c, int n, int kk) { return c.table[(long)n * c.max_pages + min(kk >> c.page_shift, c.max_pages - 1)]; }
 __device__ inline int page_id(const PagedArgs &c, int entry) { return min(max(entry, 0), c.num_pages - 1); }
-__device__ inline int page_of(const PagedArgs &c, int n, int kk) { return __builtin_amdgcn_readfirstlane(page_id(c, page_entry(c, n, kk))); }
 __device__ inline long row_of(const PagedArgs &c, int page, int kk, int kvh, int Hkv) {
     return (((long)page * Hkv + kvh) << c.page_shift) + (kk & ((1 << c.page_shift) - 1));
 }
@@ -81,7 +78,7 @@ __device__ inline void partial_of(const AttnArgs &a, int split, long row, int D,
 // holds a sixteenth of the elements of the eight keys whose probabilities it has, one 16-byte piece (or less) of each 16, from l % 16 on, which a 16-bit
 // transposition among its own registers turns into the operands of D / 16 products.  (So the lanes of one load stand side by side.)  No LDS traffic and no barrier until the waves of a workgroup, which share out the
 // keys of one split, join their sums.  32 sequences of 16 heads of 128 over up to 2048 keys in bf16 (374 MB): 72 us, 5.2 TB/s; one over 32768 e4m3 keys of 4 heads (34 MB):
-// 11 us and 4 for the join.
+// 11 us and 4 for the join; one over 131072 in 4 bits (71 MB) 16 us, and 32 over up to 8192 (91 MB) 23, the vector ALU busy for a quarter of it.
 constexpr int kFewTile = 16, kFewKeys = 32, kFewWaves = 4;
 // Twice as many waves per workgroup where there are few workgroups, if their registers allow it.
 template <typename T> constexpr bool few_twice(int d) { return d * sizeof(T) <= 256; }
@@ -122,7 +119,6 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
     // 4-bit pages bring so many keys per byte that the vector ALU's work shows beside the reading: sums are rescaled only when a row's maximum has grown by 2^8, and
     // probabilities enter the second product as one bf16 term.
     constexpr bool LAZY = FP4, TWO_TERMS = !FP4;
-    constexpr int AHEAD = 1;
     constexpr int FB = FP4 ? D / kGroup : 1, FW = FP4 ? FB : 1; // factors of a row; words with those of four rows
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int Hkv = a.r.Hkv, G = a.r.Hq / Hkv;
@@ -163,13 +159,12 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
     const float c = a.scale * kLog2e;
 
     const char *kp = static_cast<const char *>(a.c.kp), *vp = static_cast<const char *>(a.c.vp);
-    // `AHEAD` steps are on their way while one is worked on: step i stands in buffer i % AHEAD
-    unsigned kw_[AHEAD][2][KW], vw_[AHEAD][8][VW];
-    float4 ks_[AHEAD][2], vs_[AHEAD][2];
+    int page[2];
+    unsigned kw[2][KW], vw[8][VW];
+    float4 ks[2], vs[2];
     // 4-bit pages: the factors' bytes, of key col's groups, and of all groups of the values 4 g .. 4 g + 3
-    unsigned kf_[AHEAD][2][FP4 && D > 128 ? 2 : 1], vf_[AHEAD][2][FW];
-    auto load_k = [&](int at, int k0, const int (&page)[2], int range) __attribute__((always_inline)) {
-        auto &kw = kw_[at]; auto &ks = ks_[at]; auto &kf = kf_[at];
+    unsigned kf[2][FP4 && D > 128 ? 2 : 1], vf[2][FW];
+    auto load_k = [&](int k0, int range) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const long row = row_of(a.c, page[h], k0 + 16 * h, kvh, Hkv);
@@ -182,8 +177,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
             if constexpr (FP8) ks[h] = *reinterpret_cast<const float4 *>(a.c.ks + row + 4 * g);
         }
     };
-    auto load_v = [&](int at, int k0, const int (&page)[2], int range) __attribute__((always_inline)) {
-        auto &vw = vw_[at]; auto &vs = vs_[at]; auto &vf = vf_[at];
+    auto load_v = [&](int k0, int range) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const long row = row_of(a.c, page[h], k0 + 16 * h, kvh, Hkv);
@@ -207,37 +201,31 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
     // paths meet, and with it all that was requested before.  Page entries are fetched a step before their pages.
     constexpr int STEP = WAVES * kFewKeys;
     int k0 = k_begin + wave * kFewKeys;
-    int page[AHEAD][2], entry[2];
+    int entry[2];
     auto look_up = [&](int kk) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) entry[h] = page_entry(a.c, n, kk + 16 * h);
     };
     if (k0 < k_end) {
+        look_up(k0);
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const int kk = k0 + i * STEP < k_end ? k0 + i * STEP : k0;
-            look_up(kk);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) page[i][h] = __builtin_amdgcn_readfirstlane(page_id(a.c, entry[h]));
-            load_k(i, kk, page[i], kBufRange);
-            load_v(i, kk, page[i], kBufRange);
-        }
-        look_up(k0 + AHEAD * STEP);
+        for (int h = 0; h < 2; ++h) page[h] = __builtin_amdgcn_readfirstlane(page_id(a.c, entry[h]));
+        load_k(k0, kBufRange);
+        load_v(k0, kBufRange);
+        look_up(k0 + STEP);
         // the query is there before the loop, which would else wait for it, and for the loads behind it, in every step
 #pragma unroll
         for (int i = 0; i < (int)(KE * sizeof(T) / 4); ++i) asm volatile("" : "+v"(qw[i]));
     }
-    auto step = [&](auto buffer) __attribute__((always_inline)) {
-        constexpr int B = decltype(buffer)::value;
-        auto &kw = kw_[B]; auto &vw = vw_[B]; auto &ks = ks_[B]; auto &vs = vs_[B]; auto &kf = kf_[B]; auto &vf = vf_[B];
-        const bool more = k0 + AHEAD * STEP < k_end;
-        const int kn = more ? k0 + AHEAD * STEP : k0, range = more ? kBufRange : 0;
+    for (; k0 < k_end; k0 += STEP) {
+        const bool more = k0 + STEP < k_end;
+        const int kn = more ? k0 + STEP : k0, range = more ? kBufRange : 0;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int id = __builtin_amdgcn_readfirstlane(page_id(a.c, entry[h]));
-            page[B][h] = more ? id : page[B][h];
+            page[h] = more ? id : page[h];
         }
-        look_up(k0 + (AHEAD + 1) * STEP);
+        look_up(k0 + 2 * STEP);
         f32x4 st[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
         // (the lane's group of a key: element (4 piece + g) KV / 32)
         float kfac[2][FP4 ? KE / KV : 1];
@@ -265,7 +253,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
             }
             if constexpr (FP8) { st[h][0] *= ks[h].x; st[h][1] *= ks[h].y; st[h][2] *= ks[h].z; st[h][3] *= ks[h].w; }
         }
-        load_k(B, kn, page[B], range);
+        load_k(kn, range);
         if (k0 < all_from || k0 + kFewKeys - 1 > all_to) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -361,10 +349,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
                 o[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), pl, o[2 * w + 1], 0, 0, 0);
             }
         }
-        load_v(B, kn, page[B], range);
-    };
-    for (; k0 < k_end; k0 += STEP) {
-        step(std::integral_constant<int, 0>());
+        load_v(kn, range);
     }
 
     // the waves' sums: o of element (16 piece + 4 g + r) VV + j and query col stands at o[piece VV + j][r]
@@ -416,8 +401,8 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
 //
 // Products, softmax, products in turn: prompts of 4 x 2048 tokens, 16 heads of 128, 88 to 91 us (760 TFLOP/s of the 1195 of a large matrix product), the matrix pipes busy for 0.32 of the time, the
 // vector ALU for 0.33 or more (exponentials count as one instruction), the LDS for 0.16; the waves wait for 0.27 of theirs and are ready but not issued for 0.31.  512 tokens of 16 heads (4 of keys)
-// behind 15872, 86 us with the join (10), 0.37, 0.34, 0.19, 0.22, 0.32.  Without the requests, the exponentials or half of the products it would still take 90 % (80 %).  A workgroup has 128
-// rows, 32 per wave, and walks over its keys 64 at a time: K and V travel straight, 8-bit pages through registers (they become bf16 on the way, exactly), into one of two LDS buffers while the other
+// behind 15872, 86 us with the join (10), 0.37, 0.34, 0.19, 0.22, 0.32 (in 4 bits 90.5 with its append; the prompts, 4 heads of keys, 97 with append and reading back).  Without the requests, the exponentials or half of the products it would still take 90 % (80 %).  A workgroup has 128
+// rows, 32 per wave, and walks over its keys 64 at a time: K and V travel straight, 8- and 4-bit pages through registers (they become bf16 on the way, exactly), into one of two LDS buffers while the other
 // is worked on, so that a tile costs one barrier.  Rows of a tile are not padded: their 16-byte pieces are permuted by an XOR with the row, which spreads both the row
 // reads (K) and the transposing reads (V, four rows at a time) over the banks.
 constexpr int kWideRows = 128, kWideWaves = 4;
@@ -799,8 +784,8 @@ __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_wide(
     attend_wide<CT, D>(a, cut, few_rows, true, blockIdx.x, lds);
 }
 // Chunks beside single tokens: both kinds of workgroup in one launch, the long ones first, so that the short ones, which wait for memory, run under them.  12 chunks of up to 256 tokens
-// and 12 single ones, 32 heads (8 of keys) of 64, e4m3, window 1024: 39.5 us, the matrix pipes busy for 0.13, the vector ALU for 0.34, the waves waiting for 0.44 of their time: with 8-bit pages at d = 64 and 128 the compiled
-// loop waits for the tile that it has just requested before it takes the first maximum, so that no request is under way under the softmax.
+// and 12 single ones, 32 heads (8 of keys) of 64, window 1024: 38 us in e4m3 and in 4 bits, whose matrix pipes are busy for 0.15, vector ALU for 0.31, waves waiting for 0.34 and ready but not issued for 0.24 of their time; 464 workgroups
+// are 1.8 per CU.
 template <typename CT, int D>
 __global__ __launch_bounds__(64 * kWideWaves, D > 128 ? 1 : 2) void k_attn_both(AttnArgs a, int tiles, Cut few, Cut wide, int few_rows, int wide_blocks) {
     extern __shared__ __align__(16) unsigned char lds[];
@@ -960,6 +945,7 @@ Plan plan_attn(int dtype, int d, const AttnArgs &a) {
     // 640 0.98, 0.96, 0.97.  (Between 256 and 512 ragged batches go either way: at 320 0.89, 0.92, 1.07.)
     const bool twice = !p.slots && (dtype == 0 ? few_twice<float>(d) : few_twice<bf16>(d)) && (blocks <= 256 || blocks >= 512) && seen > kFewWaves * kFewKeys;
     p.waves = twice ? 2 * kFewWaves : kFewWaves;
+    // (4-bit pages: two workgroups of eight waves per CU, whose loads bring a quarter of the bytes: 32 contexts of up to 8192 keys, 4 heads of 128, with their append 31 us instead of 35.)
     const long want = twice && !a.c.fp4 ? 256 : 512;
     p.few = p.per_seq && N ? cut_keys(seen, blocks, 64 * blocks < want ? 64 * blocks : want, least > 256 ? least : 256, kFewKeys * p.waves) : Cut{1, 128};
     return p;

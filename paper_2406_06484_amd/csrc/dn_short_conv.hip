@@ -346,7 +346,8 @@ int column_blocks(const ConvArgs &a, int V) { return (a.C / V + 63) / 64; }
 
 constexpr int kMostBlocks = 1 << 15; // along the rows; waves go on to further slots
 
-// Bytes of a row that a lane has: 16 forward and 8 backward (more registers), half of that where there are no two waves for each SIMD, which a strip's instructions then keep busy longer than the memory does.
+// Bytes of a row that a lane has: 16 forward and 8 backward (more registers), half of that where there are no two waves for each SIMD, which a strip's instructions then keep busy longer than the memory does
+// (32 sequences of one row of 6144 channels, backward: 6.1 us instead of 8.6).
 constexpr long kFewWaves = 2048;
 
 template <typename T, int W, int R> const void *fwd_of(bool thin) {

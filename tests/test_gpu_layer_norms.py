@@ -147,6 +147,50 @@ def test_block_norm_in_place():
         assert all(torch.equal(p, q) for p, q in zip(want[:3], got[:3]))
 
 
+def test_first_norm_in_place_of_the_branch_keeps_the_stream():
+    x = rng(9)(torch.bfloat16, 19, 512).cuda()
+    want, h = dn.deltanet_block_norm_fwd(x)
+    assert h.data_ptr() == x.data_ptr()
+    y = x.clone()
+    got, h = dn.deltanet_block_norm_fwd(y, y=y)
+    assert got.data_ptr() == y.data_ptr() and h.data_ptr() != y.data_ptr()
+    assert torch.equal(got, want) and torch.equal(h, x)
+
+
+@pytest.mark.parametrize("T,D", [(16, 512), (17, 512), (128, 64), (129, 64), (4, 4096), (5, 4096)])
+def test_block_norm_where_one_workgroup_ends_to_have_all_rows(T, D):
+    rand = rng(T + D)
+    h, w, dy, u, x = rand(torch.bfloat16, T, D), rand(torch.bfloat16, D), rand(torch.bfloat16, T, D), rand(torch.bfloat16, D), rand(torch.bfloat16, T, D)
+    got = dn.deltanet_block_norm_bwd(dy.cuda(), h.cuda(), x.cuda(), w.cuda(), gate=u.cuda())
+    want = ref.block_norm_grad(wide(dy), None, wide(h), wide(x), wide(w), wide(u), False, 1.0, 1.0, EPS, "bf16", "bf16")
+    for name, a, (v, e) in zip(("dx", "dresidual", "dw", "dgate"), got, want):
+        near(a, v, e, "%dx%d %s" % (T, D, name))
+
+
+@pytest.mark.parametrize("T", [32, 33])
+def test_output_norm_where_one_workgroup_ends_to_have_all_rows(T):
+    rand = rng(T)
+    o, g, w, dy = rand(torch.bfloat16, T, 4, 128), rand(torch.bfloat16, T, 4, 128), rand(torch.bfloat16, 128), rand(torch.bfloat16, T, 4, 128)
+    got = dn.deltanet_out_norm_bwd(o.cuda(), dy.cuda(), g.cuda(), w.cuda())
+    for name, a, (v, e) in zip(("do", "dgate", "dw"), got, ref.out_norm_grad(wide(o), wide(g), wide(w), EPS, "silu", wide(dy), "bf16")):
+        near(a, v, e, name)
+
+
+def test_norms_on_another_stream():
+    rand = rng(10)
+    o, g, w = (rand(torch.bfloat16, *s).cuda() for s in ((300, 4, 64), (300, 4, 64), (64,)))
+    x, res = (rand(torch.bfloat16, 300, 256).cuda() for _ in range(2))
+    calls = [lambda **k: [dn.deltanet_out_norm_fwd(o, g, w, **k)], lambda **k: dn.deltanet_out_norm_bwd(o, g, g, w, **k),
+             lambda **k: dn.deltanet_block_norm_fwd(x, res, post_norm=True, **k), lambda **k: dn.deltanet_block_norm_bwd(x, res, x, post_norm=True, **k)]
+    side = torch.cuda.Stream()
+    for call in calls:
+        want = call()
+        side.wait_stream(torch.cuda.current_stream())
+        got = call(stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        assert all((a is None and b is None) or torch.equal(a, b) for a, b in zip(want, got))
+
+
 def test_a_row_of_nan_or_infinity_stays_in_its_row():
     rand = rng(7)
     for D in (64, 1024, 2048, 8192):

@@ -89,6 +89,14 @@ def test_one_part_is_a_tensor_and_values_of_every_size():
     c.check_backward(dn.deltanet_short_conv_bwd(c.x, c.w, c.dy[0], c.b, c.s, c.ds, cu_seqlens=c.cu), "large")
 
 
+@pytest.mark.parametrize("T", [0, 2])
+def test_dense_sequences_of_fewer_rows_than_taps(T):
+    c = Case([T, T, T], [16], [True], 4, "bf16", True, True, packed=False)
+    y, last = dn.deltanet_short_conv_fwd(c.x, c.w, c.b, c.s, **c.kw)
+    c.check_forward(y, last, "T %d" % T)
+    c.check_backward(dn.deltanet_short_conv_bwd(c.x, c.w, c.dy, c.b, c.s, c.ds, **c.kw), "T %d" % T)
+
+
 @pytest.mark.parametrize("W", [2, 3, 4])
 def test_chunks_and_single_tokens_continue_a_sequence_with_states_in_place(W):
     c = Case([37, 37], [96], [True], W, "bf16", False, True, packed=False)
