@@ -431,15 +431,23 @@ template <typename CT, int D> struct WideTile {
     static constexpr int NL = KEYS * LPR / (64 * kWideWaves); // loads per thread and tensor
     static constexpr int BYTES = KEYS * ROWB;
     static constexpr int oV = BYTES, oKS = 2 * BYTES, oVS = oKS + (FP8 ? 4 * KEYS : 0), SIZE = oVS + (FP8 ? 4 * KEYS : 0);
-    // The row among a wave's that the q-th group of LPR lanes has.  Of 8- and 4-bit pages a lane's load becomes two or four pieces, stored one after the other, so that lanes that store together have pieces as far
-    // apart; the groups beside each other therefore have rows whose XOR differs in the bits in between (in order, two or four lanes met in each bank: prompts of 4 x 2048 tokens in 4 bits, with append and reading back, 110 us
-    // instead of 99).
+    // Of 8- and 4-bit pages a lane's load becomes two or four pieces, which it stores one after the other.  Eight lanes that store together meet no bank twice if their pieces differ in the low three bits of their place: the
+    // lanes of a row, whose pieces are two or four apart, begin with different ones of them (`turn`), and rows that two groups of lanes beside each other store differ in the swizzle's bits that those do not (`order`: the
+    // row among a wave's that the q-th group has).  (Two chunks of 1024 behind 3072, 8 heads of 256, 8-bit: 148 us instead of 156 with two lanes to a bank; in 4 bits 141 instead of 143.)  4 bits at d = 128 have the order only,
+    // two lanes to a bank: prompts of 4 x 2048 tokens, with append and reading back, 97 us, 98 with the turn, whose selections cost more than it saves, and 110 with neither.
+    static constexpr bool TURN = PER > 1 && D != 64 && !(FP4 && D == 128);
     __device__ static inline int order(int q) {
         if constexpr (PER == 1) return q;
-        else if constexpr (D == 64) return (q & 9) | (q & 2) << 1 | (q & 4) >> 1;
-        else if constexpr (LPR == 4) return (q & 3) << 2 | q >> 2;
-        else if constexpr (LPR == 8) return (q & 1) << 2 | q >> 1;
+        else if constexpr (D == 64) return (q & 10) | (q & 1) << 2 | (q & 4) >> 2;
+        else if constexpr (FP4 && D == 128) return (q & 3) << 2 | q >> 2;
         else return q;
+    }
+    __device__ static inline int turn(int piece) { return !TURN ? 0 : FP4 ? piece >> 1 & 3 : piece >> 2 & 1; }
+    // the words of a load as the pieces turn ^ 0, turn ^ 1, .. hold them
+    __device__ static inline u32x4 turned(u32x4 v, int turn) {
+        if constexpr (!TURN) return v;
+        if constexpr (FP4) v = turn & 1 ? u32x4{v[1], v[0], v[3], v[2]} : v;
+        return turn & (FP4 ? 2 : 1) ? u32x4{v[2], v[3], v[0], v[1]} : v;
     }
     __device__ static inline int swizzle(int row) { return D == 64 ? ((row >> 1) & 1) << 2 | ((row >> 2) & 3) : (row & 3) << 2 | ((row >> 2) & 3); }
 };
@@ -587,22 +595,24 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
 #pragma unroll
         for (int i = 0; i < W::NL; ++i) {
             const int r = (i * 256 + wave * 64) / W::LPR + W::order(lane / W::LPR);
-            u32x4 v = rv[i];
+            const int turn = W::turn(piece), place = ((W::PER * piece) ^ turn ^ W::swizzle(r)) << 4;
+            const u32x4 k = W::turned(rk[i], turn);
+            u32x4 v = W::turned(rv[i], turn);
             if (ends && dead(k0 + r)) v = u32x4{0, 0, 0, 0};
             if constexpr (FP4) {
                 const float ck = fp4_factor(fk[i]), cv = fp4_factor(ends && dead(k0 + r) ? 127u : fv[i]);
 #pragma unroll
                 for (int u = 0; u < W::PER; ++u) {
-                    unsigned char *at = buf + r * W::ROWB + (((W::PER * piece + u) ^ W::swizzle(r)) << 4);
-                    *reinterpret_cast<u32x4 *>(at) = from_fp4x8(rk[i][u], ck);
+                    unsigned char *at = buf + r * W::ROWB + (place ^ u << 4);
+                    *reinterpret_cast<u32x4 *>(at) = from_fp4x8(k[u], ck);
                     *reinterpret_cast<u32x4 *>(at + W::oV) = from_fp4x8(v[u], cv);
                 }
                 continue;
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                unsigned char *at = buf + r * W::ROWB + (((2 * piece + u) ^ W::swizzle(r)) << 4);
-                *reinterpret_cast<u32x4 *>(at) = widen(rk[i][2 * u], rk[i][2 * u + 1]);
+                unsigned char *at = buf + r * W::ROWB + (place ^ u << 4);
+                *reinterpret_cast<u32x4 *>(at) = widen(k[2 * u], k[2 * u + 1]);
                 *reinterpret_cast<u32x4 *>(at + W::oV) = widen(v[2 * u], v[2 * u + 1]);
             }
         }
