@@ -433,7 +433,7 @@ template <typename CT, int D> struct WideTile {
     static constexpr int oV = BYTES, oKS = 2 * BYTES, oVS = oKS + (FP8 ? 4 * KEYS : 0), SIZE = oVS + (FP8 ? 4 * KEYS : 0);
     // Of 8- and 4-bit pages a lane's load becomes two or four pieces, which it stores one after the other.  Eight lanes that store together meet no bank twice if their pieces differ in the low three bits of their place: the
     // lanes of a row, whose pieces are two or four apart, begin with different ones of them (`turn`), and rows that two groups of lanes beside each other store differ in the swizzle's bits that those do not (`order`: the
-    // row among a wave's that the q-th group has).  (Two chunks of 1024 behind 3072, 8 heads of 256, 8-bit: 148 us instead of 156 with two lanes to a bank; in 4 bits 141 instead of 143.)  4 bits at d = 128 have the order only,
+    // row among a wave's that the q-th group has).  (Two chunks of 1024 at the end of 4096 keys, 8 heads of 256, 8-bit: 148 us instead of 156 with two lanes to a bank; in 4 bits 141 instead of 143.)  4 bits at d = 128 have the order only,
     // two lanes to a bank: prompts of 4 x 2048 tokens, with append and reading back, 97 us, 98 with the turn, whose selections cost more than it saves, and 110 with neither.
     static constexpr bool TURN = PER > 1 && D != 64 && !(FP4 && D == 128);
     __device__ static inline int order(int q) {
