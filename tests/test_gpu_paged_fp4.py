@@ -4,6 +4,7 @@ import torch
 
 import paper_2406_06484_amd as dn
 from tests import attention_reference as ref
+from tests import attention_roundings
 from tests import fp4_reference as f4
 from tests.attention_util import near, replays
 from tests.fp4_reference import Batch4
@@ -209,3 +210,17 @@ def test_refusals():
         dn.deltanet_paged_attn_fwd(q.float(), *b.tensors(), b.cu, **b.scales())
     with pytest.raises(TypeError):
         dn.deltanet_paged_read(*b.tensors(), b.cu, 1, dtype=torch.float16, **b.scales())
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("qs,kvs", [([1, 1, 3, 2], [2, 40, 200, 1030]), ([2], [9000]), ([1, 130, 3], [300, 200, 70])])
+def test_few_rows_carry_two_terms(d, qs, kvs):
+    """As over 16- and 8-bit pages; the last batch has a chunk of many rows beside the few."""
+    b = Batch4(qs, kvs, 2, d, page=16, seed=d + len(qs))
+    q, q64 = b.rows(8)
+    o = b.attend(q, max_q=max(qs), max_kv=max(kvs))
+    for n, (m, kv) in enumerate(zip(qs, kvs)):
+        if m <= 8:
+            lo = int(b.cu_host[n])
+            want, size, top = ref.attention(q64[lo:lo + m], b.k[n], b.v[n], kv - m, d ** -0.5, 0)
+            near(o[lo:lo + m], want, attention_roundings.bound(want, size, top, d, kv), "d %d seq %d (%d of %d)" % (d, n, m, kv))
