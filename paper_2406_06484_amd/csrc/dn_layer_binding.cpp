@@ -287,8 +287,8 @@ PyObject *block_fwd(Args a) {
     k.s.x_stride = row_step(x, "x", k.type, x.sizes());
     if (res) k.s.residual_stride = row_step(*res, "residual", k.stream, x.sizes());
     const at::Tensor y = out(gy, "y", x.sizes(), x, k.type);
-    // without a residual, norm, gate or scale the stream is the branch itself, unless y takes its place
-    const bool same = !res && !gh && !gate && !k.s.post_norm && k.s.scale == 1.f && !(gy && gy->data_ptr() == x.data_ptr());
+    // without a residual, norm, gate or scale the stream is the branch itself, unless y takes its place or its rows are apart (the backward pass takes a contiguous one)
+    const bool same = !res && !gh && !gate && !k.s.post_norm && k.s.scale == 1.f && x.is_contiguous() && !(gy && gy->data_ptr() == x.data_ptr());
     const at::Tensor h = same ? x : out(gh, "h", x.sizes(), x, k.stream);
     const int rc = lib.block_fwd(&k.s, x.data_ptr(), ptr(res), ptr(w), ptr(gate), y.data_ptr(), same ? nullptr : h.data_ptr(), stream_of(x));
     return rc ? PyLong_FromLong(rc) : tuple_of({&y, &h});

@@ -97,7 +97,7 @@ def deltanet_block_norm_fwd(x, residual=None, weight=None, *, gate=None, post_no
                             eps: float = 1e-6, y=None, h=None, stream=None) -> Tuple["torch.Tensor", "torch.Tensor"]:
     """Between two blocks: h = residual_scale * residual + scale * gate * x, with x normalised first if post_norm, and y, the RMS norm of h times
     weight; returns (y, h).  x and residual [T, D] or [B, L, D] may have rows apart; residual and h have x's type or are float32.  Without a residual (in front of the
-    first block) h is the branch; x itself, where nothing changes it."""
+    first block) h is the branch; x itself, where that is contiguous and nothing changes it."""
     return _call("block_norm_fwd", stream, x, residual, weight, gate, post_norm, scale, residual_scale, eps, y, h)
 
 

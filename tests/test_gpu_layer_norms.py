@@ -240,3 +240,24 @@ def test_more_elements_than_31_bits_count():
     b, c, _ = dn.deltanet_out_norm_bwd(o, a, o)
     b1, c1, _ = dn.deltanet_out_norm_bwd(o[-8:].clone(), a[-8:].clone(), o[-8:].clone())
     assert torch.equal(b[-8:], b1) and torch.equal(c[-8:], c1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,D", [(1, 64), (11, 256), (300, 1032)])
+@pytest.mark.parametrize("weighted", [True, False])
+def test_first_norm_of_a_column_block_and_its_gradient(dtype, T, D, weighted):
+    """A model's first norm on rows apart: the stream that the forward call returns is what the backward call takes."""
+    rand, td = rng(T + D), ref.TYPES[dtype]
+    x, w, dy, dh = rand(td, T, D), rand(td, D) if weighted else None, rand(td, T, D), rand(td, T, D)
+    wd = None if w is None else w.cuda()
+    y, h = dn.deltanet_block_norm_fwd(column_block(x), None, wd)
+    near(y, *ref.block_norm(wide(x), None, wide(w), None, False, 1.0, 1.0, EPS, dtype, dtype)[0], "y")
+    assert h.is_contiguous() and torch.equal(h.cpu(), x)
+    dx, dr, dw, dg = dn.deltanet_block_norm_bwd(dy.cuda(), h, None, wd, dh.cuda(), want_dresidual=False)
+    want = ref.block_norm_grad(wide(dy), wide(dh), wide(x), None, wide(w), None, False, 1.0, 1.0, EPS, dtype, dtype)
+    near(dx, *want[0], "dx")
+    assert dr is None and dg is None
+    if weighted:
+        near(dw, *want[2], "dw")
+    dense = dn.deltanet_block_norm_fwd(column_block(x).unsqueeze(0), None, wd)
+    assert all(t.shape == (1, T, D) and torch.equal(t[0], s) for t, s in zip(dense, (y, h)))
