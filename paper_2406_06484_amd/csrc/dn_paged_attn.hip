@@ -163,6 +163,10 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
     float4 ks[2], vs[2];
     // 4-bit pages: the factors' bytes, of key col's groups, and of all groups of the values 4 g .. 4 g + 3
     unsigned kf[2][FP4 && D > 128 ? 2 : 1], vf[2][FW];
+    auto load_factors = [&](const float *at, int range) __attribute__((always_inline)) {
+        const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(at, range), 16 * g, 0, 0);
+        return make_float4(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]), __uint_as_float(x[3]));
+    };
     auto load_k = [&](int k0, int range) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -173,7 +177,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
                 if constexpr (FB == 2) kf[h][0] = __builtin_amdgcn_raw_buffer_load_b16(fa, col * FB, 0, 0);
                 else load_words(kf[h], fa, col * FB);
             }
-            if constexpr (FP8) ks[h] = *reinterpret_cast<const float4 *>(a.c.ks + row + 4 * g);
+            if constexpr (FP8) ks[h] = load_factors(a.c.ks + row, range);
         }
     };
     auto load_v = [&](int k0, int range) __attribute__((always_inline)) {
@@ -187,7 +191,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
                 else load_words(vw[4 * h + i], va, (4 * g + i) * RB + col * (VV * RB / D), 256);
             }
             if constexpr (FP4) load_words(vf[h], make_rsrc(reinterpret_cast<const char *>(a.c.vs) + row * FB, range), 4 * g * FB);
-            if constexpr (FP8) vs[h] = *reinterpret_cast<const float4 *>(a.c.vs + row + 4 * g);
+            if constexpr (FP8) vs[h] = load_factors(a.c.vs + row, range);
         }
     };
 
