@@ -261,3 +261,35 @@ def test_first_norm_of_a_column_block_and_its_gradient(dtype, T, D, weighted):
         near(dw, *want[2], "dw")
     dense = dn.deltanet_block_norm_fwd(column_block(x).unsqueeze(0), None, wd)
     assert all(t.shape == (1, T, D) and torch.equal(t[0], s) for t, s in zip(dense, (y, h)))
+
+
+@pytest.mark.parametrize("dtype,stream", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("T,D", [(13, 32), (1031, 32), (131, 64), (7, 136), (333, 136), (21, 512), (6, 1024), (5, 2056), (3, 8192), (67, 8192)])
+@pytest.mark.parametrize("post,gated", [(False, False), (True, True)])
+def test_block_norm_in_place_at_every_width(dtype, stream, T, D, post, gated):
+    """Rows that share a wave, whose lanes past the last row read it again while its owner stores; rows of some waves; one workgroup and several."""
+    rand, td, ts = rng(T + D), ref.TYPES[dtype], ref.TYPES[stream]
+    x, res, w, u, dy, dh = (rand(t, *s).cuda() for t, s in ((td, (T, D)), (ts, (T, D)), (td, (D,)), (td, (D,)), (td, (T, D)), (ts, (T, D))))
+    kw = dict(gate=u if gated else None, post_norm=post, scale=0.5)
+    y, h = dn.deltanet_block_norm_fwd(x, res, w, **kw)
+    y2, h2 = x.clone(), res.clone()
+    dn.deltanet_block_norm_fwd(y2, h2, w, y=y2, h=h2, **kw)
+    assert torch.equal(y, y2) and torch.equal(h, h2)
+    want = dn.deltanet_block_norm_bwd(dy, h, x, w, dh, **kw)
+    a, b = dy.clone(), dh.clone()
+    got = dn.deltanet_block_norm_bwd(a, h, x, w, b, dx=a, dresidual=b, **kw)
+    assert got[0].data_ptr() == a.data_ptr() and got[1].data_ptr() == b.data_ptr()
+    assert all((p is None and q is None) or torch.equal(p, q) for p, q in zip(want, got))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H,d", [(1, 1, 32), (37, 3, 32), (1031, 3, 32), (7, 5, 64), (333, 4, 128), (3, 2, 256), (129, 3, 256)])
+def test_output_norm_in_place(dtype, T, H, d):
+    rand, td = rng(T + d), ref.TYPES[dtype]
+    o, g, w, dy = (rand(td, *s).cuda() for s in ((T, H, d), (T, H, d), (d,), (T, H, d)))
+    y = o.clone()
+    want, got = dn.deltanet_out_norm_fwd(o, g, w), dn.deltanet_out_norm_fwd(y, g, w, y=y)
+    assert got.data_ptr() == y.data_ptr() and torch.equal(got, want)
+    want, a = dn.deltanet_out_norm_bwd(o, dy, g, w), dy.clone()
+    got = dn.deltanet_out_norm_bwd(o, a, g, w, d_o=a)
+    assert got[0].data_ptr() == a.data_ptr() and all(torch.equal(p, q) for p, q in zip(want, got))

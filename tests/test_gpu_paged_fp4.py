@@ -224,3 +224,54 @@ def test_few_rows_carry_two_terms(d, qs, kvs):
             lo = int(b.cu_host[n])
             want, size, top = ref.attention(q64[lo:lo + m], b.k[n], b.v[n], kv - m, d ** -0.5, 0)
             near(o[lo:lo + m], want, attention_roundings.bound(want, size, top, d, kv), "d %d seq %d (%d of %d)" % (d, n, m, kv))
+
+
+class Rising(Batch4):
+    """Scores that climb or fall along the contexts: key j is j / 128 times a direction, and some noise; rows(..) of it are this direction with a slope per head."""
+
+    def __init__(self, qs, kvs, Hkv, d, **kw):
+        super().__init__(qs, kvs, Hkv, d, **kw)
+        self.way = torch.randint(0, 2, (d,), generator=self.gen).double() * 2 - 1
+        for n, kv in enumerate(kvs):
+            p = torch.arange(kv)
+            x = (p / 128.0)[:, None, None] * self.way + 0.2 * torch.randn(kv, Hkv, d, generator=self.gen, dtype=torch.float64)
+            codes, factors = f4.quantise(x.bfloat16().double())
+            ids, slots = self.table_host[n].long()[p // self.page].cuda(), (p % self.page).cuda()
+            self.k_pages.view(torch.uint8)[ids, :, slots] = f4.packed(codes).cuda()
+            self.k_scale.view(torch.uint8)[ids, :, slots] = factors.to(torch.uint8).cuda()
+            self.k[n] = f4.values(codes, factors)
+
+    def slopes(self, each):
+        """rows whose scores change by each[h % len] powers of two every 128 keys, at scale d^-0.5"""
+        s = torch.tensor(each, dtype=torch.float64).repeat(self.Hkv) * 0.6931471805599453 * self.d ** -0.5
+        q = (s[:, None] * self.way + 0.02 * torch.randn(self.T, s.numel(), self.d, generator=self.gen, dtype=torch.float64)).bfloat16()
+        return q.cuda(), q.double()
+
+
+@pytest.mark.parametrize("d,qs,kvs,window", [(64, [1, 2, 1], [1200, 900, 1280], 0), (128, [1, 1], [640, 513], 0), (128, [1, 1, 130], [3000, 2500, 200], 0), (256, [1, 1], [300, 3000], 0), (64, [1, 3, 1], [2000, 3000, 700], 1100)])
+def test_scores_that_rise_along_a_context(d, qs, kvs, window):
+    """Sums are rescaled where a maximum has grown by 2^8 since it was last taken: here by a little less and by a little more between two steps of a wave (128 or 256 keys), by far more and not
+    at all, beside each other, in one piece and in several, with waves and pieces whose maxima are far apart."""
+    b = Rising(qs, kvs, 2, d, page=32, seed=d + len(kvs))
+    q, q64 = b.slopes([3.9, 7.9, 8.1, 20.0, 100.0, -5.0, -40.0, 0.5])
+    o = b.attend(q, window=window, max_q=max(qs), max_kv=max(kvs))
+    for n, (m, kv) in enumerate(zip(qs, kvs)):
+        if m <= 4:
+            lo = int(b.cu_host[n])
+            want, size, top = ref.attention(q64[lo:lo + m], b.k[n], b.v[n], kv - m, d ** -0.5, window)
+            near(o[lo:lo + m], want, attention_roundings.bound(want, size, top, d, kv), "d %d seq %d (%d of %d)" % (d, n, m, kv))
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("scale", [1.0, 1e-3])
+def test_large_keys(d, scale):
+    """Scores in the hundreds, in no order.  Beside the usual bound: a weight under 2^-126 of the row's largest, fp32's least normal number, may count as nothing, and so may either of its bf16 terms;
+    the weights sum to one or more, so that the output is off by 3 * 2^-126 of the largest value for each key at most (which shows where the heaviest keys' values are exactly zero)."""
+    qs, kvs = [1, 2, 60], [1300, 3000, 300]
+    b = Batch4(qs, kvs, 1, d, page=64, seed=d, k_size=30.0)
+    q, q64 = b.rows(8)
+    o = b.attend(q, scale=scale)
+    for n, (m, kv) in enumerate(zip(qs, kvs)):
+        lo = int(b.cu_host[n])
+        want, size, top = ref.attention(q64[lo:lo + m], b.k[n], b.v[n], kv - m, scale, 0)
+        near(o[lo:lo + m], want, ref.attention_bound(want, size, top, d, kv, "bf16") + 3 * kv * 2.0 ** -126 * b.v[n].abs().max(), "d %d seq %d" % (d, n))
