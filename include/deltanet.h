@@ -341,7 +341,8 @@ int deltanet_paged_attn_fwd(const dn_paged_shape *shape, const void *q, const dn
 /*
  * Around a mixer: the short convolution in front of it, the norm of its output with its gate, and what stands between two blocks.  The conventions at the top hold; rows
  * may be strided where a stride is given (elements, a multiple of 16 bytes), so that inputs and gradients may be column blocks of a projection's; other tensors are contiguous.
- * Sums are fp32 and in an order that the sizes alone decide.
+ * Sums are fp32 and in an order that the sizes, and of packed sequences the offsets, decide.  Sigmoids are those of the hardware's exponential and reciprocal: within (|g| + 16) 2^-24 of their value, and
+ * zero in the place of one under 2^-126.
  *
  * Short convolution.  Causal and per channel, with W taps (2, 3 or 4; the last one meets the present row): with X_t the sequence's rows, in front of its first row those of
  * initial_state (zeros where there is none),

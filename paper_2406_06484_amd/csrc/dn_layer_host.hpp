@@ -56,7 +56,7 @@ int short_conv_bwd_blocks(int dtype, const ConvArgs &a);
 int out_norm_bwd_blocks(int dtype, int d, int T, int H);
 int block_norm_bwd_blocks(int dtype, int T, int D);
 
-// Sums `count` partial vectors of n elements, in their order: the first n1 of a vector go to out1, the others to out2 (null: not wanted).
+// Sums `count` partial vectors of n elements, in an order that count and n decide (some threads an element, each with every so manieth vector, joined in turn): the first n1 of a vector go to out1, the others to out2 (null: not wanted).
 int run_sum_partials(const float *partial, int count, long n, long n1, float *out1, float *out2, hipStream_t stream);
 
 } // namespace dn

@@ -78,7 +78,7 @@ __device__ inline void partial_of(const AttnArgs &a, int split, long row, int D,
 // holds a sixteenth of the elements of the eight keys whose probabilities it has, one 16-byte piece (or less) of each 16, from l % 16 on, which a 16-bit
 // transposition among its own registers turns into the operands of D / 16 products.  (So the lanes of one load stand side by side.)  No LDS traffic and no barrier until the waves of a workgroup, which share out the
 // keys of one split, join their sums.  32 sequences of 16 heads of 128 over up to 2048 keys in bf16 (374 MB): 72 us, 5.2 TB/s; one over 32768 e4m3 keys of 4 heads (34 MB):
-// 11 us and 4 for the join; one over 131072 in 4 bits (71 MB) 16 us, and 32 over up to 8192 (91 MB) 23, the vector ALU busy for a quarter of it.
+// 11 us and 4 for the join; one over 131072 in 4 bits (71 MB) 17 us, and 32 over up to 8192 (91 MB) 26, the vector ALU busy for 0.28 of it.
 constexpr int kFewTile = 16, kFewKeys = 32, kFewWaves = 4;
 // Twice as many waves per workgroup where there are few workgroups, if their registers allow it.
 template <typename T> constexpr bool few_twice(int d) { return d * sizeof(T) <= 256; }
@@ -116,7 +116,8 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
     constexpr int KW = KB / 4, VW = VB < 4 ? 1 : VB / 4; // in words
     constexpr int KP = KB < 16 ? KB : 16, KV = KP * D / RB; // bytes, elements of a piece of a key: (4 piece + g) KV ..
     constexpr int VV = VB > 16 ? 16 * D / RB : VE;      // ... and of a value: (16 piece + col) VV ..
-    // 4-bit pages bring so many keys per byte that the vector ALU's work shows beside the reading: sums are rescaled only when a row's maximum has grown by 2^8.
+    // 4-bit pages bring so many keys per byte that the vector ALU's work shows beside the reading: sums are rescaled only when a row's maximum has grown by 2^8 (32 contexts of up to 8192 keys, 4 heads of 128, with
+    // their append: 30.8 us instead of 31.4).
     constexpr bool LAZY = FP4;
     constexpr int FB = FP4 ? D / kGroup : 1, FW = FP4 ? FB : 1; // factors of a row; words with those of four rows
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
@@ -323,7 +324,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
         } else {
             // Probabilities as two bf16 terms: the products wait for memory anyway, and the output then carries the one rounding of its own (in one
             // term, 1.4 times its error).  Over 4-bit pages, which are read in a third of the time, the second term costs 4 to 6 % (32 contexts of up to 8192 keys,
-            // 4 heads of 128, with their append: 30.5 us instead of 28.8).
+            // 4 heads of 128, with their append: 30.8 us instead of 29).
             bf16x8 pt, pl;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -958,7 +959,9 @@ Plan plan_attn(int dtype, int d, const AttnArgs &a) {
     // 640 0.98, 0.96, 0.97.  (Between 256 and 512 ragged batches go either way: at 320 0.89, 0.92, 1.07.)
     const bool twice = !p.slots && (dtype == 0 ? few_twice<float>(d) : few_twice<bf16>(d)) && (blocks <= 256 || blocks >= 512) && seen > kFewWaves * kFewKeys;
     p.waves = twice ? 2 * kFewWaves : kFewWaves;
-    // (4-bit pages: two workgroups of eight waves per CU, whose loads bring a quarter of the bytes: 32 contexts of up to 8192 keys, 4 heads of 128, with their append 31 us instead of 35.)
+    // (4-bit pages: two workgroups of eight waves per CU, whose loads bring a quarter of the bytes.  512 instead of 256, with the append, 4 heads of 128: 32 contexts of up to 8192 keys 30.8 us instead of
+    // 32.4, 8 of up to 32768 32.0 instead of 33.7, 33 of up to 8192 36.9 instead of 47.2.  Where 256 would leave 129 to 256 contexts and heads whole, it costs a join, which short contexts and equal ones near 256
+    // do not bring back: 50 contexts of up to 4000 keys 31.2 instead of 26.6, of 16384 each 101.6 instead of 93.7, of up to 16384 88.1 instead of 89.3.)
     const long want = twice && !a.c.fp4 ? 256 : 512;
     p.few = p.per_seq && N ? cut_keys(seen, blocks, 64 * blocks < want ? 64 * blocks : want, least > 256 ? least : 256, kFewKeys * p.waves) : Cut{1, 128};
     return p;

@@ -6,7 +6,7 @@
 // A sequence's W - 1 last rows are its final_state; rows in front of it take their gradient to dinitial_state, and a gradient with respect to final_state is
 // added to those rows' own.  z is formed again in the backward pass (W products an element, where keeping it would be another tensor of traffic).
 //
-// Bound by HBM: 16384 rows of 6144 channels in bf16 take 71 us forward (403 MB, 5.7 TB/s) and 117 backward (604 MB, 5.2 TB/s) and 4 for the weights' sums.  Workgroups that follow each other have neighbouring columns of the same
+// Bound by HBM: 16384 rows of 6144 channels in bf16 take 72 us forward (403 MB, 5.6 TB/s), 124 backward (604 MB, 4.9 TB/s) and 5 for the weights' sums under a trace, 193 together without (5.2 TB/s).  Workgroups that follow each other have neighbouring columns of the same
 // rows, so that what is under way at a time is whole rows (the other way round, with a kilobyte of a row each, 237 us for both passes instead of 218), and outputs are stored past the caches (193).
 // A wave has V channels per lane and walks down a strip of a sequence's rows with the W - 1 rows behind it in registers, so that a row is fetched once, and W - 1
 // more at the ends of a strip.  Strips are cut from each sequence's start: strip i of sequence n is at slot cu[n] / S + n + i, slots that are left over have
@@ -308,7 +308,7 @@ __global__ __launch_bounds__(256) void k_short_conv_bwd(ConvArgs a, int slots, i
     }
 }
 
-// Sums of partial vectors: E elements a workgroup, 1024 / E threads for each.
+// Sums of partial vectors: E elements a workgroup, P = 1024 / E threads for each, the p-th of which has vectors p, p + P, ..
 template <int E>
 __global__ __launch_bounds__(1024) void k_sum_partials(const float *partial, int count, long n, long n1, float *out1, float *out2) {
     constexpr int P = 1024 / E;
