@@ -60,6 +60,9 @@ template <typename T, int D> __device__ inline void zero_rest(const AttnArgs &a,
     }
 }
 
+// By how much a maximum may grow before sums are rescaled: 2^8 of their weights, and whatever the scale, far less than the scores that fp32 holds, so that a row's first one counts as more than kNoScore.
+__device__ inline float score_growth(float c) { return fminf(8.f / c, 0x1p100f); }
+
 // What a sum of weights divides by: nothing where there is nothing, and NaN stays NaN.
 __device__ inline float inverse_sum(float l) { return l > 0.f ? 1.f / l : (l == l ? 0.f : l); }
 
@@ -157,6 +160,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
         }
     }
     const float c = a.scale * kLog2e;
+    const float grown = score_growth(c);
 
     const char *kp = static_cast<const char *>(a.c.kp), *vp = static_cast<const char *>(a.c.vp);
     int page[2];
@@ -276,7 +280,7 @@ __device__ __forceinline__ void attend_few(const AttnArgs &a, int tiles, Cut cut
             mt = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
         }
         const float mn = fmaxf(m, mt);
-        if (LAZY ? __any((mt - m) * c > 8.f) : __any(mn > m)) {
+        if (LAZY ? __any(mt - m > grown) : __any(mn > m)) {
             const float f = __builtin_amdgcn_exp2f((m - mn) * c);
             l *= f;
 #pragma unroll
@@ -536,6 +540,7 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
     // A score's exponent is c s - off, one operation, where c m is rounded by a small part of a power of two (the same for all of a row's scores); with a row
     // whose scores are larger, the wave subtracts m first.  (off is finite also before the first key: masked scores are -infinity.)
     float m = kNoScore, l = 0.f, off;
+    const float grown = score_growth(c);
     bool far;
     auto set_off = [&]() __attribute__((always_inline)) { off = fmaxf(m * c, kNoScore); far = __any(m > kNoScore && fabsf(off) > kFarScore); };
     set_off();
@@ -675,8 +680,8 @@ __device__ __forceinline__ void attend_wide(const AttnArgs &a, Cut cut, int few,
             const auto x = __builtin_amdgcn_permlane32_swap(u, u, false, false);
             mt = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
         }
-        // m need not be the maximum, only near it: sums are rescaled when a row's has grown by 2^8 or more
-        if (__any((mt - m) * c > 8.f)) {
+        // m need not be the maximum, only near it: sums are rescaled when a row's has grown by more than 2^8
+        if (__any(mt - m > grown)) {
             const float mn = fmaxf(m, mt), f = __builtin_amdgcn_exp2f((m - mn) * c);
             l *= f;
 #pragma unroll

@@ -6,8 +6,9 @@ import paper_2406_06484_amd as dn
 from tests import attention_reference as ref
 from tests import attention_roundings
 from tests import fp4_reference as f4
-from tests.attention_util import near, replays
+from tests.attention_util import Batch, near, replays
 from tests.fp4_reference import Batch4
+from tests.test_gpu_attention_scores import _put
 
 pytestmark = pytest.mark.gpu
 
@@ -226,6 +227,16 @@ def test_few_rows_carry_two_terms(d, qs, kvs):
             near(o[lo:lo + m], want, attention_roundings.bound(want, size, top, d, kv), "d %d seq %d (%d of %d)" % (d, n, m, kv))
 
 
+def put(b, n, x):
+    """gives sequence n the keys x (float64 [kv, Hkv, d]), as 4 bits hold them"""
+    codes, factors = f4.quantise(x)
+    p = torch.arange(b.kvs[n])
+    ids, slots = b.table_host[n].long()[p // b.page].cuda(), (p % b.page).cuda()
+    b.k_pages.view(torch.uint8)[ids, :, slots] = f4.packed(codes).cuda()
+    b.k_scale.view(torch.uint8)[ids, :, slots] = factors.to(torch.uint8).cuda()
+    b.k[n] = f4.values(codes, factors)
+
+
 class Rising(Batch4):
     """Scores that climb or fall along the contexts: key j is j / 128 times a direction, and some noise; rows(..) of it are this direction with a slope per head."""
 
@@ -235,11 +246,7 @@ class Rising(Batch4):
         for n, kv in enumerate(kvs):
             p = torch.arange(kv)
             x = (p / 128.0)[:, None, None] * self.way + 0.2 * torch.randn(kv, Hkv, d, generator=self.gen, dtype=torch.float64)
-            codes, factors = f4.quantise(x.bfloat16().double())
-            ids, slots = self.table_host[n].long()[p // self.page].cuda(), (p % self.page).cuda()
-            self.k_pages.view(torch.uint8)[ids, :, slots] = f4.packed(codes).cuda()
-            self.k_scale.view(torch.uint8)[ids, :, slots] = factors.to(torch.uint8).cuda()
-            self.k[n] = f4.values(codes, factors)
+            put(self, n, x.bfloat16().double())
 
     def slopes(self, each):
         """rows whose scores change by each[h % len] powers of two every 128 keys, at scale d^-0.5"""
@@ -275,3 +282,48 @@ def test_large_keys(d, scale):
         lo = int(b.cu_host[n])
         want, size, top = ref.attention(q64[lo:lo + m], b.k[n], b.v[n], kv - m, scale, 0)
         near(o[lo:lo + m], want, ref.attention_bound(want, size, top, d, kv, "bf16") + 3 * kv * 2.0 ** -126 * b.v[n].abs().max(), "d %d seq %d" % (d, n))
+
+
+SCORES = [([1, 4], [70, 300], 0), ([1], [5000], 0), ([1, 50, 130], [70, 300, 260], 0), ([150], [1700], 40), ([140, 140], [3000, 2500], 0)]
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("qs,kvs,window", SCORES)
+@pytest.mark.parametrize("size,sign", [(18, 1), (18, -1), (54, 1), (54, -1)])
+def test_the_largest_score_takes_all(d, qs, kvs, window, size, sign):
+    """As over 16- and 8-bit pages: queries and keys along one axis, scores equal or 2^20 and more apart, so that the output is the mean of the largest ones' values."""
+    b = Batch4(qs, kvs, 2, d, page=16, seed=size)
+    for n, kv in enumerate(kvs):
+        k = torch.zeros(kv, 2, d, dtype=torch.float64)
+        for h in range(2):
+            k[:, h, 0] = sign * f4.LEVELS[2:][torch.randint(0, 6, (kv,), generator=b.gen)] * torch.exp2(size + torch.randint(0, 4, (kv,), generator=b.gen).double())
+        put(b, n, k)
+    q = torch.zeros(b.T, 4, d, dtype=torch.float64)
+    q[..., 0] = 2.0 ** size
+    o = b.attend(q.bfloat16().cuda(), window=window, max_q=max(qs), max_kv=max(kvs)).double().cpu()
+    for n, (m, kv) in enumerate(zip(qs, kvs)):
+        for i in range(m):
+            lo, hi = max(0, kv - m + i - window + 1) if window else 0, kv - m + i + 1
+            for h in range(4):
+                k, v = b.k[n][lo:hi, h // 2, 0], b.v[n][lo:hi, h // 2]
+                want = v[k == k.max()].mean(0)
+                assert ((o[int(b.cu_host[n]) + i, h] - want).abs() <= 2.0 ** -8 * v.abs().max()).all(), (n, i, h)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8", "fp4"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("qs,kvs", [([1], [600]), ([1, 3], [5000, 900]), ([1, 2, 130], [3000, 200, 260]), ([40, 40], [2500, 700])])
+def test_scores_up_to_the_largest_numbers_under_the_least_scale(cache, d, qs, kvs):
+    """Scores of 0 to 3 * 2^125, rising along the contexts, times 2^-126: weights of one size."""
+    if cache == "fp4":
+        b = Batch4(qs, kvs, 1, d, page=16, seed=d)
+    else:
+        b = Batch(qs, kvs, 1, d, "bf16", cache, 16, seed=d, junk=0.0)
+    for n, kv in enumerate(kvs):
+        k = torch.zeros(kv, 1, d, dtype=torch.float64)
+        k[:, 0, 0] = torch.tensor([0.0, 0.5, 1.0, 2.0, 3.0], dtype=torch.float64)[torch.arange(kv) * 5 // kv] * 2.0 ** 62
+        put(b, n, k) if cache == "fp4" else _put(b, n, k)
+    q = torch.zeros(b.T, 4, d, dtype=torch.float64)
+    q[..., 0] = 2.0 ** 63
+    o = b.attend(q.bfloat16().cuda(), scale=2.0 ** -126, max_q=max(qs), max_kv=max(kvs))
+    b.check(o, q, 2.0 ** -126, 0, "%s d %d" % (cache, d))
